@@ -307,6 +307,57 @@ int agrl_token_logprob_noalloc(int64_t T, int64_t max_act, int32_t d, int32_t V,
                                const uint8_t* action_mask, const agrl_options* opt, float* logp,
                                float* lse, void* stream);
 
+/*
+ * Layer or RMS norm of token rows: the final norm whose output is the policy
+ * loss's H, and (backward) which takes its dH.  Per live row
+ *   AGRL_NORM_LAYER  mean = (1/d) sum x, var = (1/d) sum (x - mean)^2,
+ *                    rstd = 1/sqrt(var + eps), y = (x - mean) rstd weight + bias
+ *   AGRL_NORM_RMS    rstd = 1/sqrt((1/d) sum x^2 + eps), y = x rstd weight + bias
+ * Statistics, products and sums are fp32; y is rounded once to `dtype`.
+ *   T, d             rows and row length, 1 <= d <= 16384 (AGRL_E_UNSUPPORTED above)
+ *   dtype, w_dtype   type of x and y, and of weight and bias: AGRL_BF16 or AGRL_F32
+ *   x[T, d]          rows ld_x >= d elements apart; y likewise with ld_y
+ *   weight, bias[d]  NULL: 1, and 0
+ *   action_mask[T]   uint8; NULL: every row is live.  Rows with mask 0 are never
+ *                    read; their y is +0, their mean and rstd 0
+ *   eps              finite, >= 0
+ * Outputs: y, mean[T] (layer; NULL: not written), rstd[T] (NULL: not written).
+ * x, y and the parameters may start at any element.  y may be x itself (the
+ * same pointer and stride); arrays that overlap in another way are not
+ * supported.  A constant row has y = bias up to rounding (layer).  A NaN
+ * or infinite element makes its own row NaN and no other.
+ */
+enum { AGRL_NORM_LAYER = 0, AGRL_NORM_RMS = 1 };
+int agrl_token_norm_fwd(int64_t T, int32_t d, int32_t kind, int32_t dtype, int32_t w_dtype,
+                        const void* x, int64_t ld_x, const void* weight, const void* bias,
+                        const uint8_t* action_mask, float eps, void* y, int64_t ld_y, float* mean,
+                        float* rstd, void* stream);
+
+/* Bytes of workspace for agrl_token_norm_bwd's sums over rows; 0 for invalid
+ * sizes.  Host-only. */
+size_t agrl_token_norm_bwd_workspace_size(int64_t T, int32_t d);
+
+/*
+ * Backward of agrl_token_norm_fwd.  With xh = (x - mean) rstd (RMS: x rstd) and
+ * g = dy weight:
+ *   dx      = rstd (g - (1/d) sum g - xh (1/d) sum (g xh))   (RMS: without sum g)
+ *   dweight = sum over live rows of dy xh,  dbias = sum over live rows of dy
+ *   dy[T, d]      in dy_dtype (the policy loss's dH is AGRL_F32), rows ld_dy apart
+ *   mean, rstd    as the forward left them (mean is not read for RMS)
+ *   accumulate    0: dweight and dbias are overwritten, 1: added to
+ *   workspace     4-byte aligned; not needed when dweight and dbias are NULL
+ * Outputs: dx[T, d] in `dtype`, rows ld_dx apart (+0 on masked rows, whose x, dy,
+ * mean and rstd are never read); dweight[d], dbias[d] fp32 (NULL: not formed).
+ * With T = 0, or no live row, dweight and dbias are 0 (or keep their values).
+ * dx may be x or dy itself where type and stride agree.
+ */
+int agrl_token_norm_bwd(int64_t T, int32_t d, int32_t kind, int32_t dtype, int32_t w_dtype,
+                        int32_t dy_dtype, const void* x, int64_t ld_x, const void* weight,
+                        const uint8_t* action_mask, const void* dy, int64_t ld_dy,
+                        const float* mean, const float* rstd, int32_t accumulate, void* workspace,
+                        size_t ws_bytes, void* dx, int64_t ld_dx, float* dweight, float* dbias,
+                        void* stream);
+
 /* Text for a status code (static storage). */
 const char* agrl_status_string(int status);
 

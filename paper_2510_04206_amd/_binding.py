@@ -18,6 +18,8 @@ LIB_PATH = os.path.join(_HERE, "libagrl.so")
 
 AGRL_BF16 = 0
 AGRL_F32 = 1
+AGRL_NORM_LAYER = 0
+AGRL_NORM_RMS = 1
 AGRL_NOALLOC_SCRATCH_BYTES = 64 << 20     # include/agrl.h
 ERROR_BITS = {1: "token id out of range", 2: "trajectory id out of range",
               4: "task id out of range", 8: "group id out of range",
@@ -61,6 +63,12 @@ _SIGS = {
     "agrl_token_logprob_noalloc": (_c_i32, [_c_i64, _c_i64, _c_i32, _c_i32, _c_i32, _c_p, _c_p,
                                             _c_p, _c_p, _c_p, _c_p, _c_p, _c_p]),
     "agrl_sequence_mean_weights": (_c_i32, [_c_i64, _c_i32, _c_p, _c_p, _c_p, _c_p, _c_p]),
+    "agrl_token_norm_fwd": (_c_i32, [_c_i64, _c_i32, _c_i32, _c_i32, _c_i32, _c_p, _c_i64, _c_p,
+                                     _c_p, _c_p, _c_f32, _c_p, _c_i64, _c_p, _c_p, _c_p]),
+    "agrl_token_norm_bwd_workspace_size": (_c_sz, [_c_i64, _c_i32]),
+    "agrl_token_norm_bwd": (_c_i32, [_c_i64, _c_i32, _c_i32, _c_i32, _c_i32, _c_i32, _c_p, _c_i64,
+                                     _c_p, _c_p, _c_p, _c_i64, _c_p, _c_p, _c_i32, _c_p, _c_sz,
+                                     _c_p, _c_i64, _c_p, _c_p, _c_p]),
     "agrl_status_string": (ctypes.c_char_p, [_c_i32]),
     "agrl_last_error": (ctypes.c_char_p, []),
     "agrl_get_device_error": (_c_i32, [_c_p, _c_p]),
@@ -94,6 +102,18 @@ def _ptr(t: Optional[torch.Tensor]):
         raise ValueError("agrl: arrays must be GPU tensors (the ABI takes device pointers)")
     if not t.is_contiguous():
         raise ValueError("agrl: arrays must be contiguous (the ABI takes plain pointers)")
+    return ctypes.c_void_p(t.data_ptr())
+
+
+def _rows(t: Optional[torch.Tensor]):
+    """Device address of a GPU tensor whose last dimension is contiguous (the ABI takes the
+    distance between its rows)."""
+    if t is None:
+        return None
+    if not t.is_cuda:
+        raise ValueError("agrl: arrays must be GPU tensors (the ABI takes device pointers)")
+    if t.shape[-1] > 1 and t.stride(-1) != 1:
+        raise ValueError("agrl: the elements of a row must be adjacent")
     return ctypes.c_void_p(t.data_ptr())
 
 
@@ -188,6 +208,26 @@ def agrl_sequence_mean_weights(T, n_traj, traj_id, action_mask, seq_count, token
     _check("agrl_sequence_mean_weights", lib().agrl_sequence_mean_weights(
         T, n_traj, _ptr(traj_id), _ptr(action_mask), _ptr(seq_count), _ptr(token_weight),
         _stream(stream)))
+
+
+def agrl_token_norm_fwd(T, d, kind, dtype, w_dtype, x, ld_x, weight, bias, action_mask, eps, y,
+                        ld_y, mean, rstd, stream=None) -> None:
+    _check("agrl_token_norm_fwd", lib().agrl_token_norm_fwd(
+        T, d, kind, dtype, w_dtype, _rows(x), ld_x, _ptr(weight), _ptr(bias), _ptr(action_mask),
+        eps, _rows(y), ld_y, _ptr(mean), _ptr(rstd), _stream(stream)))
+
+
+def agrl_token_norm_bwd_workspace_size(T, d) -> int:
+    return int(lib().agrl_token_norm_bwd_workspace_size(T, d))
+
+
+def agrl_token_norm_bwd(T, d, kind, dtype, w_dtype, dy_dtype, x, ld_x, weight, action_mask, dy,
+                        ld_dy, mean, rstd, accumulate, workspace, ws_bytes, dx, ld_dx, dweight,
+                        dbias, stream=None) -> None:
+    _check("agrl_token_norm_bwd", lib().agrl_token_norm_bwd(
+        T, d, kind, dtype, w_dtype, dy_dtype, _rows(x), ld_x, _ptr(weight), _ptr(action_mask),
+        _rows(dy), ld_dy, _ptr(mean), _ptr(rstd), accumulate, _ptr(workspace), ws_bytes, _rows(dx),
+        ld_dx, _ptr(dweight), _ptr(dbias), _stream(stream)))
 
 
 def agrl_get_device_error(stream=None) -> int:

@@ -7,6 +7,44 @@ import torch
 
 from . import _binding as B
 
+_CODES = {torch.bfloat16: B.AGRL_BF16, torch.float32: B.AGRL_F32}
+
+
+def _need(t: torch.Tensor, name: str, shape, dtypes) -> None:
+    """The binding sees only addresses: what a tensor must be is checked here."""
+    if tuple(t.shape) != tuple(shape):
+        raise ValueError(f"agrl: {name} has shape {tuple(t.shape)}, expected {tuple(shape)}")
+    if t.dtype not in dtypes:
+        raise TypeError(f"agrl: {name} has dtype {t.dtype}, expected one of {dtypes}")
+
+
+def _row_stride(t: torch.Tensor) -> int:
+    """Elements between rows (a single row has no neighbour: its own length)."""
+    return t.stride(-2) if t.shape[-2] > 1 else max(t.shape[-1], 1)
+
+
+class _Owned:
+    """Buffers of a handle and the stream they were made on.  A call on another stream first
+    waits for that one (once per stream), and the allocator is told of the use."""
+
+    def __init__(self, device):
+        self.device = torch.device(device)
+        self._made_on = torch.cuda.current_stream(self.device)
+        self._seen = {self._made_on.cuda_stream}
+
+    def _on(self, stream, buffers):
+        raw = (torch._C._cuda_getCurrentRawStream(self._made_on.device_index) if stream is None
+               else stream.cuda_stream)
+        # (a capture cannot wait for work outside it; whoever captures has synchronised before)
+        if raw in self._seen or torch.cuda.is_current_stream_capturing():
+            return
+        use = stream if stream is not None else torch.cuda.current_stream(self.device)
+        use.wait_stream(self._made_on)
+        for b in buffers:
+            if b is not None:
+                b.record_stream(use)
+        self._seen.add(raw)
+
 
 def task_adv_norm(traj_id: torch.Tensor, action_mask: torch.Tensor, traj_task: torch.Tensor,
                   traj_group: Optional[torch.Tensor], reward: torch.Tensor, n_task: int,
@@ -122,3 +160,70 @@ class TokenLogprob:
                              action_mask, self.opt, self.workspace, self.ws_bytes, self.logp,
                              self.lse, stream)
         return self.logp, self.lse
+
+
+class TokenNorm(_Owned):
+    """Layer or RMS norm of T token rows of d, forward and backward (agrl_token_norm_*).
+
+    Holds its outputs and the workspace, so repeated steps allocate nothing.  ``forward``
+    returns (y, mean, rstd), mean None for kind "rms"; ``backward`` reads the mean and rstd of
+    the last forward and returns (dx, dweight, dbias), dbias None for kind "rms" unless
+    ``bias_grad``.  Rows of x and dy may lie further apart than their length.  grads=False
+    leaves the backward's buffers out.
+    """
+
+    def __init__(self, T: int, d: int, dtype: torch.dtype, kind: str = "layer", eps: float = 1e-5,
+                 grads: bool = True, bias_grad: Optional[bool] = None, device="cuda"):
+        super().__init__(device)
+        if kind not in ("layer", "rms"):
+            raise ValueError("agrl: kind is 'layer' or 'rms'")
+        if dtype not in _CODES:
+            raise TypeError(f"unsupported dtype {dtype}")
+        self.T, self.d, self.dtype, self.eps = int(T), int(d), dtype, float(eps)
+        self.kind = B.AGRL_NORM_LAYER if kind == "layer" else B.AGRL_NORM_RMS
+        new = lambda *n, dt=torch.float32: torch.empty(n, dtype=dt, device=self.device)  # noqa: E731
+        self.y = new(self.T, self.d, dt=dtype)
+        self.mean = new(self.T) if kind == "layer" else None
+        self.rstd = new(self.T)
+        self.dx = self.dweight = self.dbias = self.workspace = None
+        self.ws_bytes = 0
+        if grads:
+            self.ws_bytes = B.agrl_token_norm_bwd_workspace_size(self.T, self.d)
+            self.workspace = new(max(self.ws_bytes, 4), dt=torch.uint8)
+            self.dx = new(self.T, self.d, dt=dtype)
+            self.dweight = new(self.d)
+            if bias_grad or (bias_grad is None and kind == "layer"):
+                self.dbias = new(self.d)
+
+    def _check(self, x, weight, action_mask):
+        _need(x, "x", (self.T, self.d), (self.dtype,))
+        if weight is not None:
+            _need(weight, "weight", (self.d,), _CODES)
+        if action_mask is not None:
+            _need(action_mask, "action_mask", (self.T,), (torch.uint8,))
+
+    def forward(self, x, weight=None, bias=None, action_mask=None, stream=None):
+        self._check(x, weight, action_mask)
+        par = weight if weight is not None else bias
+        if bias is not None:
+            _need(bias, "bias", (self.d,), (par.dtype,))
+        self._on(stream, (self.y, self.mean, self.rstd))
+        B.agrl_token_norm_fwd(self.T, self.d, self.kind, _CODES[self.dtype],
+                              B.AGRL_F32 if par is None else _CODES[par.dtype], x, _row_stride(x),
+                              weight, bias, action_mask, self.eps, self.y, self.d, self.mean,
+                              self.rstd, stream)
+        return self.y, self.mean, self.rstd
+
+    def backward(self, x, weight, dy, action_mask=None, accumulate: bool = False, stream=None):
+        if self.dx is None:
+            raise ValueError("agrl: this TokenNorm was made with grads=False")
+        self._check(x, weight, action_mask)
+        _need(dy, "dy", (self.T, self.d), _CODES)
+        self._on(stream, (self.mean, self.rstd, self.workspace, self.dx, self.dweight, self.dbias))
+        B.agrl_token_norm_bwd(self.T, self.d, self.kind, _CODES[self.dtype],
+                              B.AGRL_F32 if weight is None else _CODES[weight.dtype],
+                              _CODES[dy.dtype], x, _row_stride(x), weight, action_mask, dy,
+                              _row_stride(dy), self.mean, self.rstd, int(accumulate),
+                              self.workspace, self.ws_bytes, self.dx, self.d, self.dweight,
+                              self.dbias, stream)
+        return self.dx, self.dweight, self.dbias

@@ -10,15 +10,16 @@ import sys
 HERE = os.path.dirname(os.path.abspath(__file__))
 CSRC = os.path.join(HERE, "csrc")
 LIB = os.path.join(HERE, "libagrl.so")
-SOURCES = ["abi.hip", "adv_norm.hip", "policy_loss.hip", "noalloc.hip"]
+SOURCES = ["abi.hip", "adv_norm.hip", "policy_loss.hip", "noalloc.hip", "norm.hip"]
 ARCH = "gfx950"
 
 COMMON = ["-O3", "-std=c++17", "-fPIC", f"--offload-arch={ARCH}",
           # never emit packed fp32 VALU instructions
           "-Xclang", "-target-feature", "-Xclang", "-packed-fp32-ops",
           "-Wno-unused-command-line-argument"]
-# per-file extras: the advantage statistics must be one rounding per operation
-EXTRA = {"adv_norm.hip": ["-ffp-contract=off"]}
+# per-file extras: the advantage statistics must be one rounding per operation, and the norms'
+# differences must be taken from the mean as it was rounded
+EXTRA = {"adv_norm.hip": ["-ffp-contract=off"], "norm.hip": ["-ffp-contract=off"]}
 
 
 def hipcc() -> str:
