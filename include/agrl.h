@@ -358,6 +358,62 @@ int agrl_token_norm_bwd(int64_t T, int32_t d, int32_t kind, int32_t dtype, int32
                         size_t ws_bytes, void* dx, int64_t ld_dx, float* dweight, float* dbias,
                         void* stream);
 
+/*
+ * Newton-Schulz orthogonalisation of a stack of `batch` matrices G [m, n]:
+ *   X = G / (|G|_F + eps)
+ *   `steps` times: A = X X^T, B = b A + c A A, X = a X + B X    (m <= n;
+ *   for m > n the same on the transpose, X = a X + X B with A = X^T X)
+ *   O = X
+ * the odd polynomial a s + b s^3 + c s^5 applied to G's singular values, `steps`
+ * times.  The coefficients must keep singular values that start in [0, 1] below
+ * about 3.5: larger ones overflow the operands' range and the result is not finite.
+ */
+typedef struct {
+  int32_t steps;     /* 0 selects 5 */
+  float a, b, c;     /* all 0 selects 3.4445, -4.7750, 2.0315 */
+  float eps;         /* 0 selects 1e-7 */
+} agrl_ns_options;
+
+/* Bytes of workspace for agrl_orthogonalize and agrl_muon_step (out_dtype: the
+ * type of O or of the parameter); 0 for invalid sizes.  Host-only. */
+size_t agrl_orthogonalize_workspace_size(int64_t batch, int64_t m, int64_t n, int32_t out_dtype);
+
+/*
+ *   batch, m, n      0 in any of them enqueues nothing; m, n <= 2^20, the smaller
+ *                    <= 65536, batch <= 65535
+ *   dtype            type of G: AGRL_BF16 or AGRL_F32; rows ld_g >= n elements apart,
+ *                    matrices stride_g apart (not read for batch 1)
+ *   out_dtype        type of O: AGRL_BF16 or AGRL_F32; ld_o, stride_o likewise
+ *   ns               NULL or options (zero-initialised: the defaults)
+ *   workspace        256-byte aligned, agrl_orthogonalize_workspace_size bytes
+ * G and O may start at any element and must not overlap.
+ * Precision goes by out_dtype.  AGRL_F32: products as exact as fp32 ones (each of
+ * three fp16 products of operands split in two).  AGRL_BF16: products of operands
+ * rounded to fp16, the iterate held in 22 bits, fp32 sums; up to 2e-3 of O's norm
+ * besides O's rounding.  |G|_F is summed in 64 bits.  A zero matrix gives 0; a
+ * NaN or infinite entry makes its whole matrix NaN, and no other.
+ */
+int agrl_orthogonalize(int64_t batch, int64_t m, int64_t n, int32_t dtype, const void* G,
+                       int64_t ld_g, int64_t stride_g, int32_t out_dtype,
+                       const agrl_ns_options* ns, void* workspace, size_t ws_bytes, void* O,
+                       int64_t ld_o, int64_t stride_o, void* stream);
+
+/*
+ * One optimiser step for a stack of weight matrices [m, n]:
+ *   momentum <- mu momentum + grad
+ *   u        =  grad + mu momentum (nesterov 1) or momentum (0)
+ *   param    <- (1 - lr weight_decay) param - lr scale O(u)
+ * with O as above.  grad as G above; param [m, n] in param_dtype, updated in place,
+ * rows ld_param and matrices stride_param apart; momentum fp32, contiguous
+ * [batch, m, n], 4-byte aligned.  scale 0 selects sqrt(max(1, m / n)).  A bf16
+ * parameter is rounded to nearest once per step.  The three must not overlap.
+ */
+int agrl_muon_step(int64_t batch, int64_t m, int64_t n, int32_t grad_dtype, const void* grad,
+                   int64_t ld_grad, int64_t stride_grad, int32_t param_dtype, void* param,
+                   int64_t ld_param, int64_t stride_param, float* momentum, float lr, float mu,
+                   int32_t nesterov, float weight_decay, float scale, const agrl_ns_options* ns,
+                   void* workspace, size_t ws_bytes, void* stream);
+
 /* Text for a status code (static storage). */
 const char* agrl_status_string(int status);
 

@@ -38,6 +38,11 @@ class agrl_options(ctypes.Structure):
                 ("drop_uniform_groups", ctypes.c_int32), ("adv_ranges", ctypes.c_void_p)]
 
 
+class agrl_ns_options(ctypes.Structure):
+    _fields_ = [("steps", ctypes.c_int32), ("a", ctypes.c_float), ("b", ctypes.c_float),
+                ("c", ctypes.c_float), ("eps", ctypes.c_float)]
+
+
 class AgrlError(RuntimeError):
     def __init__(self, fn: str, status: int, msg: str):
         super().__init__(f"{fn} failed with status {status}: {msg}")
@@ -69,6 +74,12 @@ _SIGS = {
     "agrl_token_norm_bwd": (_c_i32, [_c_i64, _c_i32, _c_i32, _c_i32, _c_i32, _c_i32, _c_p, _c_i64,
                                      _c_p, _c_p, _c_p, _c_i64, _c_p, _c_p, _c_i32, _c_p, _c_sz,
                                      _c_p, _c_i64, _c_p, _c_p, _c_p]),
+    "agrl_orthogonalize_workspace_size": (_c_sz, [_c_i64, _c_i64, _c_i64, _c_i32]),
+    "agrl_orthogonalize": (_c_i32, [_c_i64, _c_i64, _c_i64, _c_i32, _c_p, _c_i64, _c_i64, _c_i32,
+                                    _c_p, _c_p, _c_sz, _c_p, _c_i64, _c_i64, _c_p]),
+    "agrl_muon_step": (_c_i32, [_c_i64, _c_i64, _c_i64, _c_i32, _c_p, _c_i64, _c_i64, _c_i32,
+                                _c_p, _c_i64, _c_i64, _c_p, _c_f32, _c_f32, _c_i32, _c_f32, _c_f32,
+                                _c_p, _c_p, _c_sz, _c_p]),
     "agrl_status_string": (ctypes.c_char_p, [_c_i32]),
     "agrl_last_error": (ctypes.c_char_p, []),
     "agrl_get_device_error": (_c_i32, [_c_p, _c_p]),
@@ -228,6 +239,30 @@ def agrl_token_norm_bwd(T, d, kind, dtype, w_dtype, dy_dtype, x, ld_x, weight, a
         T, d, kind, dtype, w_dtype, dy_dtype, _rows(x), ld_x, _ptr(weight), _ptr(action_mask),
         _rows(dy), ld_dy, _ptr(mean), _ptr(rstd), accumulate, _ptr(workspace), ws_bytes, _rows(dx),
         ld_dx, _ptr(dweight), _ptr(dbias), _stream(stream)))
+
+
+def agrl_orthogonalize_workspace_size(batch, m, n, out_dtype) -> int:
+    return int(lib().agrl_orthogonalize_workspace_size(batch, m, n, out_dtype))
+
+
+def _ns(ns):
+    return None if ns is None else ctypes.byref(ns)
+
+
+def agrl_orthogonalize(batch, m, n, dtype, G, ld_g, stride_g, out_dtype, ns, workspace, ws_bytes, O,
+                       ld_o, stride_o, stream=None) -> None:
+    _check("agrl_orthogonalize", lib().agrl_orthogonalize(
+        batch, m, n, dtype, _rows(G), ld_g, stride_g, out_dtype, _ns(ns), _ptr(workspace), ws_bytes,
+        _rows(O), ld_o, stride_o, _stream(stream)))
+
+
+def agrl_muon_step(batch, m, n, grad_dtype, grad, ld_grad, stride_grad, param_dtype, param, ld_param,
+                   stride_param, momentum, lr, mu, nesterov, weight_decay, scale, ns, workspace,
+                   ws_bytes, stream=None) -> None:
+    _check("agrl_muon_step", lib().agrl_muon_step(
+        batch, m, n, grad_dtype, _rows(grad), ld_grad, stride_grad, param_dtype, _rows(param),
+        ld_param, stride_param, _ptr(momentum), lr, mu, nesterov, weight_decay, scale, _ns(ns),
+        _ptr(workspace), ws_bytes, _stream(stream)))
 
 
 def agrl_get_device_error(stream=None) -> int:

@@ -227,3 +227,72 @@ class TokenNorm(_Owned):
                               self.workspace, self.ws_bytes, self.dx, self.d, self.dweight,
                               self.dbias, stream)
         return self.dx, self.dweight, self.dbias
+
+
+class _Stack(_Owned):
+    """What Orthogonalize and MuonStep share: a stack of matrices' shape, options and workspace."""
+
+    def __init__(self, m, n, code_of, batch, steps, coeffs, eps, device):
+        super().__init__(device)
+        if code_of not in _CODES:
+            raise TypeError(f"unsupported dtype {code_of}")
+        if steps < 1:
+            raise ValueError("agrl: steps is at least 1")
+        self.m, self.n = int(m), int(n)
+        self.batch = None if batch is None else int(batch)
+        self.shape = (self.m, self.n) if batch is None else (self.batch, self.m, self.n)
+        self.count = 1 if batch is None else self.batch
+        self.dtype, self.code = code_of, _CODES[code_of]
+        a, b, c = (0.0, 0.0, 0.0) if coeffs is None else coeffs
+        self.ns = B.agrl_ns_options(steps=int(steps), a=a, b=b, c=c, eps=eps)
+        self.ws_bytes = B.agrl_orthogonalize_workspace_size(self.count, self.m, self.n, self.code)
+        self.workspace = torch.empty(max(self.ws_bytes, 1), dtype=torch.uint8, device=self.device)
+
+    @staticmethod
+    def _strides(t):
+        return _row_stride(t), (t.stride(0) if t.dim() == 3 else 0)
+
+
+class Orthogonalize(_Stack):
+    """Newton-Schulz orthogonalisation of [m, n] matrices (agrl_orthogonalize), a stack of them
+    with ``batch``.  Holds the workspace and the output; the result's type sets the products'
+    precision.  ``__call__`` takes fp32 or bf16 and returns the output."""
+
+    def __init__(self, m: int, n: int, out_dtype: torch.dtype = torch.bfloat16,
+                 batch: Optional[int] = None, steps: int = 5, coeffs=None, eps: float = 1e-7,
+                 device="cuda"):
+        super().__init__(m, n, out_dtype, batch, steps, coeffs, eps, device)
+        self.out = torch.empty(self.shape, dtype=out_dtype, device=self.device)
+
+    def __call__(self, g, stream=None):
+        _need(g, "g", self.shape, _CODES)
+        self._on(stream, (self.workspace, self.out))
+        B.agrl_orthogonalize(self.count, self.m, self.n, _CODES[g.dtype], g, *self._strides(g),
+                             self.code, self.ns, self.workspace, self.ws_bytes, self.out, self.n,
+                             self.m * self.n, stream)
+        return self.out
+
+
+class MuonStep(_Stack):
+    """One step of the orthogonalised-momentum optimiser for [m, n] weights, or a stack of them
+    (agrl_muon_step).  Holds the workspace; the caller holds the weight and the fp32 momentum,
+    which ``__call__`` updates in place."""
+
+    def __init__(self, m: int, n: int, param_dtype: torch.dtype = torch.float32,
+                 batch: Optional[int] = None, momentum: float = 0.95, nesterov: bool = True,
+                 weight_decay: float = 0.0, scale: float = 0.0, steps: int = 5, coeffs=None,
+                 eps: float = 1e-7, device="cuda"):
+        super().__init__(m, n, param_dtype, batch, steps, coeffs, eps, device)
+        self.mu, self.nesterov = float(momentum), int(bool(nesterov))
+        self.weight_decay, self.scale = float(weight_decay), float(scale)
+
+    def __call__(self, param, grad, momentum, lr: float, stream=None):
+        _need(param, "param", self.shape, (self.dtype,))
+        _need(grad, "grad", self.shape, _CODES)
+        _need(momentum, "momentum", self.shape, (torch.float32,))
+        self._on(stream, (self.workspace,))
+        B.agrl_muon_step(self.count, self.m, self.n, _CODES[grad.dtype], grad, *self._strides(grad),
+                         self.code, param, *self._strides(param), momentum, float(lr), self.mu,
+                         self.nesterov, self.weight_decay, self.scale, self.ns, self.workspace,
+                         self.ws_bytes, stream)
+        return param
