@@ -22,7 +22,6 @@ int fail(int code, const char* fn, const char* what) {
 
 typedef _Float16 f16x8 __attribute__((ext_vector_type(8)));
 typedef _Float16 f16x4 __attribute__((ext_vector_type(4)));
-typedef _Float16 f16x2 __attribute__((ext_vector_type(2)));
 
 // What the matrix cores multiply is fp16 (11 bits), scaled by S so that entries far below the
 // largest keep their bits: |X|, |A|, |B| stay below about 4 for coefficients that keep the
@@ -33,25 +32,41 @@ typedef _Float16 f16x2 __attribute__((ext_vector_type(2)));
 // hi alone: the rounding of the operands to 11 bits leaves 2e-4 to 1.6e-3 relative in the result
 // (the more, the flatter the singular values), which the result's own rounding (1.7e-3) covers.
 // For an fp32 result every operand is hi + lo and a product is three (hi hi + hi lo + lo hi),
-// which is as exact as fp32 products.
+// which is as exact as fp32 products.  Matrices of few rows take that way too: there the
+// roundings average over few entries (33 x 65: 2.0e-3) and the time is latency.
 constexpr float S = 4096.0f;
+constexpr int SPLIT_ROWS = 128;
 
 struct HiLo {
   _Float16 hi, lo;
 };
+// (v as it was rounded to fp32: merged into the conversion, a product or sum that forms v would be
+// rounded once to hi and, for lo, twice, and the two would differ by a unit of hi now and then)
 __device__ __forceinline__ HiLo split(float v) {
+  asm("" : "+v"(v));
   const _Float16 h = (_Float16)v;
   return HiLo{h, (_Float16)(v - (float)h)};
 }
 
-// One stack of matrices in the workspace: plane p (0 hi, 1 lo), matrix z.
+// One stack of matrices in the workspace.  What is multiplied lies in memory as the matrix
+// cores' stages take it, 128 bytes of a row at a time:
+//   one part    64 columns of hi; lo, where it is kept (X), in a plane of its own
+//   two parts   32 columns of hi, then the same 32 of lo
 struct Planes {
   _Float16* at;
-  int64_t plane, matrix;   // elements
-  __host__ __device__ _Float16* get(int p, int64_t z) const { return at + p * plane + z * matrix; }
+  int64_t matrix, lo;      // elements between matrices; from a hi to its lo's plane (one part)
+  int64_t ld;              // columns (padded)
 };
+template <bool SPLIT>
+__device__ __forceinline__ int64_t place(int64_t ld, int64_t row, int64_t col) {
+  return SPLIT ? row * 2 * ld + ((col >> 5) << 6) + (col & 31) : row * ld + col;
+}
+template <bool SPLIT>
+__device__ __forceinline__ int64_t lo_at(const Planes& p) {
+  return SPLIT ? 32 : p.lo;
+}
 
-enum { GRAM, SQUARE, UPDATE };   // A = X X^T; B = bA + cAA + shift I; X = aX + BX
+enum { GRAM, SQUARE, UPDATE, RESULT };   // A = X X^T; B = bA + cAA + shift I; X = aX + BX, twice
 
 // What the last product writes: O, or the weight it updates.
 struct Result {
@@ -64,211 +79,496 @@ struct Result {
 
 struct Args {
   Planes P, Q;        // P: rows of the tile (UPDATE: X, read transposed); Q: columns
-  int64_t ldp, ldq;
-  int32_t K, tiles_m, tiles_n;
+  int32_t K, tiles_m, tiles_n, tiles, items;   // tiles of a matrix, of the stack
   Planes C;           // A, B or the next X
-  int64_t ldc;
   float alpha, beta, shift;   // UPDATE: beta X + P Q; SQUARE: beta A + alpha P Q + shift I
-  int32_t last;
-  Result res;
+  Result res;         // RESULT: in place of C
 };
 
-// A tile of BM x BN by WM x WN waves, each BI x BJ blocks of 16 x 16; NST stages of 64 k in LDS
-template <int WM_, int WN_, int BI_, int BJ_, int NST_>
+// A tile of BM x BN by WM x WN waves, each BI x BJ blocks of 16 x 16; NST stages in LDS, each 128
+// bytes of every row: 64 k, or 32 k in two parts.
+template <int WM_, int WN_, int BI_, int BJ_, int NST_, int PER_CU_>
 struct Tile {
   static constexpr int WM = WM_, WN = WN_, BI = BI_, BJ = BJ_, NST = NST_;
+  static constexpr int PER_CU = PER_CU_;         // workgroups of a compute unit
+  // registers: 256 per lane hold all of a tile up to 128 x 128, and no accumulator then moves
+  // between the two register files
+  static constexpr int EU_WAVES = BI_ * BJ_ <= 16 ? 2 : 1;
   static constexpr int BM = WM * BI * 16, BN = WN * BJ * 16, WAVES = WM * WN;
-  static constexpr int SK = 64, ROW = 2 * SK;
-  static constexpr int P_BYTES = BM * ROW, STAGE = (BM + BN) * ROW;
-  static constexpr int CP = BM / 8 / WAVES, CQ = BN / 8 / WAVES;   // 1 KiB copies per wave
+  static constexpr int HALVES = BM / BN;         // column tiles of a square of BM
+  static constexpr int P_BYTES = BM * 128, STAGE = (BM + BN) * 128;
+  static constexpr int CP = BM / 8 / WAVES, CQ = BN / 8 / WAVES;   // 1 KiB copies of a wave
 };
 
+// Tile t of the lower triangle (rows of tiles 0 .. n - 1, columns up to the row's own), in
+// groups of 8 rows, column by column inside a group: tiles that follow each other share panels.
+__device__ __forceinline__ void triangle_tile(int t, int n, int& tm, int& tn) {
+  int g = 0;
+  while (8 * (g + 1) < n && 32 * (g + 1) * (g + 1) + 4 * (g + 1) <= t) ++g;
+  t -= 32 * g * g + 4 * g;
+  const int h = min(8, n - 8 * g);
+  if (t < 8 * g * h) {
+    tm = 8 * g + t % h;
+    tn = t / h;
+  } else {
+    t -= 8 * g * h;
+    int c = 0;
+    while (t >= h - c) t -= h - c, ++c;
+    tm = 8 * g + c + t;
+    tn = 8 * g + c;
+  }
+}
+
+// Part 0 (hi) or 1 (lo) of four entries, two to a register.
+__device__ __forceinline__ u32x2 packed(const f32x4& v, int part) {
+  f16x4 f;
+#pragma unroll
+  for (int q = 0; q < 4; ++q) {
+    const HiLo s = split(v[q]);
+    f[q] = part ? s.lo : s.hi;
+  }
+  return __builtin_bit_cast(u32x2, f);
+}
+
+// Four lanes with rows 0..3 of a column each -> lane k with row k of the four columns.
+template <int CTRL>
+__device__ __forceinline__ uint32_t quad(uint32_t v) {
+  return (uint32_t)__builtin_amdgcn_update_dpp(0, (int)v, CTRL, 0xf, 0xf, true);
+}
+__device__ __forceinline__ u32x2 quad_transpose(u32x2 v, int lane) {
+  const u32x2 o = {quad<0xb1>(v[0]), quad<0xb1>(v[1])};       // the other lane of the pair
+  const uint32_t sel = lane & 1 ? 0x03020706u : 0x05040100u;  // (other's, own) odd or (own, other's) even
+  const u32x2 w = {__builtin_amdgcn_perm(o[0], v[0], sel), __builtin_amdgcn_perm(o[1], v[1], sel)};
+  const u32x2 t = {quad<0x4e>(w[0]), quad<0x4e>(w[1])};       // the other pair
+  return lane & 2 ? u32x2{t[1], w[1]} : u32x2{w[0], t[0]};
+}
+
+// The same for 32-bit entries.
+__device__ __forceinline__ f32x4 quad_transpose(const f32x4& v, int lane) {
+  uint32_t w[4], o[4];
+#pragma unroll
+  for (int q = 0; q < 4; ++q) o[q] = quad<0xb1>(__float_as_uint(v[q]));
+#pragma unroll
+  for (int h = 0; h < 2; ++h) {      // even lanes: entry 2 h of the pair's columns, odd: 2 h + 1
+    w[2 * h] = lane & 1 ? o[2 * h + 1] : __float_as_uint(v[2 * h]);
+    w[2 * h + 1] = lane & 1 ? __float_as_uint(v[2 * h + 1]) : o[2 * h];
+  }
+#pragma unroll
+  for (int q = 0; q < 4; ++q) o[q] = quad<0x4e>(w[q]);
+  const uint32_t x0 = lane & 2 ? o[2] : w[0], x1 = lane & 2 ? o[3] : w[1];
+  const uint32_t x2 = lane & 2 ? w[2] : o[0], x3 = lane & 2 ? w[3] : o[1];
+  return f32x4{__uint_as_float(x0), __uint_as_float(x1), __uint_as_float(x2), __uint_as_float(x3)};
+}
+
+// The last product's entries: rows r .. r + 3 (16 apart by block i) of column c (by block j) of
+// X, which are four neighbours in a row of the result (behind a transpose of lane quads where X
+// is the result's transpose).  A step reads up to 8 blocks' old values at once.
+template <int BI, int BJ>
+__device__ __forceinline__ void write_result(const Result& o, const f32x4 (&val)[BI][BJ], int z,
+                                             int r0, int c0, int lane) {
+  typedef f32x4 f32x4_a4 __attribute__((aligned(4)));
+  typedef u32x2 u32x2_a2 __attribute__((aligned(2)));
+  constexpr int N = BI * BJ < 8 ? BI * BJ : 8;     // blocks at once
+  float* const out32 = (float*)o.out + (int64_t)z * o.matrix;
+  uint16_t* const out16 = (uint16_t*)o.out + (int64_t)z * o.matrix;
+  static_for<BI * BJ / N>([&](auto part_c) {
+    constexpr int first = decltype(part_c)::value * N;
+    auto place_of = [&](int b, int& row, int& col) {
+      const int r = r0 + 16 * (b / BJ), c = c0 + 16 * (b % BJ);
+      row = o.tall ? r + (lane & 3) : c;
+      col = o.tall ? c - (lane & 3) : r;
+      return (int64_t)row * o.ld + col;
+    };
+    f32x4 old[N];
+    if (o.step)
+      static_for<N>([&](auto b_c) {
+        constexpr int b = decltype(b_c)::value;
+        int row, col;
+        const int64_t to = place_of(first + b, row, col);
+        if (row < o.rows && col + 3 < o.cols) {
+          if (o.f32) {
+            old[b] = *(const f32x4_a4*)(out32 + to);
+          } else {
+            const u32x2 u = *(const u32x2_a2*)(out16 + to);
+            old[b][0] = __uint_as_float(u[0]), old[b][1] = __uint_as_float(u[1]);
+          }
+        } else if (row < o.rows) {
+          uint32_t u[2] = {0, 0};
+#pragma unroll
+          for (int q = 0; q < 3; ++q)
+            if (col + q < o.cols) {
+              if (o.f32)
+                old[b][q] = out32[to + q];
+              else
+                u[q >> 1] |= (uint32_t)out16[to + q] << (16 * (q & 1));
+            }
+          if (!o.f32) old[b][0] = __uint_as_float(u[0]), old[b][1] = __uint_as_float(u[1]);
+        }
+      });
+    static_for<N>([&](auto b_c) {
+      constexpr int b = decltype(b_c)::value;
+      int row, col;
+      const int64_t to = place_of(first + b, row, col);
+      f32x4 w = val[(first + b) / BJ][(first + b) % BJ];
+      if (o.tall) w = quad_transpose(w, lane);
+      w *= 1.0f / S;
+      if (o.step) {
+        f32x4 was = old[b];
+        if (!o.f32) {
+          const uint32_t u0 = __float_as_uint(old[b][0]), u1 = __float_as_uint(old[b][1]);
+          was = f32x4{__uint_as_float(u0 << 16), __uint_as_float(u0 & 0xffff0000u),
+                      __uint_as_float(u1 << 16), __uint_as_float(u1 & 0xffff0000u)};
+        }
+#pragma unroll
+        for (int q = 0; q < 4; ++q) w[q] = fmaf(o.keep, was[q], -o.rate * w[q]);
+      }
+      if (row >= o.rows) return;
+      uint16_t h[4];
+#pragma unroll
+      for (int q = 0; q < 4; ++q) h[q] = f32_to_bf16_bits(w[q]);
+      if (col + 3 < o.cols) {
+        if (o.f32)
+          *(f32x4_a4*)(out32 + to) = w;
+        else
+          *(u32x2_a2*)(out16 + to) =
+              u32x2{h[0] | (uint32_t)h[1] << 16, h[2] | (uint32_t)h[3] << 16};
+      } else {
+#pragma unroll
+        for (int q = 0; q < 3; ++q)
+          if (col + q < o.cols) {
+            if (o.f32)
+              out32[to + q] = w[q];
+            else
+              out16[to + q] = h[q];
+          }
+      }
+    });
+  });
+}
+
+// Fragment reads before slot q of a stage: spread over the first 7/8 of the slots, so that the
+// last ones have come back when the stage ends.
+constexpr int reads_before(int q, int reads, int slots) {
+  return q * reads * 8 / (slots * 7) < reads ? q * reads * 8 / (slots * 7) : reads;
+}
+
+// C = P Q^T, a persistent grid over the tiles of a stack.  The loop keeps a stage's fragments in
+// registers and, between its matrix instructions, reads the next stage's from LDS and starts the
+// copies of the stage NST ahead, so one barrier a stage orders everything: behind it every wave
+// has its fragments of this stage (whose buffer the new copies refill), and the next stage has
+// landed.  Stages run on from a workgroup's tile to its next one (an even number of them per
+// tile: the two register sets alternate), so a tile's first stages arrive under the last
+// products and the epilogue of the tile before.
 template <int MODE, bool SPLIT, class T>
-__global__ void __launch_bounds__(64 * T::WAVES) ns_product_kernel(Args a) {
-  constexpr int BM = T::BM, BN = T::BN, BI = T::BI, BJ = T::BJ, ROW = T::ROW, NST = T::NST;
-  constexpr int CP = T::CP, CQ = T::CQ;
-  constexpr bool TR = MODE == UPDATE;
-  constexpr int TROW = BM * 2;                   // bytes of a k-row of a transposed stage
+__global__ void __launch_bounds__(64 * T::WAVES)
+    __attribute__((amdgpu_waves_per_eu(T::EU_WAVES, T::EU_WAVES))) ns_product_kernel(Args a) {
+  constexpr int BM = T::BM, BN = T::BN, BI = T::BI, BJ = T::BJ, NST = T::NST;
+  constexpr int CP = T::CP, CQ = T::CQ, COPIES = CP + CQ;
+  constexpr bool TR = MODE == UPDATE || MODE == RESULT;
+  constexpr int KROWS = SPLIT ? 32 : 64;         // k of a stage
+  constexpr int TROW = BM * 128 / KROWS;         // bytes of a k-row of a transposed stage
   constexpr int LPR = TROW / 16;                 // lanes of a copy per k-row
   __shared__ __attribute__((aligned(1024))) uint8_t smem[NST * T::STAGE];
   const int lane = threadIdx.x & 63;
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int wm = wave / T::WN, wn = wave % T::WN;
-  const int64_t z = blockIdx.y;
-  int tm, tn;
-  if constexpr (TR) {
-    tm = blockIdx.x % a.tiles_m;
-    tn = blockIdx.x / a.tiles_m;
-  } else {
-    // lower triangle, row by row: tile t is (tm, tn <= tm)
-    const int t = blockIdx.x;
-    tm = (int)((sqrtf(8.0f * (float)t + 1.0f) - 1.0f) * 0.5f);
-    while ((tm + 1) * (tm + 2) / 2 <= t) ++tm;
-    while (tm * (tm + 1) / 2 > t) --tm;
-    tn = t - tm * (tm + 1) / 2;
-  }
-  const int m0 = tm * BM, n0 = tn * BN;
+  // workgroups go to the 8 XCDs in turn: each XCD takes a contiguous run of the tiles, its
+  // workgroups neighbours in it, whose panels its L2 then holds
+  const int nx = min(8, (int)gridDim.x), xcd = blockIdx.x % nx;
+  const int share = a.items / nx, extra = a.items % nx;
+  const int first = xcd * share + min(xcd, extra), end = first + share + (xcd < extra ? 1 : 0);
+  const int stride = (gridDim.x - xcd + nx - 1) / nx;    // workgroups on this XCD
+  struct At {
+    int z, m0, n0, tm, tn;
+  };
+  auto tile_at = [&](int item) {
+    At at;
+    const int t = item % a.tiles;
+    at.z = item / a.tiles;
+    if constexpr (TR) {
+      grouped_tile(t, a.tiles_m, a.tiles_n, 8, at.tm, at.tn);
+    } else {
+      triangle_tile(t / T::HALVES, a.tiles_m, at.tm, at.tn);
+      at.tn = at.tn * T::HALVES + t % T::HALVES;
+    }
+    at.z = __builtin_amdgcn_readfirstlane(at.z);
+    at.tm = __builtin_amdgcn_readfirstlane(at.tm);
+    at.tn = __builtin_amdgcn_readfirstlane(at.tn);
+    at.m0 = at.tm * BM, at.n0 = at.tn * BN;
+    return at;
+  };
+  int item = first + blockIdx.x / nx;
+  if (item >= end) return;
 
   uint32_t offp[CP], offq[CQ];
+  const uint32_t pitch_p = (uint32_t)(place<SPLIT>(a.P.ld, 1, 0) * 2);
+  const uint32_t pitch_q = (uint32_t)(place<SPLIT>(a.Q.ld, 1, 0) * 2);
   // row-major: 8 rows of 128 bytes per copy, chunk c of row r at c ^ ((r >> 1) & 7)
 #pragma unroll
   for (int q = 0; q < CQ; ++q) {
     const int row = (wave * CQ + q) * 8 + (lane >> 3);
-    offq[q] = (uint32_t)(row * (a.ldq * 2)) + (((lane & 7) ^ row_swizzle(row)) << 4);
+    offq[q] = row * pitch_q + (((lane & 7) ^ row_swizzle(row)) << 4);
   }
 #pragma unroll
   for (int q = 0; q < CP; ++q) {
     if constexpr (TR) {
-      // k-rows of BM entries: 64-byte window w of k-row k at w ^ swz(k), its 32-byte halves
-      // swapped when bit 3 of k is set (see the reads below)
+      // k-rows of the tile's rows, 64-byte window w of k-row k at w ^ swz(k), its 32-byte halves
+      // swapped when bit 3 of k is set: the 8 k-rows that half a wave reads (see below) then lie
+      // in 8 distinct parts of the 256 bytes that LDS serves at once
       const int kr = (wave * CP + q) * (64 / LPR) + lane / LPR, p = lane % LPR;
-      const int w = (p >> 2) ^ (BM >= 128 ? kr & 3 : (kr >> 1) & 1);
-      const int col = w * 32 + ((((p >> 1) & 1) ^ ((kr >> 3) & 1)) << 4) + (p & 1) * 8;
-      offp[q] = (uint32_t)(kr * (a.ldp * 2) + col * 2);
+      const int w = (p >> 2) ^ (TROW >= 256 ? kr & 3 : (kr >> 1) & 1);
+      const int half = ((p >> 1) & 1) ^ ((kr >> 3) & 1);
+      offp[q] = kr * pitch_p + w * 64 + half * 32 + (p & 1) * 16;
     } else {
       const int row = (wave * CP + q) * 8 + (lane >> 3);
-      offp[q] = (uint32_t)(row * (a.ldp * 2)) + (((lane & 7) ^ row_swizzle(row)) << 4);
+      offp[q] = row * pitch_p + (((lane & 7) ^ row_swizzle(row)) << 4);
     }
   }
   const uint32_t lds0 = __builtin_amdgcn_readfirstlane((uint32_t)(uintptr_t)(lds_void_t*)smem);
-  const int nk = a.K / T::SK, total = SPLIT ? 3 * nk : nk;
-  const int64_t p_first = TR ? (int64_t)m0 : m0 * a.ldp, p_step = TR ? T::SK * a.ldp : T::SK;
-  auto copy_stage = [&](int s) {
-    const int buf = s % NST;
-    int kk = min(s, total - 1), pp = 0, pq = 0;
-    if constexpr (SPLIT) {
-      const int seg = kk / nk;       // hi lo, lo hi, then hi hi: the small terms first
-      kk -= seg * nk;
-      pp = seg == 1, pq = seg == 0;
-    }
-    const _Float16* p = a.P.get(pp, z) + p_first + kk * p_step;
-    const _Float16* q = a.Q.get(pq, z) + n0 * a.ldq + kk * T::SK;
-    const uint32_t lp = lds0 + buf * T::STAGE + wave * CP * 1024;
-    const uint32_t lq = lds0 + buf * T::STAGE + T::P_BYTES + wave * CQ * 1024;
-    static_for<CP>([&](auto c) { bf16k::copy16<c.value * 1024>(p, offp[c.value], lp); });
-    static_for<CQ>([&](auto c) { bf16k::copy16<c.value * 1024>(q, offq[c.value], lq); });
+  const int total = a.K / KROWS;
+  const int64_t p_step = TR ? (int64_t)KROWS * pitch_p : 128;
+  // the next stage to copy: its operands, the stages left of its tile, that tile's item
+  const uint8_t *p_at, *q_at;
+  int left, copying = item;
+  auto aim = [&](int it) {
+    const At at = tile_at(it);
+    p_at = (const uint8_t*)(a.P.at + at.z * a.P.matrix +
+                            place<SPLIT>(a.P.ld, TR ? 0 : at.m0, TR ? at.m0 : 0));
+    q_at = (const uint8_t*)(a.Q.at + at.z * a.Q.matrix + place<SPLIT>(a.Q.ld, at.n0, 0));
+    left = total;
   };
+  auto copy = [&](uint32_t buf, auto c_c) {
+    constexpr int c = decltype(c_c)::value;
+    if constexpr (c < CQ)
+      bf16k::copy16<T::P_BYTES + c * 1024>(q_at, offq[c], buf + wave * CQ * 1024);
+    else
+      bf16k::copy16<(c - CQ) * 1024>(p_at, offp[c - CQ], buf + wave * CP * 1024);
+  };
+  // (behind the last tile's last stage that stage is copied again, and read for nothing)
+  auto advance = [&]() {
+    if (--left > 0) {
+      p_at += p_step;
+      q_at += 128;
+    } else if (copying + stride < end) {
+      copying += stride;
+      aim(copying);
+    } else {
+      left = 1;
+    }
+  };
+  aim(item);
 
-  f32x4 acc[BI][BJ];
-#pragma unroll
-  for (int i = 0; i < BI; ++i)
-#pragma unroll
-    for (int j = 0; j < BJ; ++j) acc[i][j] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
+  // Two parts: a stage's three terms are summed by themselves and then added (rounded to
+  // nearest) to the running sum: the matrix cores' own additions onto a large sum would lose
+  // more than the operands do.
+  f32x4 acc[BI][BJ], term3[2];
   const int fr = lane & 15, g = lane >> 4;
   int rp[2], rq[2];
 #pragma unroll
   for (int kk = 0; kk < 2; ++kk) {
     const int chk = ((kk * 4 + g) ^ row_swizzle(fr)) << 4;
-    rp[kk] = (wm * BI * 16 + fr) * ROW + chk;
-    rq[kk] = T::P_BYTES + (wn * BJ * 16 + fr) * ROW + chk;
+    rp[kk] = (wm * BI * 16 + fr) * 128 + chk;
+    rq[kk] = T::P_BYTES + (wn * BJ * 16 + fr) * 128 + chk;
   }
   // transposing reads: in 16-lane group g, lane s supplies k-row 8 g + (s >> 2) (+ 4 in the
   // second read) and rows 4 (s & 3) .. + 3 of the block; it receives row s of those k-rows
   const int q4 = (lane >> 2) & 3;
-  const int tswz = BM >= 128 ? q4 : q4 >> 1;     // (the same for k-row + 4, + 8, + 32)
-  const int tp = (8 * g + q4) * TROW + 8 * (lane & 3);
-
+  const int tswz = ((TROW >= 256 ? q4 : q4 >> 1) << 6) | ((g & 1) << 5);
+  int ta[TR ? BI : 1][TR && SPLIT ? 2 : 1];
+  if constexpr (TR) {
 #pragma unroll
-  for (int s = 0; s < NST - 1; ++s) copy_stage(s);
-  for (int s = 0; s < total; ++s) {
-    // this wave's copies of stage s have landed, then every wave's; and every wave has read
-    // the buffer that the next copies refill (stages past the last copy it again)
-    bf16k::wait_vmcnt<(NST - 2) * (CP + CQ)>();
-    lds_barrier();
-    copy_stage(s + NST - 1);
-    const uint8_t* st = smem + (s % NST) * T::STAGE;
+    for (int i = 0; i < BI; ++i)
 #pragma unroll
-    for (int kk = 0; kk < 2; ++kk) {
-      f16x8 fp[BI], fq[BJ];
-#pragma unroll
-      for (int i = 0; i < BI; ++i) {
-        if constexpr (TR) {
-          const int b = wm * BI + i;             // block of 16 rows: window b / 2, half b & 1
-          const uint8_t* at = st + tp + kk * 32 * TROW + (((b >> 1) ^ tswz) << 6) +
-                              (((b & 1) ^ (g & 1)) << 5);
-          bf16x8 v;
-          v.lo = bf16k::read_tr(at);
-          v.hi = bf16k::read_tr(at + 4 * TROW);
-          fp[i] = __builtin_bit_cast(f16x8, v);
-        } else {
-          fp[i] = *(const f16x8*)(st + rp[kk] + i * 16 * ROW);
-        }
+      for (int part = 0; part < (SPLIT ? 2 : 1); ++part) {
+        const int b = wm * BI + i;             // block of 16 rows: window b / 2, half b & 1
+        const int win = SPLIT ? (b >> 1) * 2 + part : b >> 1;
+        ta[i][part] = (8 * g + q4) * TROW + 8 * (lane & 3) + ((win << 6 | (b & 1) << 5) ^ tswz);
       }
+  }
+
+  // slice kk: the stage's k half, or its part
+  f16x8 fp[2][BI][2], fq[2][BJ][2];
+  auto read_p = [&](const uint8_t* st, int i, int kk) {
+    if constexpr (TR) {
+      const uint8_t* at = st + ta[i][SPLIT ? kk : 0] + (SPLIT ? 0 : kk * 32 * TROW);
+      bf16x8 v;
+      v.lo = bf16k::read_tr(at);
+      v.hi = bf16k::read_tr(at + 4 * TROW);
+      return __builtin_bit_cast(f16x8, v);
+    } else {
+      return *(const f16x8*)(st + rp[kk] + i * 16 * 128);
+    }
+  };
+  auto read_q = [&](const uint8_t* st, int j, int kk) {
+    return *(const f16x8*)(st + rq[kk] + j * 16 * 128);
+  };
+
+  // (pinned where it stands: gathered behind the stage, the additions would not hide under it)
+  auto add = [](f32x4& to, const f32x4& v) {
+    to += v;
+    asm volatile("" : "+v"(to));
+  };
+  constexpr int READS = 2 * (BI + BJ), TERMS = SPLIT ? 3 : 2, SLOTS = BI * BJ * TERMS;
+  int buf = 0;
+  auto stage = [&](auto par_c) {
+    constexpr int P = decltype(par_c)::value;
+    bf16k::wait_vmcnt<(NST - 2) * COPIES>();
+    lds_barrier();
+    __builtin_amdgcn_sched_barrier(0);
+    const int next = buf + 1 == NST ? 0 : buf + 1;
+    const uint8_t* st = smem + next * T::STAGE;
+    const uint32_t into = lds0 + buf * T::STAGE;
+    static_for<SLOTS>([&](auto q_c) {
+      constexpr int q = decltype(q_c)::value;
+      constexpr int term = q % TERMS, i = q / TERMS / BJ, j = q / TERMS % BJ;
+      // two parts: hi lo, lo hi, hi hi; one part: the stage's two k halves
+      constexpr int kp = SPLIT ? term == 1 : term, kq = SPLIT ? term == 0 : term;
+      if constexpr (SPLIT) {
+        constexpr int b = q / TERMS;             // block: its three terms, then the one before's sum
+        const f32x4 zero = {0.0f, 0.0f, 0.0f, 0.0f};
+        term3[b & 1] = __builtin_amdgcn_mfma_f32_16x16x32_f16(
+            fp[P][i][kp], fq[P][j][kq], term ? term3[b & 1] : zero, 0, 0, 0);
+        if constexpr (term == 2 && b > 0) add(acc[(b - 1) / BJ][(b - 1) % BJ], term3[(b - 1) & 1]);
+      } else {
+        acc[i][j] =
+            __builtin_amdgcn_mfma_f32_16x16x32_f16(fp[P][i][kp], fq[P][j][kq], acc[i][j], 0, 0, 0);
+      }
+      constexpr int r0 = reads_before(q, READS, SLOTS), r1 = reads_before(q + 1, READS, SLOTS);
+      static_for<r1 - r0>([&](auto n_c) {
+        constexpr int n = r0 + decltype(n_c)::value, kk = n / (BI + BJ), x = n % (BI + BJ);
+        if constexpr (x < BJ)
+          fq[P ^ 1][x][kk] = read_q(st, x, kk);
+        else
+          fp[P ^ 1][x - BJ][kk] = read_p(st, x - BJ, kk);
+      });
+      constexpr int c0 = q * COPIES / SLOTS, c1 = (q + 1) * COPIES / SLOTS;
+      static_for<c1 - c0>([&](auto n_c) {
+        copy(into, std::integral_constant<int, c0 + decltype(n_c)::value>{});
+      });
+      __builtin_amdgcn_sched_barrier(0);
+    });
+    if constexpr (SPLIT) add(acc[BI - 1][BJ - 1], term3[(BI * BJ - 1) & 1]);
+    advance();
+    buf = next;
+  };
 #pragma unroll
-      for (int j = 0; j < BJ; ++j) fq[j] = *(const f16x8*)(st + rq[kk] + j * 16 * ROW);
+  for (int s = 0; s < NST; ++s) {
+    static_for<COPIES>([&](auto c) { copy(lds0 + s * T::STAGE, c); });
+    advance();
+  }
+  bf16k::wait_vmcnt<(NST - 1) * COPIES>();
+  lds_barrier();
+#pragma unroll
+  for (int kk = 0; kk < 2; ++kk) {
+#pragma unroll
+    for (int j = 0; j < BJ; ++j) fq[0][j][kk] = read_q(smem, j, kk);
+#pragma unroll
+    for (int i = 0; i < BI; ++i) fp[0][i][kk] = read_p(smem, i, kk);
+  }
+  for (; item < end; item += stride) {
+#pragma unroll
+    for (int i = 0; i < BI; ++i)
+#pragma unroll
+      for (int j = 0; j < BJ; ++j) acc[i][j] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
+    // (the wide tile's sums live in the accumulation registers on both sides of the loop:
+    // otherwise the allocator moves them to and fro inside it)
+    auto pin = [&]() {
+      if constexpr (T::EU_WAVES == 1)
+#pragma unroll
+        for (int i = 0; i < BI; ++i)
+#pragma unroll
+          for (int j = 0; j < BJ; ++j) asm volatile("" : "+a"(acc[i][j]));
+    };
+    pin();
+    const At at = tile_at(item);
+    // block (i, j) of a lane: column c = 16 j + (lane & 15), rows r .. r + 3, r = 16 i + 4 g
+    const int r0 = at.m0 + wm * BI * 16 + 4 * g, c0 = at.n0 + wn * BJ * 16 + fr;
+    // What the epilogue adds to: a small tile reads it ahead of its products (a launch of few of
+    // them is latency), a larger one half a tile at a time behind them.
+    constexpr bool OLD = MODE != GRAM, LO = SPLIT || TR, OLD_LO = OLD && LO;
+    constexpr bool EARLY = BI * BJ <= 4;
+    constexpr int HALF_J = EARLY ? BJ : BJ / 2;
+    f16x4 oh[OLD ? BI : 1][HALF_J], ol[OLD_LO ? BI : 1][HALF_J];
+    auto read_old = [&](auto j_c) {
+      constexpr int j0 = decltype(j_c)::value;
+      const _Float16* const old = a.P.at + at.z * a.P.matrix;
 #pragma unroll
       for (int i = 0; i < BI; ++i)
 #pragma unroll
-        for (int j = 0; j < BJ; ++j)
-          acc[i][j] = __builtin_amdgcn_mfma_f32_16x16x32_f16(fp[i], fq[j], acc[i][j], 0, 0, 0);
+        for (int j = 0; j < HALF_J; ++j) {
+          const _Float16* p = old + place<SPLIT>(a.P.ld, c0 + 16 * (j0 + j), r0 + 16 * i);
+          oh[i][j] = *(const f16x4*)p;
+          if constexpr (OLD_LO) ol[i][j] = *(const f16x4*)(p + lo_at<SPLIT>(a.P));
+        }
+    };
+    if constexpr (OLD && EARLY) read_old(std::integral_constant<int, 0>{});
+    for (int s = 0; s < total; s += 2) {
+      stage(std::integral_constant<int, 0>{});
+      stage(std::integral_constant<int, 1>{});
+    }
+    pin();
+    f32x4 val[BI][BJ];
+    if constexpr (OLD) {
+      static_for<BJ / HALF_J>([&](auto half) {
+        constexpr int j0 = decltype(half)::value * HALF_J;
+        if constexpr (!EARLY) read_old(std::integral_constant<int, j0>{});
+#pragma unroll
+        for (int i = 0; i < BI; ++i)
+#pragma unroll
+          for (int j = 0; j < HALF_J; ++j)
+#pragma unroll
+            for (int q = 0; q < 4; ++q) {
+              const float o =
+                  (float)oh[i][j][q] + (OLD_LO ? (float)ol[OLD_LO ? i : 0][j][q] : 0.0f);
+              float v = acc[i][j0 + j][q] * (1.0f / S);
+              v = MODE == SQUARE ? fmaf(a.alpha, v, a.beta * o) : fmaf(a.beta, o, v);
+              if (MODE == SQUARE && r0 + 16 * i + q == c0 + 16 * (j0 + j)) v += a.shift * S;
+              val[i][j0 + j][q] = v;
+            }
+      });
+    } else {
+#pragma unroll
+      for (int i = 0; i < BI; ++i)
+#pragma unroll
+        for (int j = 0; j < BJ; ++j) val[i][j] = acc[i][j] * (1.0f / S);
+    }
+    if constexpr (MODE == RESULT) {
+      write_result<BI, BJ>(a.res, val, at.z, r0, c0, lane);
+      continue;
+    }
+    _Float16* const out = a.C.at + at.z * a.C.matrix;
+#pragma unroll
+    for (int j = 0; j < BJ; ++j)
+#pragma unroll
+      for (int i = 0; i < BI; i += 2)
+#pragma unroll
+        for (int part = 0; part < (LO ? 2 : 1); ++part) {
+          const u32x2 x = packed(val[i][j], part), y = packed(val[i + 1][j], part);
+          // blocks i and i + 1: after the swap a lane holds 8 consecutive rows of one of them,
+          // and a store covers 64 consecutive bytes of 16 columns
+          _Float16* p = out + part * lo_at<SPLIT>(a.C) +
+                        place<SPLIT>(a.C.ld, c0 + 16 * j,
+                                     r0 - 4 * g + 16 * (i + (g & 1)) + 8 * (g >> 1));
+          const auto s0 = __builtin_amdgcn_permlane16_swap(x[0], y[0], false, false);
+          const auto s1 = __builtin_amdgcn_permlane16_swap(x[1], y[1], false, false);
+          *(u32x4*)p = u32x4{s0[0], s1[0], s0[1], s1[1]};
+        }
+    if constexpr (!TR) {
+      if (at.tn < at.tm * T::HALVES) {               // (a diagonal square is written whole)
+#pragma unroll
+        for (int i = 0; i < BI; ++i)
+#pragma unroll
+          for (int j = 0; j < BJ; ++j)
+#pragma unroll
+            for (int part = 0; part < (LO ? 2 : 1); ++part) {
+              _Float16* p = out + part * lo_at<SPLIT>(a.C) +
+                            place<SPLIT>(a.C.ld, r0 + 16 * i + (lane & 3), c0 + 16 * j - (lane & 3));
+              *(u32x2*)p = quad_transpose(packed(val[i][j], part), lane);
+            }
+      }
     }
   }
-  asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)" ::: "memory");
-
-  // block (i, j) of a lane: column c = 16 j + (lane & 15), rows r .. r + 3, r = 16 i + 4 g
-#pragma unroll
-  for (int i = 0; i < BI; ++i)
-#pragma unroll
-    for (int j = 0; j < BJ; ++j) {
-      const int64_t r = m0 + (wm * BI + i) * 16 + 4 * g, c = n0 + (wn * BJ + j) * 16 + fr;
-      float v[4];
-#pragma unroll
-      for (int q = 0; q < 4; ++q) v[q] = acc[i][j][q] * (1.0f / S);
-      if constexpr (MODE == SQUARE) {
-        const f16x4 h = *(const f16x4*)(a.P.get(0, z) + c * a.ldp + r);
-        f16x4 l = {0, 0, 0, 0};
-        if constexpr (SPLIT) l = *(const f16x4*)(a.P.get(1, z) + c * a.ldp + r);
-#pragma unroll
-        for (int q = 0; q < 4; ++q) {
-          v[q] = fmaf(a.alpha, v[q], a.beta * ((float)h[q] + (float)l[q]));
-          if (r + q == c) v[q] += a.shift * S;
-        }
-      }
-      if constexpr (MODE == UPDATE) {
-        const f16x4 h = *(const f16x4*)(a.P.get(0, z) + c * a.ldp + r);
-        const f16x4 l = *(const f16x4*)(a.P.get(1, z) + c * a.ldp + r);
-#pragma unroll
-        for (int q = 0; q < 4; ++q) v[q] = fmaf(a.beta, (float)h[q] + (float)l[q], v[q]);
-        if (a.last) {
-          const Result& o = a.res;
-#pragma unroll
-          for (int q = 0; q < 4; ++q) {
-            const int64_t row = o.tall ? r + q : c, col = o.tall ? c : r + q;
-            if (row < o.rows && col < o.cols) {
-              const int64_t at = z * o.matrix + row * o.ld + col;
-              float w = v[q] * (1.0f / S);
-              if (o.f32) {
-                float* p = (float*)o.out + at;
-                *p = o.step ? fmaf(o.keep, *p, -o.rate * w) : w;
-              } else {
-                uint16_t* p = (uint16_t*)o.out + at;
-                if (o.step) w = fmaf(o.keep, bf16_bits_to_f32(*p), -o.rate * w);
-                *p = f32_to_bf16_bits(w);
-              }
-            }
-          }
-          continue;
-        }
-      }
-      f16x4 h, l;
-#pragma unroll
-      for (int q = 0; q < 4; ++q) {
-        const HiLo s = split(v[q]);
-        h[q] = s.hi, l[q] = s.lo;
-      }
-      constexpr bool LO = SPLIT || MODE == UPDATE;
-      *(f16x4*)(a.C.get(0, z) + c * a.ldc + r) = h;
-      if constexpr (LO) *(f16x4*)(a.C.get(1, z) + c * a.ldc + r) = l;
-      if constexpr (MODE != UPDATE) {
-        if (tm != tn) {
-#pragma unroll
-          for (int q = 0; q < 4; ++q) {
-            a.C.get(0, z)[(r + q) * a.ldc + c] = h[q];
-            if constexpr (LO) a.C.get(1, z)[(r + q) * a.ldc + c] = l[q];
-          }
-        }
-      }
-    }
+  asm volatile("s_waitcnt vmcnt(0)" ::: "memory");   // no copy outlives the workgroup's LDS
 }
 
 // ---------------------------------------------------------------------------
@@ -283,76 +583,141 @@ struct Source {
   int32_t nesterov;
 };
 constexpr int NORM_GROUPS = 256;   // workgroups of a matrix's sum of squares, at most
-constexpr int PRE = 256;
+constexpr int NORM_THREADS = 1024, PRE = 256;
 
-__device__ __forceinline__ float grad_at(const Source& s, int64_t z, int64_t i, int64_t j) {
-  const int64_t at = z * s.matrix + i * s.ld + j;
-  return s.f32 ? ((const float*)s.g)[at] : bf16_bits_to_f32(((const uint16_t*)s.g)[at]);
-}
+typedef f32x4 f32x4_any __attribute__((aligned(4)));
+typedef u32x4 u32x4_any __attribute__((aligned(2)));
 
-__global__ void __launch_bounds__(PRE) ns_norm_kernel(Source s, double* part) {
-  const int64_t z = blockIdx.y, n = (int64_t)s.rows * s.cols;
-  double sum = 0.0;
-  for (int64_t e = (int64_t)blockIdx.x * PRE + threadIdx.x; e < n; e += (int64_t)gridDim.x * PRE) {
-    const int64_t i = e / s.cols, j = e - i * s.cols;
-    float u = grad_at(s, z, i, j);
-    if (s.m) {
-      float* m = s.m + z * n + e;
-      const float v = fmaf(s.mu, *m, u);
-      *m = v;
-      u = s.nesterov ? fmaf(s.mu, v, u) : v;
-    }
-    sum += (double)u * (double)u;
-  }
-  __shared__ double red[PRE];
-  red[threadIdx.x] = sum;
-  __syncthreads();
+// Eight neighbours in a row, `n` of them there (rows start at any element).
+__device__ __forceinline__ void load8(const void* p, bool f32, int64_t at, int n, float (&v)[8]) {
+  if (n >= 8 && f32) {
+    const f32x4 a = *(const f32x4_any*)((const float*)p + at);
+    const f32x4 b = *(const f32x4_any*)((const float*)p + at + 4);
 #pragma unroll
-  for (int o = PRE / 2; o > 0; o >>= 1) {
-    if ((int)threadIdx.x < o) red[threadIdx.x] += red[threadIdx.x + o];
-    __syncthreads();
+    for (int k = 0; k < 4; ++k) v[k] = a[k], v[k + 4] = b[k];
+  } else if (n >= 8) {
+    const u32x4 a = *(const u32x4_any*)((const uint16_t*)p + at);
+#pragma unroll
+    for (int k = 0; k < 4; ++k) {
+      v[2 * k] = __uint_as_float(a[k] << 16);
+      v[2 * k + 1] = __uint_as_float(a[k] & 0xffff0000u);
+    }
+  } else {
+#pragma unroll
+    for (int k = 0; k < 8; ++k)
+      v[k] = k >= n ? 0.0f
+             : f32  ? ((const float*)p)[at + k]
+                    : bf16_bits_to_f32(((const uint16_t*)p)[at + k]);
   }
-  if (threadIdx.x == 0) part[z * gridDim.x + blockIdx.x] = red[0];
 }
 
-// X [r_pad, k_pad], 64 x 64 tiles (transposed through LDS where the matrix is tall)
+// Sum over the workgroup in every thread of wave 0, in a fixed order.
+template <int THREADS>
+__device__ __forceinline__ double block_sum(double v, double* lds) {
+#pragma unroll
+  for (int o = 32; o >= 1; o >>= 1) v += __shfl_xor(v, o);
+  if ((threadIdx.x & 63) == 0) lds[threadIdx.x >> 6] = v;
+  __syncthreads();
+  v = 0.0;
+#pragma unroll
+  for (int w = 0; w < THREADS / 64; ++w) v += lds[w];
+  return v;
+}
+
+// Runs of 8 entries, `runs` of them a row.
+__global__ void __launch_bounds__(NORM_THREADS) ns_norm_kernel(Source s, double* part) {
+  const int64_t z = blockIdx.y;
+  const int runs = (s.cols + 7) / 8;
+  const int64_t all = (int64_t)s.rows * runs, step = (int64_t)gridDim.x * NORM_THREADS;
+  float* const mom = s.m ? s.m + z * s.rows * s.cols : nullptr;
+  const int64_t step_i = step / runs;
+  const int step_j = (int)(step - step_i * runs);
+  int64_t e = (int64_t)blockIdx.x * NORM_THREADS + threadIdx.x;
+  int64_t i = e / runs;
+  int j = (int)(e - i * runs);
+  double sum[2] = {0.0, 0.0};
+  for (; e < all; e += step) {
+    const int n = s.cols - 8 * j;
+    float u[8];
+    load8(s.g, s.f32, z * s.matrix + i * s.ld + 8 * j, n, u);
+    if (mom) {
+      float* const p = mom + i * s.cols + 8 * j;
+      float m[8];
+      load8(p, true, 0, n, m);
+#pragma unroll
+      for (int k = 0; k < 8; ++k) {
+        m[k] = fmaf(s.mu, m[k], u[k]);
+        u[k] = s.nesterov ? fmaf(s.mu, m[k], u[k]) : m[k];
+      }
+      if (n >= 8) {
+        *(f32x4_any*)p = f32x4{m[0], m[1], m[2], m[3]};
+        *(f32x4_any*)(p + 4) = f32x4{m[4], m[5], m[6], m[7]};
+      } else {
+#pragma unroll
+        for (int k = 0; k < 7; ++k)
+          if (k < n) p[k] = m[k];
+      }
+    }
+#pragma unroll
+    for (int k = 0; k < 8; ++k) sum[k & 1] = fma((double)u[k], (double)u[k], sum[k & 1]);
+    i += step_i;
+    j += step_j;
+    if (j >= runs) j -= runs, ++i;
+  }
+  __shared__ double red[NORM_THREADS / 64];
+  const double total = block_sum<NORM_THREADS>(sum[0] + sum[1], red);
+  if (threadIdx.x == 0) part[z * gridDim.x + blockIdx.x] = total;
+}
+
+// X [r_pad, k_pad] by tiles of 64 x 64, through LDS where the matrix is tall.
+template <bool SPLIT>
 __global__ void __launch_bounds__(PRE)
-    ns_start_kernel(Source s, const double* part, int n_part, float eps, int tall, Planes X,
-                    int64_t ldx) {
-  __shared__ double red[PRE];
+    ns_start_kernel(Source s, const double* part, int n_part, float eps, int tall, Planes X) {
+  __shared__ double red[PRE / 64];
   __shared__ float tile[64][65];
   const int64_t z = blockIdx.z;
   const int t = threadIdx.x;
-  red[t] = t < n_part ? part[z * n_part + t] : 0.0;
-  __syncthreads();
-#pragma unroll
-  for (int o = PRE / 2; o > 0; o >>= 1) {
-    if (t < o) red[t] += red[t + o];
-    __syncthreads();
-  }
-  const float inv = (float)((double)S / (sqrt(red[0]) + (double)eps));
   const int64_t i0 = (int64_t)(tall ? blockIdx.x : blockIdx.y) * 64;   // in the matrix
   const int64_t j0 = (int64_t)(tall ? blockIdx.y : blockIdx.x) * 64;
-  const int tx = t & 63, ty = t >> 6;
-  for (int y = ty; y < 64; y += 4) {
-    const int64_t i = i0 + y, j = j0 + tx;
-    float u = 0.0f;
-    if (i < s.rows && j < s.cols) {
-      u = grad_at(s, z, i, j);
-      if (s.m) {
-        const float v = s.m[z * s.rows * s.cols + i * s.cols + j];
-        u = s.nesterov ? fmaf(s.mu, v, u) : v;
-      }
+  float v[2][8];
+#pragma unroll
+  for (int h = 0; h < 2; ++h) {
+    const int64_t i = i0 + (t >> 3) + 32 * h, j = j0 + (t & 7) * 8;
+    const int n = i < s.rows ? (int)max((int64_t)0, min((int64_t)8, s.cols - j)) : 0;
+    load8(s.g, s.f32, z * s.matrix + i * s.ld + j, n, v[h]);
+    if (s.m) {
+      float m[8];
+      load8(s.m, true, z * s.rows * s.cols + i * s.cols + j, n, m);
+#pragma unroll
+      for (int k = 0; k < 8; ++k) v[h][k] = s.nesterov ? fmaf(s.mu, m[k], v[h][k]) : m[k];
     }
-    tile[y][tx] = u * inv;
   }
-  __syncthreads();
-  const int64_t r0 = (int64_t)blockIdx.y * 64, c0 = (int64_t)blockIdx.x * 64;   // in X
-  for (int y = ty; y < 64; y += 4) {
-    const HiLo v = split(tall ? tile[tx][y] : tile[y][tx]);
-    const int64_t at = (r0 + y) * ldx + c0 + tx;
-    X.get(0, z)[at] = v.hi;
-    X.get(1, z)[at] = v.lo;
+  const double total = block_sum<PRE>(t < n_part ? part[z * n_part + t] : 0.0, red);
+  const float inv = (float)((double)S / (sqrt(total) + (double)eps));
+  if (tall) {
+#pragma unroll
+    for (int h = 0; h < 2; ++h)
+#pragma unroll
+      for (int k = 0; k < 8; ++k) tile[(t >> 3) + 32 * h][(t & 7) * 8 + k] = v[h][k];
+    __syncthreads();
+#pragma unroll
+    for (int h = 0; h < 2; ++h)
+#pragma unroll
+      for (int k = 0; k < 8; ++k) v[h][k] = tile[(t & 7) * 8 + k][(t >> 3) + 32 * h];
+  }
+#pragma unroll
+  for (int h = 0; h < 2; ++h) {
+    f16x8 hi, lo;
+#pragma unroll
+    for (int k = 0; k < 8; ++k) {
+      const HiLo x = split(v[h][k] * inv);
+      hi[k] = x.hi, lo[k] = x.lo;
+    }
+    _Float16* p = X.at + z * X.matrix +
+                  place<SPLIT>(X.ld, (int64_t)blockIdx.y * 64 + (t >> 3) + 32 * h,
+                               (int64_t)blockIdx.x * 64 + (t & 7) * 8);
+    *(f16x8*)p = hi;
+    *(f16x8*)(p + lo_at<SPLIT>(X)) = lo;
   }
 }
 
@@ -362,12 +727,42 @@ constexpr int64_t MAX_SIDE = (int64_t)1 << 20, MAX_SHORT = (int64_t)1 << 16, MAX
 // Sizes and the workspace of a stack of matrices
 struct Plan {
   int64_t batch;
-  int32_t r, k, tall, tile;
+  int32_t r, k, tall;
+  int32_t tile[3];                          // rows of a tile of A, B and X
   int64_t r_pad, k_pad;
   int32_t split, n_part;
   int64_t x_plane, a_plane;                 // elements
   size_t part, x[2], a, b, total;           // bytes
 };
+
+// Each product takes the tile that is done first: a round of workgroups lasts its stages, and a
+// tile's start and end come on top.  Nanoseconds a stage (measured, one part / two parts; a
+// 128 x 128 tile by whether a compute unit has one or two) and microseconds a launch:
+//   64 x 64   240 / 300                    6   five to nine stages in flight: few, small matrices
+//   128       650 / 900, 950 / 1300        6
+//   256 x 128 820                         10
+// e.g. B X of 1024 x 1024: 9.5, 18 and 24 us; of 8 of them 42, 32 and 29; of 4096 x 4096 254, 137
+// and 125.  In two parts: 16 and 36 us; 95 and 57; 557 and 342.
+void choose_tiles(Plan* p) {
+  const double unit = 256.0;
+  for (int i = 0; i < 3; ++i) {
+    double best = 0.0;
+    for (int t = 64; t <= (p->split ? 128 : 256); t *= 2) {
+      const double r = (double)cdiv(p->r, t), k = (double)cdiv(p->k, t);
+      const double items = p->batch * (i == 2 ? r * k : r * (r + 1) / 2) * (t == 256 ? 2 : 1);
+      const double stages = (i == 0 ? p->k : p->r) / (p->split ? 32.0 : 64.0);
+      double cost;
+      if (t == 64)
+        cost = ceil(items / unit) * stages * (p->split ? 0.30 : 0.24) + 6;
+      else if (t == 128)
+        cost = items <= unit ? stages * (p->split ? 0.90 : 0.65) + 6
+                             : ceil(items / (2 * unit)) * stages * (p->split ? 1.30 : 0.95) + 6;
+      else
+        cost = ceil(items / unit) * stages * 0.82 + 10;
+      if (t == 64 || cost < best) best = cost, p->tile[i] = t;
+    }
+  }
+}
 
 bool make_plan(int64_t batch, int64_t m, int64_t n, int32_t out_dtype, Plan* p) {
   if (batch <= 0 || batch > MAX_BATCH || m <= 0 || n <= 0 || m > MAX_SIDE || n > MAX_SIDE)
@@ -375,12 +770,13 @@ bool make_plan(int64_t batch, int64_t m, int64_t n, int32_t out_dtype, Plan* p) 
   const int64_t r = m < n ? m : n, k = m < n ? n : m;
   if (r > MAX_SHORT) return false;
   p->batch = batch, p->r = (int32_t)r, p->k = (int32_t)k, p->tall = m > n;
-  auto tiles = [&](int64_t t) { return batch * cdiv(r, t) * cdiv(k, t); };
-  p->tile = tiles(256) >= 192 ? 256 : tiles(128) >= 128 ? 128 : 64;
-  p->r_pad = cdiv(r, (int64_t)p->tile) * p->tile;
-  p->k_pad = cdiv(k, (int64_t)p->tile) * p->tile;
-  p->split = out_dtype == AGRL_F32;
-  const int64_t per = cdiv(m * n, (int64_t)PRE * 8);
+  p->split = out_dtype == AGRL_F32 || r <= SPLIT_ROWS;
+  choose_tiles(p);
+  int64_t pad = 128;
+  for (int i = 0; i < 3; ++i) pad = p->tile[i] > pad ? p->tile[i] : pad;
+  p->r_pad = cdiv(r, pad) * pad;
+  p->k_pad = cdiv(k, pad) * pad;
+  const int64_t per = cdiv(m * cdiv(n, (int64_t)8), (int64_t)NORM_THREADS);
   p->n_part = (int32_t)(per < NORM_GROUPS ? per : NORM_GROUPS);
   p->x_plane = batch * p->r_pad * p->k_pad;
   p->a_plane = batch * p->r_pad * p->r_pad;
@@ -400,16 +796,37 @@ bool make_plan(int64_t batch, int64_t m, int64_t n, int32_t out_dtype, Plan* p) 
 }
 
 template <int MODE, class T>
-void launch(const Plan& p, Args a, hipStream_t s) {
-  a.tiles_m = (int32_t)((MODE == UPDATE ? p.k_pad : p.r_pad) / T::BM);
+void launch_tile(const Plan& p, Args a, hipStream_t s) {
+  constexpr bool TR = MODE == UPDATE || MODE == RESULT;
+  a.tiles_m = (int32_t)((TR ? p.k_pad : p.r_pad) / T::BM);
   a.tiles_n = (int32_t)(p.r_pad / T::BN);
-  const int64_t tiles = MODE == UPDATE ? (int64_t)a.tiles_m * a.tiles_n
-                                       : (int64_t)a.tiles_n * (a.tiles_n + 1) / 2;
-  const dim3 grid((unsigned)tiles, (unsigned)p.batch), block(64 * T::WAVES);
-  if (p.split)
-    hipLaunchKernelGGL((ns_product_kernel<MODE, true, T>), grid, block, 0, s, a);
+  const int64_t tiles = TR ? (int64_t)a.tiles_m * a.tiles_n
+                           : (int64_t)a.tiles_m * (a.tiles_m + 1) / 2 * T::HALVES;
+  a.tiles = (int32_t)tiles, a.items = (int32_t)(tiles * p.batch);
+  const int64_t most = (int64_t)device_cu_count() * T::PER_CU;
+  const dim3 grid((unsigned)(a.items < most ? a.items : most)), block(64 * T::WAVES);
+  if constexpr (T::BM <= 128) {       // (the two sums of the wide tile do not fit the registers)
+    if (p.split) {
+      hipLaunchKernelGGL((ns_product_kernel<MODE, true, T>), grid, block, 0, s, a);
+      return;
+    }
+  }
+  hipLaunchKernelGGL((ns_product_kernel<MODE, false, T>), grid, block, 0, s, a);
+}
+
+using Tile64 = Tile<2, 2, 2, 2, 9, 1>;
+using Tile128 = Tile<2, 2, 4, 4, 2, 2>;
+using Tile256 = Tile<2, 2, 8, 4, 3, 1>;
+
+template <int MODE>
+void launch(const Plan& p, const Args& a, hipStream_t s) {
+  const int tile = p.tile[MODE == GRAM ? 0 : MODE == SQUARE ? 1 : 2];
+  if (tile == 256)
+    launch_tile<MODE, Tile256>(p, a, s);
+  else if (tile == 128)
+    launch_tile<MODE, Tile128>(p, a, s);
   else
-    hipLaunchKernelGGL((ns_product_kernel<MODE, false, T>), grid, block, 0, s, a);
+    launch_tile<MODE, Tile64>(p, a, s);
 }
 
 struct Steps {
@@ -417,38 +834,40 @@ struct Steps {
   float a, b, c, eps;
 };
 
-template <class T>
 void run(const Plan& p, const Steps& o, const Source& src, const Result& res, uint8_t* ws,
          hipStream_t s) {
   double* part = (double*)(ws + p.part);
-  hipLaunchKernelGGL(ns_norm_kernel, dim3(p.n_part, (unsigned)p.batch), dim3(PRE), 0, s, src, part);
+  hipLaunchKernelGGL(ns_norm_kernel, dim3(p.n_part, (unsigned)p.batch), dim3(NORM_THREADS), 0, s,
+                     src, part);
   Planes X[2], A, B;
+  const int64_t parts = p.split ? 2 : 1;      // interleaved
   for (int i = 0; i < 2; ++i)
-    X[i] = Planes{(_Float16*)(ws + p.x[i]), p.x_plane, p.r_pad * p.k_pad};
-  A = Planes{(_Float16*)(ws + p.a), p.a_plane, p.r_pad * p.r_pad};
-  B = Planes{(_Float16*)(ws + p.b), p.a_plane, p.r_pad * p.r_pad};
-  hipLaunchKernelGGL(ns_start_kernel,
-                     dim3((unsigned)(p.k_pad / 64), (unsigned)(p.r_pad / 64), (unsigned)p.batch),
-                     dim3(PRE), 0, s, src, part, p.n_part, o.eps, p.tall, X[0], p.k_pad);
+    X[i] = Planes{(_Float16*)(ws + p.x[i]), parts * p.r_pad * p.k_pad, p.x_plane, p.k_pad};
+  A = Planes{(_Float16*)(ws + p.a), parts * p.r_pad * p.r_pad, 0, p.r_pad};
+  B = Planes{(_Float16*)(ws + p.b), parts * p.r_pad * p.r_pad, 0, p.r_pad};
+  const dim3 grid((unsigned)(p.k_pad / 64), (unsigned)(p.r_pad / 64), (unsigned)p.batch);
+  if (p.split)
+    hipLaunchKernelGGL(ns_start_kernel<true>, grid, dim3(PRE), 0, s, src, part, p.n_part, o.eps,
+                       p.tall, X[0]);
+  else
+    hipLaunchKernelGGL(ns_start_kernel<false>, grid, dim3(PRE), 0, s, src, part, p.n_part, o.eps,
+                       p.tall, X[0]);
   for (int i = 0; i < o.n; ++i) {
     Args a = {};
-    a.P = a.Q = X[i & 1], a.ldp = a.ldq = p.k_pad, a.K = (int32_t)p.k_pad;
-    a.C = A, a.ldc = p.r_pad;
-    launch<GRAM, T>(p, a, s);
+    a.P = a.Q = X[i & 1], a.K = (int32_t)p.k_pad, a.C = A;
+    launch<GRAM>(p, a, s);
     const float sigma = p.split || i < o.n - 2 ? 0.0f : -(o.b + o.c) * (i == o.n - 1 ? 1.0f : 0.5f);
-    a.P = a.Q = A, a.ldp = a.ldq = p.r_pad, a.K = (int32_t)p.r_pad;
+    a.P = a.Q = A, a.K = (int32_t)p.r_pad;
     a.C = B, a.alpha = o.c, a.beta = o.b, a.shift = sigma;
-    launch<SQUARE, T>(p, a, s);
-    a.P = X[i & 1], a.ldp = p.k_pad, a.Q = B;
-    a.C = X[(i + 1) & 1], a.ldc = p.k_pad, a.beta = o.a - sigma;
-    a.last = i == o.n - 1, a.res = res;
-    launch<UPDATE, T>(p, a, s);
+    launch<SQUARE>(p, a, s);
+    a.P = X[i & 1], a.Q = B, a.C = X[(i + 1) & 1], a.beta = o.a - sigma;
+    a.res = res;
+    if (i == o.n - 1)
+      launch<RESULT>(p, a, s);
+    else
+      launch<UPDATE>(p, a, s);
   }
 }
-
-using Tile64 = Tile<2, 2, 2, 2, 4>;
-using Tile128 = Tile<2, 2, 4, 4, 2>;
-using Tile256 = Tile<2, 4, 8, 4, 2>;
 
 int start(const char* fn, const Plan& p, const agrl_ns_options* opt, const Source& src,
           const Result& res, void* ws, size_t ws_bytes, hipStream_t s) {
@@ -465,12 +884,7 @@ int start(const char* fn, const Plan& p, const agrl_ns_options* opt, const Sourc
   }
   if (!ws || ws_bytes < p.total) return fail(AGRL_E_WORKSPACE, fn, "workspace missing or too small");
   if ((uintptr_t)ws % 256 != 0) return fail(AGRL_E_UNSUPPORTED, fn, "workspace must be 256-byte aligned");
-  if (p.tile == 256)
-    run<Tile256>(p, o, src, res, (uint8_t*)ws, s);
-  else if (p.tile == 128)
-    run<Tile128>(p, o, src, res, (uint8_t*)ws, s);
-  else
-    run<Tile64>(p, o, src, res, (uint8_t*)ws, s);
+  run(p, o, src, res, (uint8_t*)ws, s);
   return hip_status(hipGetLastError());
 }
 
