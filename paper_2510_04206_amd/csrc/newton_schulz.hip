@@ -79,7 +79,11 @@ struct Result {
 
 struct Args {
   Planes P, Q;        // P: rows of the tile (UPDATE: X, read transposed); Q: columns
-  int32_t K, tiles_m, tiles_n, tiles, items;   // tiles of a matrix, of the stack
+  int32_t K;
+  // The stack's products are numbered in units of unit_m x unit_n (matrix by matrix, `units` each,
+  // units_m down and units_n across); a launch takes `count` of them from `first` on, by tiles
+  // that divide a unit.
+  int32_t unit_m, unit_n, units_m, units_n, units, first, count;
   Planes C;           // A, B or the next X
   float alpha, beta, shift;   // UPDATE: beta X + P Q; SQUARE: beta A + alpha P Q + shift I
   Result res;         // RESULT: in place of C
@@ -95,7 +99,6 @@ struct Tile {
   // between the two register files
   static constexpr int EU_WAVES = BI_ * BJ_ <= 16 ? 2 : 1;
   static constexpr int BM = WM * BI * 16, BN = WN * BJ * 16, WAVES = WM * WN;
-  static constexpr int HALVES = BM / BN;         // column tiles of a square of BM
   static constexpr int P_BYTES = BM * 128, STAGE = (BM + BN) * 128;
   static constexpr int CP = BM / 8 / WAVES, CQ = BN / 8 / WAVES;   // 1 KiB copies of a wave
 };
@@ -162,82 +165,97 @@ __device__ __forceinline__ f32x4 quad_transpose(const f32x4& v, int lane) {
 
 // The last product's entries: rows r .. r + 3 (16 apart by block i) of column c (by block j) of
 // X, which are four neighbours in a row of the result (behind a transpose of lane quads where X
-// is the result's transpose).  A step reads up to 8 blocks' old values at once.
-template <int BI, int BJ>
+// is the result's transpose).  A step reads its old values ahead of its stores, eight blocks' at a
+// time; a one-part product's result is bf16.
+// FULL: the whole tile lies in the result (no bounds, so no branches between the loads).
+template <bool SPLIT, bool FULL, int BI, int BJ>
 __device__ __forceinline__ void write_result(const Result& o, const f32x4 (&val)[BI][BJ], int z,
                                              int r0, int c0, int lane) {
   typedef f32x4 f32x4_a4 __attribute__((aligned(4)));
   typedef u32x2 u32x2_a2 __attribute__((aligned(2)));
-  constexpr int N = BI * BJ < 8 ? BI * BJ : 8;     // blocks at once
+  typedef std::conditional_t<SPLIT, f32x4, u32x2> Old;       // fp32, or four bf16
+  constexpr int N = !FULL || BI * BJ < 8 ? BJ : 8;           // blocks at once
+  const bool f32 = SPLIT && o.f32;
   float* const out32 = (float*)o.out + (int64_t)z * o.matrix;
   uint16_t* const out16 = (uint16_t*)o.out + (int64_t)z * o.matrix;
+  // (r, c) and the steps of i and j in the result's rows and columns
+  const int row0 = o.tall ? r0 + (lane & 3) : c0, col0 = o.tall ? c0 - (lane & 3) : r0;
   static_for<BI * BJ / N>([&](auto part_c) {
     constexpr int first = decltype(part_c)::value * N;
-    auto place_of = [&](int b, int& row, int& col) {
-      const int r = r0 + 16 * (b / BJ), c = c0 + 16 * (b % BJ);
-      row = o.tall ? r + (lane & 3) : c;
-      col = o.tall ? c - (lane & 3) : r;
-      return (int64_t)row * o.ld + col;
-    };
-    f32x4 old[N];
-    if (o.step)
+    auto each = [&](auto&& f) {
       static_for<N>([&](auto b_c) {
-        constexpr int b = decltype(b_c)::value;
-        int row, col;
-        const int64_t to = place_of(first + b, row, col);
-        if (row < o.rows && col + 3 < o.cols) {
-          if (o.f32) {
-            old[b] = *(const f32x4_a4*)(out32 + to);
-          } else {
-            const u32x2 u = *(const u32x2_a2*)(out16 + to);
-            old[b][0] = __uint_as_float(u[0]), old[b][1] = __uint_as_float(u[1]);
-          }
-        } else if (row < o.rows) {
-          uint32_t u[2] = {0, 0};
+        constexpr int i = 16 * ((first + decltype(b_c)::value) / BJ);
+        constexpr int j = 16 * ((first + decltype(b_c)::value) % BJ);
+        const int row = row0 + (o.tall ? i : j), col = col0 + (o.tall ? j : i);
+        const int there = FULL ? 4 : row < o.rows ? min(o.cols - col, 4) : 0;
+        f(b_c, there, (int64_t)row * o.ld + col);
+      });
+    };
+    Old old[N];
+    if (o.step)
+      each([&](auto b_c, int there, int64_t to) {
+        Old& v = old[decltype(b_c)::value];
+        u32x2 u = {0, 0};
+        if (there >= 4) {
+          if constexpr (SPLIT)
+            if (f32) v = *(const f32x4_a4*)(out32 + to);
+          if (!f32) u = *(const u32x2_a2*)(out16 + to);
+        } else if constexpr (!FULL) {
 #pragma unroll
           for (int q = 0; q < 3; ++q)
-            if (col + q < o.cols) {
-              if (o.f32)
-                old[b][q] = out32[to + q];
-              else
-                u[q >> 1] |= (uint32_t)out16[to + q] << (16 * (q & 1));
+            if (q < there) {
+              if constexpr (SPLIT)
+                if (f32) v[q] = out32[to + q];
+              if (!f32) u[q >> 1] |= (uint32_t)out16[to + q] << (16 * (q & 1));
             }
-          if (!o.f32) old[b][0] = __uint_as_float(u[0]), old[b][1] = __uint_as_float(u[1]);
         }
+        if constexpr (!SPLIT)
+          v = u;
+        else if (!f32)
+          v[0] = __uint_as_float(u[0]), v[1] = __uint_as_float(u[1]);
       });
-    static_for<N>([&](auto b_c) {
-      constexpr int b = decltype(b_c)::value;
-      int row, col;
-      const int64_t to = place_of(first + b, row, col);
-      f32x4 w = val[(first + b) / BJ][(first + b) % BJ];
-      if (o.tall) w = quad_transpose(w, lane);
-      w *= 1.0f / S;
-      if (o.step) {
-        f32x4 was = old[b];
-        if (!o.f32) {
-          const uint32_t u0 = __float_as_uint(old[b][0]), u1 = __float_as_uint(old[b][1]);
-          was = f32x4{__uint_as_float(u0 << 16), __uint_as_float(u0 & 0xffff0000u),
-                      __uint_as_float(u1 << 16), __uint_as_float(u1 & 0xffff0000u)};
-        }
+    f32x4 w[N];
 #pragma unroll
-        for (int q = 0; q < 4; ++q) w[q] = fmaf(o.keep, was[q], -o.rate * w[q]);
+    for (int b = 0; b < N; ++b) w[b] = val[(first + b) / BJ][(first + b) % BJ];
+    if (o.tall)
+#pragma unroll
+      for (int b = 0; b < N; ++b) w[b] = quad_transpose(w[b], lane);
+#pragma unroll
+    for (int b = 0; b < N; ++b) {
+      w[b] *= 1.0f / S;
+      if (o.step) {
+        f32x4 was;
+        u32x2 u = {0, 0};
+        if constexpr (SPLIT) {
+          was = old[b];
+          u = u32x2{__float_as_uint(old[b][0]), __float_as_uint(old[b][1])};
+        } else {
+          u = old[b];
+        }
+        if (!f32)
+          was = f32x4{__uint_as_float(u[0] << 16), __uint_as_float(u[0] & 0xffff0000u),
+                      __uint_as_float(u[1] << 16), __uint_as_float(u[1] & 0xffff0000u)};
+#pragma unroll
+        for (int q = 0; q < 4; ++q) w[b][q] = fmaf(o.keep, was[q], -o.rate * w[b][q]);
       }
-      if (row >= o.rows) return;
+    }
+    each([&](auto b_c, int there, int64_t to) {
+      const f32x4 v = w[decltype(b_c)::value];
       uint16_t h[4];
 #pragma unroll
-      for (int q = 0; q < 4; ++q) h[q] = f32_to_bf16_bits(w[q]);
-      if (col + 3 < o.cols) {
-        if (o.f32)
-          *(f32x4_a4*)(out32 + to) = w;
+      for (int q = 0; q < 4; ++q) h[q] = f32_to_bf16_bits(v[q]);
+      if (there >= 4) {
+        if (f32)
+          *(f32x4_a4*)(out32 + to) = v;
         else
           *(u32x2_a2*)(out16 + to) =
               u32x2{h[0] | (uint32_t)h[1] << 16, h[2] | (uint32_t)h[3] << 16};
-      } else {
+      } else if constexpr (!FULL) {
 #pragma unroll
         for (int q = 0; q < 3; ++q)
-          if (col + q < o.cols) {
-            if (o.f32)
-              out32[to + q] = w[q];
+          if (q < there) {
+            if (f32)
+              out32[to + q] = v[q];
             else
               out16[to + q] = h[q];
           }
@@ -275,26 +293,29 @@ __global__ void __launch_bounds__(64 * T::WAVES)
   // workgroups go to the 8 XCDs in turn: each XCD takes a contiguous run of the tiles, its
   // workgroups neighbours in it, whose panels its L2 then holds
   const int nx = min(8, (int)gridDim.x), xcd = blockIdx.x % nx;
-  const int share = a.items / nx, extra = a.items % nx;
+  const int sub_m = a.unit_m / BM, subs = sub_m * (a.unit_n / BN), items = a.count * subs;
+  const int share = items / nx, extra = items % nx;
   const int first = xcd * share + min(xcd, extra), end = first + share + (xcd < extra ? 1 : 0);
   const int stride = (gridDim.x - xcd + nx - 1) / nx;    // workgroups on this XCD
   struct At {
-    int z, m0, n0, tm, tn;
+    int z, m0, n0;
+    bool below;       // a tile below the diagonal squares of its symmetric product
   };
   auto tile_at = [&](int item) {
-    At at;
-    const int t = item % a.tiles;
-    at.z = item / a.tiles;
+    const int unit = a.first + item / subs, sub = item % subs, t = unit % a.units;
+    int um, un, halves = 1;
     if constexpr (TR) {
-      grouped_tile(t, a.tiles_m, a.tiles_n, 8, at.tm, at.tn);
+      grouped_tile(t, a.units_m, a.units_n, 8, um, un);
     } else {
-      triangle_tile(t / T::HALVES, a.tiles_m, at.tm, at.tn);
-      at.tn = at.tn * T::HALVES + t % T::HALVES;
+      halves = a.unit_m / a.unit_n;
+      triangle_tile(t / halves, a.units_m, um, un);
+      un = un * halves + t % halves;
     }
-    at.z = __builtin_amdgcn_readfirstlane(at.z);
-    at.tm = __builtin_amdgcn_readfirstlane(at.tm);
-    at.tn = __builtin_amdgcn_readfirstlane(at.tn);
-    at.m0 = at.tm * BM, at.n0 = at.tn * BN;
+    At at;
+    at.z = __builtin_amdgcn_readfirstlane(unit / a.units);
+    at.m0 = __builtin_amdgcn_readfirstlane(um * a.unit_m + sub % sub_m * BM);
+    at.n0 = __builtin_amdgcn_readfirstlane(un * a.unit_n + sub / sub_m * BN);
+    at.below = __builtin_amdgcn_readfirstlane(un < um * halves);
     return at;
   };
   int item = first + blockIdx.x / nx;
@@ -533,7 +554,12 @@ __global__ void __launch_bounds__(64 * T::WAVES)
         for (int j = 0; j < BJ; ++j) val[i][j] = acc[i][j] * (1.0f / S);
     }
     if constexpr (MODE == RESULT) {
-      write_result<BI, BJ>(a.res, val, at.z, r0, c0, lane);
+      const int end_m = a.res.tall ? a.res.rows : a.res.cols;
+      const int end_n = a.res.tall ? a.res.cols : a.res.rows;
+      if (at.m0 + BM <= end_m && at.n0 + BN <= end_n)
+        write_result<SPLIT, true>(a.res, val, at.z, r0, c0, lane);
+      else if (at.m0 < end_m && at.n0 < end_n)
+        write_result<SPLIT, false>(a.res, val, at.z, r0, c0, lane);
       continue;
     }
     _Float16* const out = a.C.at + at.z * a.C.matrix;
@@ -554,7 +580,7 @@ __global__ void __launch_bounds__(64 * T::WAVES)
           *(u32x4*)p = u32x4{s0[0], s1[0], s0[1], s1[1]};
         }
     if constexpr (!TR) {
-      if (at.tn < at.tm * T::HALVES) {               // (a diagonal square is written whole)
+      if (at.below) {                                // (a diagonal square is written whole)
 #pragma unroll
         for (int i = 0; i < BI; ++i)
 #pragma unroll
@@ -728,38 +754,47 @@ constexpr int64_t MAX_SIDE = (int64_t)1 << 20, MAX_SHORT = (int64_t)1 << 16, MAX
 struct Plan {
   int64_t batch;
   int32_t r, k, tall;
-  int32_t tile[3];                          // rows of a tile of A, B and X
+  int32_t tile[3], tail[3];                 // rows of a tile of A, B and X; of its last round, or 0
   int64_t r_pad, k_pad;
   int32_t split, n_part;
   int64_t x_plane, a_plane;                 // elements
   size_t part, x[2], a, b, total;           // bytes
 };
 
-// Each product takes the tile that is done first: a round of workgroups lasts its stages, and a
-// tile's start and end come on top.  Nanoseconds a stage (measured, one part / two parts; a
-// 128 x 128 tile by whether a compute unit has one or two) and microseconds a launch:
-//   64 x 64   240 / 300                    6   five to nine stages in flight: few, small matrices
-//   128       650 / 900, 950 / 1300        6
-//   256 x 128 820                         10
+// What a launch of `items` tiles takes, in microseconds: a round of workgroups lasts its stages, a
+// tile's start and end come on top.  Measured per stage for one part and two (for 128 x 128 also by
+// whether a compute unit has one workgroup or two):
+//   64 x 64   0.24 / 0.30               + 6   nine stages in flight: few, small matrices
+//   128       0.65 / 0.90, 0.95 / 1.30  + 6
+//   256 x 128 0.82                      + 10
 // e.g. B X of 1024 x 1024: 9.5, 18 and 24 us; of 8 of them 42, 32 and 29; of 4096 x 4096 254, 137
 // and 125.  In two parts: 16 and 36 us; 95 and 57; 557 and 342.
+double product_us(int tile, bool split, double items, double stages) {
+  if (tile == 64) return ceil(items / 256) * stages * (split ? 0.30 : 0.24) + 6;
+  if (tile == 256) return ceil(items / 256) * stages * 0.82 + 10;
+  if (items <= 256) return stages * (split ? 0.90 : 0.65) + 6;
+  return ceil(items / 512) * stages * (split ? 1.30 : 0.95) + 6;
+}
+
+// Each product takes the tile that is done first; where its last round would leave most of the
+// chip idle, that round's tiles go to a launch of smaller ones (B X of 5120 x 5120: 800 tiles of
+// 256 x 128 are three rounds of 256 and 32 tiles more).
 void choose_tiles(Plan* p) {
-  const double unit = 256.0;
   for (int i = 0; i < 3; ++i) {
     double best = 0.0;
     for (int t = 64; t <= (p->split ? 128 : 256); t *= 2) {
       const double r = (double)cdiv(p->r, t), k = (double)cdiv(p->k, t);
       const double items = p->batch * (i == 2 ? r * k : r * (r + 1) / 2) * (t == 256 ? 2 : 1);
       const double stages = (i == 0 ? p->k : p->r) / (p->split ? 32.0 : 64.0);
-      double cost;
-      if (t == 64)
-        cost = ceil(items / unit) * stages * (p->split ? 0.30 : 0.24) + 6;
-      else if (t == 128)
-        cost = items <= unit ? stages * (p->split ? 0.90 : 0.65) + 6
-                             : ceil(items / (2 * unit)) * stages * (p->split ? 1.30 : 0.95) + 6;
-      else
-        cost = ceil(items / unit) * stages * 0.82 + 10;
-      if (t == 64 || cost < best) best = cost, p->tile[i] = t;
+      const double whole = floor(items / (t == 128 ? 512 : 256)) * (t == 128 ? 512 : 256);
+      for (int tail = 0; tail < t; tail = tail ? 2 * tail : 64) {
+        if (tail && (whole == 0 || whole == items)) continue;
+        const double subs = (double)t / tail * (t == 256 ? 128 : t) / tail;
+        const double us = tail ? product_us(t, p->split, whole, stages) +
+                                     product_us(tail, p->split, (items - whole) * subs, stages)
+                               : product_us(t, p->split, items, stages);
+        if (best == 0.0 || us < best) best = us, p->tile[i] = t, p->tail[i] = tail;
+      }
     }
   }
 }
@@ -795,17 +830,16 @@ bool make_plan(int64_t batch, int64_t m, int64_t n, int32_t out_dtype, Plan* p) 
   return true;
 }
 
+using Tile64 = Tile<2, 2, 2, 2, 9, 1>;
+using Tile128 = Tile<2, 2, 4, 4, 2, 2>;
+using Tile256 = Tile<2, 2, 8, 4, 3, 1>;
+
 template <int MODE, class T>
-void launch_tile(const Plan& p, Args a, hipStream_t s) {
-  constexpr bool TR = MODE == UPDATE || MODE == RESULT;
-  a.tiles_m = (int32_t)((TR ? p.k_pad : p.r_pad) / T::BM);
-  a.tiles_n = (int32_t)(p.r_pad / T::BN);
-  const int64_t tiles = TR ? (int64_t)a.tiles_m * a.tiles_n
-                           : (int64_t)a.tiles_m * (a.tiles_m + 1) / 2 * T::HALVES;
-  a.tiles = (int32_t)tiles, a.items = (int32_t)(tiles * p.batch);
+void launch_tile(const Plan& p, const Args& a, hipStream_t s) {
+  const int64_t items = (int64_t)a.count * (a.unit_m / T::BM) * (a.unit_n / T::BN);
   const int64_t most = (int64_t)device_cu_count() * T::PER_CU;
-  const dim3 grid((unsigned)(a.items < most ? a.items : most)), block(64 * T::WAVES);
-  if constexpr (T::BM <= 128) {       // (the two sums of the wide tile do not fit the registers)
+  const dim3 grid((unsigned)(items < most ? items : most)), block(64 * T::WAVES);
+  if constexpr (T::BM <= 128) {       // (a wide tile of two parts does not fit the registers)
     if (p.split) {
       hipLaunchKernelGGL((ns_product_kernel<MODE, true, T>), grid, block, 0, s, a);
       return;
@@ -814,19 +848,28 @@ void launch_tile(const Plan& p, Args a, hipStream_t s) {
   hipLaunchKernelGGL((ns_product_kernel<MODE, false, T>), grid, block, 0, s, a);
 }
 
-using Tile64 = Tile<2, 2, 2, 2, 9, 1>;
-using Tile128 = Tile<2, 2, 4, 4, 2, 2>;
-using Tile256 = Tile<2, 2, 8, 4, 3, 1>;
-
 template <int MODE>
-void launch(const Plan& p, const Args& a, hipStream_t s) {
-  const int tile = p.tile[MODE == GRAM ? 0 : MODE == SQUARE ? 1 : 2];
-  if (tile == 256)
-    launch_tile<MODE, Tile256>(p, a, s);
-  else if (tile == 128)
-    launch_tile<MODE, Tile128>(p, a, s);
-  else
-    launch_tile<MODE, Tile64>(p, a, s);
+void launch(const Plan& p, Args a, hipStream_t s) {
+  constexpr bool TR = MODE == UPDATE || MODE == RESULT;
+  const int i = MODE == GRAM ? 0 : MODE == SQUARE ? 1 : 2;
+  a.unit_m = p.tile[i], a.unit_n = p.tile[i] == 256 ? 128 : p.tile[i];
+  a.units_m = (int32_t)((TR ? p.k_pad : p.r_pad) / a.unit_m);
+  a.units_n = (int32_t)(p.r_pad / a.unit_n);
+  a.units = TR ? a.units_m * a.units_n : a.units_m * (a.units_m + 1) / 2 * (a.unit_m / a.unit_n);
+  const int32_t all = (int32_t)(a.units * p.batch);
+  const int32_t round = p.tile[i] == 128 ? 512 : 256;
+  for (int part = 0; part < 2; ++part) {
+    const int tile = part ? p.tail[i] : p.tile[i];
+    a.first = part ? all / round * round : 0;
+    a.count = (p.tail[i] && !part ? all / round * round : all) - a.first;
+    if (!tile || a.count <= 0) continue;
+    if (tile == 256)
+      launch_tile<MODE, Tile256>(p, a, s);
+    else if (tile == 128)
+      launch_tile<MODE, Tile128>(p, a, s);
+    else
+      launch_tile<MODE, Tile64>(p, a, s);
+  }
 }
 
 struct Steps {
