@@ -84,6 +84,7 @@ struct Args {
   // units_m down and units_n across); a launch takes `count` of them from `first` on, by tiles
   // that divide a unit.
   int32_t unit_m, unit_n, units_m, units_n, units, first, count;
+  int32_t sub_m_log, sub_n_log, halves_log;      // tiles of a unit down and across; units of a square
   Planes C;           // A, B or the next X
   float alpha, beta, shift;   // UPDATE: beta X + P Q; SQUARE: beta A + alpha P Q + shift I
   Result res;         // RESULT: in place of C
@@ -283,6 +284,7 @@ __global__ void __launch_bounds__(64 * T::WAVES)
   constexpr int BM = T::BM, BN = T::BN, BI = T::BI, BJ = T::BJ, NST = T::NST;
   constexpr int CP = T::CP, CQ = T::CQ, COPIES = CP + CQ;
   constexpr bool TR = MODE == UPDATE || MODE == RESULT;
+  constexpr bool SMALL = BI * BJ <= 4;
   constexpr int KROWS = SPLIT ? 32 : 64;         // k of a stage
   constexpr int TROW = BM * 128 / KROWS;         // bytes of a k-row of a transposed stage
   constexpr int LPR = TROW / 16;                 // lanes of a copy per k-row
@@ -292,34 +294,36 @@ __global__ void __launch_bounds__(64 * T::WAVES)
   const int wm = wave / T::WN, wn = wave % T::WN;
   // workgroups go to the 8 XCDs in turn: each XCD takes a contiguous run of the tiles, its
   // workgroups neighbours in it, whose panels its L2 then holds
-  const int nx = min(8, (int)gridDim.x), xcd = blockIdx.x % nx;
-  const int sub_m = a.unit_m / BM, subs = sub_m * (a.unit_n / BN), items = a.count * subs;
-  const int share = items / nx, extra = items % nx;
-  const int first = xcd * share + min(xcd, extra), end = first + share + (xcd < extra ? 1 : 0);
-  const int stride = (gridDim.x - xcd + nx - 1) / nx;    // workgroups on this XCD
+  const int sub_log = a.sub_m_log + a.sub_n_log, items = a.count << sub_log;
+  int item = blockIdx.x, end = item + 1, stride = 1;
+  if (gridDim.x >= 8) {
+    const int xcd = blockIdx.x & 7, share = items >> 3, extra = items & 7;
+    item = xcd * share + min(xcd, extra) + (blockIdx.x >> 3);
+    end = xcd * share + min(xcd, extra) + share + (xcd < extra ? 1 : 0);
+    stride = (gridDim.x - xcd + 7) >> 3;         // workgroups on this XCD
+  }
+  if (item >= end) return;
   struct At {
     int z, m0, n0;
     bool below;       // a tile below the diagonal squares of its symmetric product
   };
   auto tile_at = [&](int item) {
-    const int unit = a.first + item / subs, sub = item % subs, t = unit % a.units;
-    int um, un, halves = 1;
+    const int unit = a.first + (item >> sub_log), sub = item & ((1 << sub_log) - 1);
+    const int mat = unit < a.units ? 0 : unit / a.units, t = unit - mat * a.units;
+    int um, un;
     if constexpr (TR) {
       grouped_tile(t, a.units_m, a.units_n, 8, um, un);
     } else {
-      halves = a.unit_m / a.unit_n;
-      triangle_tile(t / halves, a.units_m, um, un);
-      un = un * halves + t % halves;
+      triangle_tile(t >> a.halves_log, a.units_m, um, un);
+      un = (un << a.halves_log) + (t & ((1 << a.halves_log) - 1));
     }
     At at;
-    at.z = __builtin_amdgcn_readfirstlane(unit / a.units);
-    at.m0 = __builtin_amdgcn_readfirstlane(um * a.unit_m + sub % sub_m * BM);
-    at.n0 = __builtin_amdgcn_readfirstlane(un * a.unit_n + sub / sub_m * BN);
-    at.below = __builtin_amdgcn_readfirstlane(un < um * halves);
+    at.z = __builtin_amdgcn_readfirstlane(mat);
+    at.m0 = __builtin_amdgcn_readfirstlane(um * a.unit_m + (sub & ((1 << a.sub_m_log) - 1)) * BM);
+    at.n0 = __builtin_amdgcn_readfirstlane(un * a.unit_n + (sub >> a.sub_m_log) * BN);
+    at.below = __builtin_amdgcn_readfirstlane(un < um << a.halves_log);
     return at;
   };
-  int item = first + blockIdx.x / nx;
-  if (item >= end) return;
 
   uint32_t offp[CP], offq[CQ];
   const uint32_t pitch_p = (uint32_t)(place<SPLIT>(a.P.ld, 1, 0) * 2);
@@ -348,7 +352,7 @@ __global__ void __launch_bounds__(64 * T::WAVES)
   const uint32_t lds0 = __builtin_amdgcn_readfirstlane((uint32_t)(uintptr_t)(lds_void_t*)smem);
   const int total = a.K / KROWS;
   const int64_t p_step = TR ? (int64_t)KROWS * pitch_p : 128;
-  // the next stage to copy: its operands, the stages left of its tile, that tile's item
+  // the next stage to copy: its operands, the stages left of its tile (0: none), that tile's item
   const uint8_t *p_at, *q_at;
   int left, copying = item;
   auto aim = [&](int it) {
@@ -365,7 +369,9 @@ __global__ void __launch_bounds__(64 * T::WAVES)
     else
       bf16k::copy16<(c - CQ) * 1024>(p_at, offp[c - CQ], buf + wave * CP * 1024);
   };
-  // (behind the last tile's last stage that stage is copied again, and read for nothing)
+  // Behind the last tile's last stage a small tile copies nothing more (its launches are latency,
+  // and of few stages); the others copy that stage again and read it for nothing, which keeps
+  // branches out of their stages.
   auto advance = [&]() {
     if (--left > 0) {
       p_at += p_step;
@@ -374,7 +380,7 @@ __global__ void __launch_bounds__(64 * T::WAVES)
       copying += stride;
       aim(copying);
     } else {
-      left = 1;
+      left = SMALL ? 0 : 1;
     }
   };
   aim(item);
@@ -431,9 +437,12 @@ __global__ void __launch_bounds__(64 * T::WAVES)
   };
   constexpr int READS = 2 * (BI + BJ), TERMS = SPLIT ? 3 : 2, SLOTS = BI * BJ * TERMS;
   int buf = 0;
-  auto stage = [&](auto par_c) {
+  auto stage_with = [&](auto par_c, auto copies_c) {
     constexpr int P = decltype(par_c)::value;
-    bf16k::wait_vmcnt<(NST - 2) * COPIES>();
+    constexpr bool COPY = decltype(copies_c)::value;
+    // the next stage has landed (vmcnt counts in order, and what else the wave has in flight is
+    // younger or makes the wait longer, never shorter); once nothing is copied any more, all have
+    bf16k::wait_vmcnt<COPY ? (NST - 2) * COPIES : 0>();
     lds_barrier();
     __builtin_amdgcn_sched_barrier(0);
     const int next = buf + 1 == NST ? 0 : buf + 1;
@@ -463,21 +472,30 @@ __global__ void __launch_bounds__(64 * T::WAVES)
           fp[P ^ 1][x - BJ][kk] = read_p(st, x - BJ, kk);
       });
       constexpr int c0 = q * COPIES / SLOTS, c1 = (q + 1) * COPIES / SLOTS;
-      static_for<c1 - c0>([&](auto n_c) {
-        copy(into, std::integral_constant<int, c0 + decltype(n_c)::value>{});
-      });
+      if constexpr (COPY)
+        static_for<c1 - c0>([&](auto n_c) {
+          copy(into, std::integral_constant<int, c0 + decltype(n_c)::value>{});
+        });
       __builtin_amdgcn_sched_barrier(0);
     });
     if constexpr (SPLIT) add(acc[BI - 1][BJ - 1], term3[(BI * BJ - 1) & 1]);
-    advance();
+    if constexpr (COPY) advance();
     buf = next;
   };
-#pragma unroll
-  for (int s = 0; s < NST; ++s) {
+  auto stage = [&](auto par_c) {
+    if (!SMALL || left > 0)
+      stage_with(par_c, std::true_type{});
+    else if constexpr (SMALL)
+      stage_with(par_c, std::false_type{});
+  };
+  for (int s = 0; s < NST && left > 0; ++s) {
     static_for<COPIES>([&](auto c) { copy(lds0 + s * T::STAGE, c); });
     advance();
   }
-  bf16k::wait_vmcnt<(NST - 1) * COPIES>();
+  if (left > 0)
+    bf16k::wait_vmcnt<(NST - 1) * COPIES>();
+  else
+    bf16k::wait_vmcnt<0>();
   lds_barrier();
 #pragma unroll
   for (int kk = 0; kk < 2; ++kk) {
@@ -507,8 +525,7 @@ __global__ void __launch_bounds__(64 * T::WAVES)
     // What the epilogue adds to: a small tile reads it ahead of its products (a launch of few of
     // them is latency), a larger one half a tile at a time behind them.
     constexpr bool OLD = MODE != GRAM, LO = SPLIT || TR, OLD_LO = OLD && LO;
-    constexpr bool EARLY = BI * BJ <= 4;
-    constexpr int HALF_J = EARLY ? BJ : BJ / 2;
+    constexpr int HALF_J = SMALL ? BJ : BJ / 2;
     f16x4 oh[OLD ? BI : 1][HALF_J], ol[OLD_LO ? BI : 1][HALF_J];
     auto read_old = [&](auto j_c) {
       constexpr int j0 = decltype(j_c)::value;
@@ -522,7 +539,7 @@ __global__ void __launch_bounds__(64 * T::WAVES)
           if constexpr (OLD_LO) ol[i][j] = *(const f16x4*)(p + lo_at<SPLIT>(a.P));
         }
     };
-    if constexpr (OLD && EARLY) read_old(std::integral_constant<int, 0>{});
+    if constexpr (OLD && SMALL) read_old(std::integral_constant<int, 0>{});
     for (int s = 0; s < total; s += 2) {
       stage(std::integral_constant<int, 0>{});
       stage(std::integral_constant<int, 1>{});
@@ -532,7 +549,7 @@ __global__ void __launch_bounds__(64 * T::WAVES)
     if constexpr (OLD) {
       static_for<BJ / HALF_J>([&](auto half) {
         constexpr int j0 = decltype(half)::value * HALF_J;
-        if constexpr (!EARLY) read_old(std::integral_constant<int, j0>{});
+        if constexpr (!SMALL) read_old(std::integral_constant<int, j0>{});
 #pragma unroll
         for (int i = 0; i < BI; ++i)
 #pragma unroll
@@ -835,8 +852,10 @@ using Tile128 = Tile<2, 2, 4, 4, 2, 2>;
 using Tile256 = Tile<2, 2, 8, 4, 3, 1>;
 
 template <int MODE, class T>
-void launch_tile(const Plan& p, const Args& a, hipStream_t s) {
-  const int64_t items = (int64_t)a.count * (a.unit_m / T::BM) * (a.unit_n / T::BN);
+void launch_tile(const Plan& p, Args a, hipStream_t s) {
+  while (T::BM << a.sub_m_log < a.unit_m) ++a.sub_m_log;
+  while (T::BN << a.sub_n_log < a.unit_n) ++a.sub_n_log;
+  const int64_t items = (int64_t)a.count << (a.sub_m_log + a.sub_n_log);
   const int64_t most = (int64_t)device_cu_count() * T::PER_CU;
   const dim3 grid((unsigned)(items < most ? items : most)), block(64 * T::WAVES);
   if constexpr (T::BM <= 128) {       // (a wide tile of two parts does not fit the registers)
@@ -855,6 +874,7 @@ void launch(const Plan& p, Args a, hipStream_t s) {
   a.unit_m = p.tile[i], a.unit_n = p.tile[i] == 256 ? 128 : p.tile[i];
   a.units_m = (int32_t)((TR ? p.k_pad : p.r_pad) / a.unit_m);
   a.units_n = (int32_t)(p.r_pad / a.unit_n);
+  a.halves_log = p.tile[i] == 256;
   a.units = TR ? a.units_m * a.units_n : a.units_m * (a.units_m + 1) / 2 * (a.unit_m / a.unit_n);
   const int32_t all = (int32_t)(a.units * p.batch);
   const int32_t round = p.tile[i] == 128 ? 512 : 256;
