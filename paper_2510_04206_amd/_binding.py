@@ -123,9 +123,9 @@ def _rows(t: Optional[torch.Tensor]):
         return None
     if not t.is_cuda:
         raise ValueError("agrl: arrays must be GPU tensors (the ABI takes device pointers)")
-    if t.shape[-1] > 1 and t.stride(-1) != 1:
+    if t.stride(-1) != 1 and t.shape[-1] > 1:
         raise ValueError("agrl: the elements of a row must be adjacent")
-    return ctypes.c_void_p(t.data_ptr())
+    return t.data_ptr()
 
 
 def _stream(stream) -> ctypes.c_void_p:

@@ -12,7 +12,7 @@ _CODES = {torch.bfloat16: B.AGRL_BF16, torch.float32: B.AGRL_F32}
 
 def _need(t: torch.Tensor, name: str, shape, dtypes) -> None:
     """The binding sees only addresses: what a tensor must be is checked here."""
-    if tuple(t.shape) != tuple(shape):
+    if t.shape != shape:
         raise ValueError(f"agrl: {name} has shape {tuple(t.shape)}, expected {tuple(shape)}")
     if t.dtype not in dtypes:
         raise TypeError(f"agrl: {name} has dtype {t.dtype}, expected one of {dtypes}")

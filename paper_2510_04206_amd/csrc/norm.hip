@@ -181,12 +181,21 @@ struct Lane {
 #pragma unroll
     for (int c = 0; c < NC; ++c)
 #pragma unroll
-      for (int k = 0; k < CH; ++k) {
-        const int i = col(c) + k;
-        w[c][k] = !p || i >= d ? none
-                  : dtype == AGRL_BF16 ? bf16_bits_to_f32(((const uint16_t*)p)[i])
-                                       : ((const float*)p)[i];
-      }
+      for (int k = 0; k < CH; ++k) w[c][k] = none;
+    if (!p) return;
+    if (dtype == AGRL_BF16)
+      param_as(w, (const uint16_t*)p);
+    else
+      param_as(w, (const float*)p);
+  }
+  template <typename T>
+  __device__ __forceinline__ void param_as(float (&w)[NC][CH], const T* p) const {
+    Chunk<T> x[NC];
+    load(x, p);
+#pragma unroll
+    for (int c = 0; c < NC; ++c)
+#pragma unroll
+      for (int k = 0; k < CH; ++k) w[c][k] = x[c].get(k);   // (past the row: 0, used by no one)
   }
 };
 
@@ -508,8 +517,9 @@ void with_team(int d, F&& f) {
 constexpr int MAX_D = 16384;
 constexpr int64_t MAX_T = (int64_t)1 << 40;
 
-// Workgroups of the backward: each leaves one partial sum of 2 d floats, so their number is
-// bounded; enough of them that every compute unit has several rows in flight.
+// Workgroups of the backward: each leaves a partial sum of 2 d floats, so their number is bounded:
+// two a compute unit, with two rows each in flight.  65536 x 4096 dense 294 us (three 320, four
+// 343), 32768 x 3584 with a third of the rows live 120 (119, 124).
 constexpr int BWD_GROUPS = 512;
 int teams_per_group(int d) { return d <= 1024 ? 4 : 1; }
 int bwd_groups(int64_t T, int d) {
@@ -550,7 +560,9 @@ extern "C" int agrl_token_norm_fwd(int64_t T, int32_t d, int32_t kind, int32_t d
   hipStream_t s = (hipStream_t)stream;
   with_team(d, [&](auto team, auto nc) {
     constexpr int TEAM = decltype(team)::value, NC = decltype(nc)::value;
-    constexpr int PER = 2048 / Shape<TEAM>::BLOCK;   // workgroups that fill a compute unit
+    // 1024 lanes on a compute unit, each team several rows: 65536 x 5120 189 us (2048 lanes 192,
+    // 512 192), 100000 x 512 44 (50, 57)
+    constexpr int PER = 1024 / Shape<TEAM>::BLOCK;
     const int64_t need = cdiv(T, (int64_t)Shape<TEAM>::TEAMS);
     const int64_t most = (int64_t)device_cu_count() * PER;
     const dim3 grid((unsigned)(need < most ? need : most)), block(Shape<TEAM>::BLOCK);
