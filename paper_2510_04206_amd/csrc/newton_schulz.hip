@@ -388,7 +388,7 @@ __global__ void __launch_bounds__(64 * T::WAVES)
   // Two parts: a stage's three terms are summed by themselves and then added (rounded to
   // nearest) to the running sum: the matrix cores' own additions onto a large sum would lose
   // more than the operands do.
-  f32x4 acc[BI][BJ], term3[2];
+  f32x4 acc[BI][BJ], terms[SPLIT ? 3 : 1];
   const int fr = lane & 15, g = lane >> 4;
   int rp[2], rq[2];
 #pragma unroll
@@ -430,10 +430,17 @@ __global__ void __launch_bounds__(64 * T::WAVES)
     return *(const f16x8*)(st + rq[kk] + j * 16 * 128);
   };
 
-  // (pinned where it stands: gathered behind the stage, the additions would not hide under it)
-  auto add = [](f32x4& to, const f32x4& v) {
-    to += v;
-    asm volatile("" : "+v"(to));
+  // half h of block b's sum (pinned where it stands: gathered behind the stage, the additions
+  // would not hide under it)
+  auto add = [&](auto b_c, auto h_c) {
+    constexpr int b = decltype(b_c)::value, h = decltype(h_c)::value;
+    f32x4& to = acc[b / BJ][b % BJ];
+#pragma unroll
+    for (int q = 2 * h; q < 2 * h + 2; ++q) {
+      float v = to[q] + terms[b % 3][q];
+      asm volatile("" : "+v"(v));
+      to[q] = v;
+    }
   };
   constexpr int READS = 2 * (BI + BJ), TERMS = SPLIT ? 3 : 2, SLOTS = BI * BJ * TERMS;
   int buf = 0;
@@ -454,11 +461,13 @@ __global__ void __launch_bounds__(64 * T::WAVES)
       // two parts: hi lo, lo hi, hi hi; one part: the stage's two k halves
       constexpr int kp = SPLIT ? term == 1 : term, kq = SPLIT ? term == 0 : term;
       if constexpr (SPLIT) {
-        constexpr int b = q / TERMS;             // block: its three terms, then the one before's sum
+        // (a block's sum is added two blocks later: the matrix pipe has it by then)
+        constexpr int b = q / TERMS;
         const f32x4 zero = {0.0f, 0.0f, 0.0f, 0.0f};
-        term3[b & 1] = __builtin_amdgcn_mfma_f32_16x16x32_f16(
-            fp[P][i][kp], fq[P][j][kq], term ? term3[b & 1] : zero, 0, 0, 0);
-        if constexpr (term == 2 && b > 0) add(acc[(b - 1) / BJ][(b - 1) % BJ], term3[(b - 1) & 1]);
+        terms[b % 3] = __builtin_amdgcn_mfma_f32_16x16x32_f16(
+            fp[P][i][kp], fq[P][j][kq], term ? terms[b % 3] : zero, 0, 0, 0);
+        if constexpr (term < 2 && b > 1) 
+          add(std::integral_constant<int, b - 2>{}, std::integral_constant<int, term>{});
       } else {
         acc[i][j] =
             __builtin_amdgcn_mfma_f32_16x16x32_f16(fp[P][i][kp], fq[P][j][kq], acc[i][j], 0, 0, 0);
@@ -478,7 +487,12 @@ __global__ void __launch_bounds__(64 * T::WAVES)
         });
       __builtin_amdgcn_sched_barrier(0);
     });
-    if constexpr (SPLIT) add(acc[BI - 1][BJ - 1], term3[(BI * BJ - 1) & 1]);
+    if constexpr (SPLIT)
+      static_for<2>([&](auto b) {
+        constexpr int last = BI * BJ - 2 + decltype(b)::value;
+        add(std::integral_constant<int, last>{}, std::integral_constant<int, 0>{});
+        add(std::integral_constant<int, last>{}, std::integral_constant<int, 1>{});
+      });
     if constexpr (COPY) advance();
     buf = next;
   };
