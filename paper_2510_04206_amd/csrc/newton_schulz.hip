@@ -278,9 +278,10 @@ constexpr int reads_before(int q, int reads, int slots) {
 // landed.  Stages run on from a workgroup's tile to its next one (an even number of them per
 // tile: the two register sets alternate), so a tile's first stages arrive under the last
 // products and the epilogue of the tile before.
+// (items item, item + stride, ... below end; smem: NST stages)
 template <int MODE, bool SPLIT, class T>
-__global__ void __launch_bounds__(64 * T::WAVES)
-    __attribute__((amdgpu_waves_per_eu(T::EU_WAVES, T::EU_WAVES))) ns_product_kernel(Args a) {
+__device__ __forceinline__ void product(const Args& a, int item, const int end, const int stride,
+                                        uint8_t* const smem) {
   constexpr int BM = T::BM, BN = T::BN, BI = T::BI, BJ = T::BJ, NST = T::NST;
   constexpr int CP = T::CP, CQ = T::CQ, COPIES = CP + CQ;
   constexpr bool TR = MODE == UPDATE || MODE == RESULT;
@@ -288,21 +289,10 @@ __global__ void __launch_bounds__(64 * T::WAVES)
   constexpr int KROWS = SPLIT ? 32 : 64;         // k of a stage
   constexpr int TROW = BM * 128 / KROWS;         // bytes of a k-row of a transposed stage
   constexpr int LPR = TROW / 16;                 // lanes of a copy per k-row
-  __shared__ __attribute__((aligned(1024))) uint8_t smem[NST * T::STAGE];
   const int lane = threadIdx.x & 63;
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int wm = wave / T::WN, wn = wave % T::WN;
-  // workgroups go to the 8 XCDs in turn: each XCD takes a contiguous run of the tiles, its
-  // workgroups neighbours in it, whose panels its L2 then holds
-  const int sub_log = a.sub_m_log + a.sub_n_log, items = a.count << sub_log;
-  int item = blockIdx.x, end = item + 1, stride = 1;
-  if (gridDim.x >= 8) {
-    const int xcd = blockIdx.x & 7, share = items >> 3, extra = items & 7;
-    item = xcd * share + min(xcd, extra) + (blockIdx.x >> 3);
-    end = xcd * share + min(xcd, extra) + share + (xcd < extra ? 1 : 0);
-    stride = (gridDim.x - xcd + 7) >> 3;         // workgroups on this XCD
-  }
-  if (item >= end) return;
+  const int sub_log = a.sub_m_log + a.sub_n_log;
   struct At {
     int z, m0, n0;
     bool below;       // a tile below the diagonal squares of its symmetric product
@@ -625,7 +615,26 @@ __global__ void __launch_bounds__(64 * T::WAVES)
       }
     }
   }
-  asm volatile("s_waitcnt vmcnt(0)" ::: "memory");   // no copy outlives the workgroup's LDS
+  // no copy outlives the workgroup's LDS, and what was written can be read behind a barrier
+  asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+}
+
+template <int MODE, bool SPLIT, class T>
+__global__ void __launch_bounds__(64 * T::WAVES)
+    __attribute__((amdgpu_waves_per_eu(T::EU_WAVES, T::EU_WAVES))) ns_product_kernel(Args a) {
+  __shared__ __attribute__((aligned(1024))) uint8_t smem[T::NST * T::STAGE];
+  // workgroups go to the 8 XCDs in turn: each XCD takes a contiguous run of the tiles, its
+  // workgroups neighbours in it, whose panels its L2 then holds
+  const int items = a.count << (a.sub_m_log + a.sub_n_log);
+  int item = blockIdx.x, end = item + 1, stride = 1;
+  if (gridDim.x >= 8) {
+    const int xcd = blockIdx.x & 7, share = items >> 3, extra = items & 7;
+    item = xcd * share + min(xcd, extra) + (blockIdx.x >> 3);
+    end = xcd * share + min(xcd, extra) + share + (xcd < extra ? 1 : 0);
+    stride = (gridDim.x - xcd + 7) >> 3;         // workgroups on this XCD
+  }
+  if (item >= end) return;
+  product<MODE, SPLIT, T>(a, item, end, stride, smem);
 }
 
 // ---------------------------------------------------------------------------
@@ -681,6 +690,54 @@ __device__ __forceinline__ double block_sum(double v, double* lds) {
   return v;
 }
 
+// What is orthogonalised, of a gradient g and the momentum m that has taken it in.
+__device__ __forceinline__ float momentum_u(const Source& s, float m, float g) {
+  return s.nesterov ? fmaf(s.mu, m, g) : m;
+}
+
+// Run j of 8 entries of row i of the matrix at `base`: the momentum takes it in, sum += u^2.
+__device__ __forceinline__ void source_run(const Source& s, int64_t base, float* mom, int64_t i,
+                                           int j, double (&sum)[2]) {
+  const int n = s.cols - 8 * j;
+  float u[8];
+  load8(s.g, s.f32, base + i * s.ld + 8 * j, n, u);
+  if (mom) {
+    float* const p = mom + i * s.cols + 8 * j;
+    float m[8];
+    load8(p, true, 0, n, m);
+#pragma unroll
+    for (int k = 0; k < 8; ++k) {
+      m[k] = fmaf(s.mu, m[k], u[k]);
+      u[k] = momentum_u(s, m[k], u[k]);
+    }
+    if (n >= 8) {
+      *(f32x4_any*)p = f32x4{m[0], m[1], m[2], m[3]};
+      *(f32x4_any*)(p + 4) = f32x4{m[4], m[5], m[6], m[7]};
+    } else {
+#pragma unroll
+      for (int k = 0; k < 7; ++k)
+        if (k < n) p[k] = m[k];
+    }
+  }
+#pragma unroll
+  for (int k = 0; k < 8; ++k) sum[k & 1] = fma((double)u[k], (double)u[k], sum[k & 1]);
+}
+
+// Eight neighbours of a row of X, scaled.
+template <bool SPLIT>
+__device__ __forceinline__ void store_x(const Planes& X, int64_t z, int64_t row, int64_t col,
+                                        const float (&v)[8], float inv) {
+  f16x8 hi, lo;
+#pragma unroll
+  for (int k = 0; k < 8; ++k) {
+    const HiLo x = split(v[k] * inv);
+    hi[k] = x.hi, lo[k] = x.lo;
+  }
+  _Float16* p = X.at + z * X.matrix + place<SPLIT>(X.ld, row, col);
+  *(f16x8*)p = hi;
+  *(f16x8*)(p + lo_at<SPLIT>(X)) = lo;
+}
+
 // Runs of 8 entries, `runs` of them a row.
 __global__ void __launch_bounds__(NORM_THREADS) ns_norm_kernel(Source s, double* part) {
   const int64_t z = blockIdx.y;
@@ -694,29 +751,7 @@ __global__ void __launch_bounds__(NORM_THREADS) ns_norm_kernel(Source s, double*
   int j = (int)(e - i * runs);
   double sum[2] = {0.0, 0.0};
   for (; e < all; e += step) {
-    const int n = s.cols - 8 * j;
-    float u[8];
-    load8(s.g, s.f32, z * s.matrix + i * s.ld + 8 * j, n, u);
-    if (mom) {
-      float* const p = mom + i * s.cols + 8 * j;
-      float m[8];
-      load8(p, true, 0, n, m);
-#pragma unroll
-      for (int k = 0; k < 8; ++k) {
-        m[k] = fmaf(s.mu, m[k], u[k]);
-        u[k] = s.nesterov ? fmaf(s.mu, m[k], u[k]) : m[k];
-      }
-      if (n >= 8) {
-        *(f32x4_any*)p = f32x4{m[0], m[1], m[2], m[3]};
-        *(f32x4_any*)(p + 4) = f32x4{m[4], m[5], m[6], m[7]};
-      } else {
-#pragma unroll
-        for (int k = 0; k < 7; ++k)
-          if (k < n) p[k] = m[k];
-      }
-    }
-#pragma unroll
-    for (int k = 0; k < 8; ++k) sum[k & 1] = fma((double)u[k], (double)u[k], sum[k & 1]);
+    source_run(s, z * s.matrix, mom, i, j, sum);
     i += step_i;
     j += step_j;
     if (j >= runs) j -= runs, ++i;
@@ -746,7 +781,7 @@ __global__ void __launch_bounds__(PRE)
       float m[8];
       load8(s.m, true, z * s.rows * s.cols + i * s.cols + j, n, m);
 #pragma unroll
-      for (int k = 0; k < 8; ++k) v[h][k] = s.nesterov ? fmaf(s.mu, m[k], v[h][k]) : m[k];
+      for (int k = 0; k < 8; ++k) v[h][k] = momentum_u(s, m[k], v[h][k]);
     }
   }
   const double total = block_sum<PRE>(t < n_part ? part[z * n_part + t] : 0.0, red);
@@ -763,18 +798,84 @@ __global__ void __launch_bounds__(PRE)
       for (int k = 0; k < 8; ++k) v[h][k] = tile[(t & 7) * 8 + k][(t >> 3) + 32 * h];
   }
 #pragma unroll
-  for (int h = 0; h < 2; ++h) {
-    f16x8 hi, lo;
+  for (int h = 0; h < 2; ++h)
+    store_x<SPLIT>(X, z, (int64_t)blockIdx.y * 64 + (t >> 3) + 32 * h,
+                   (int64_t)blockIdx.x * 64 + (t & 7) * 8, v[h], inv);
+}
+
+struct Steps {
+  int32_t n;
+  float a, b, c, eps;
+};
+
+// A matrix of up to 64 rows and SMALL_K columns: everything in one workgroup, a launch for the whole
+// stack.  What the separate launches of such a matrix take is mostly their starts (4 of 6 to 9 us
+// each, seventeen of them); one compute unit's matrix cores are enough for its products.
+using TileOne = Tile<2, 2, 2, 2, 9, 1>;
+using TileOneX = Tile<2, 2, 4, 2, 4, 1>;      // B X: fewer, wider tiles, one after the other
+constexpr int SMALL_ROWS = 64, SMALL_K = 256;
+
+__global__ void __launch_bounds__(64 * TileOne::WAVES)
+    ns_small_kernel(Source s, Steps o, Result res, Planes X0, Planes X1, Planes A, Planes B) {
+  constexpr int THREADS = 64 * TileOne::WAVES;
+  __shared__ __attribute__((aligned(1024))) uint8_t smem[TileOne::NST * TileOne::STAGE];
+  __shared__ double red[THREADS / 64];
+  const int z = blockIdx.x;
+  const int64_t base = z * s.matrix;
+  float* const mom = s.m ? s.m + (int64_t)z * s.rows * s.cols : nullptr;
+  const int runs = (s.cols + 7) / 8;
+  double sum[2] = {0.0, 0.0};
+  for (int e = threadIdx.x; e < s.rows * runs; e += THREADS)
+    source_run(s, base, mom, e / runs, e % runs, sum);
+  const double total = block_sum<THREADS>(sum[0] + sum[1], red);
+  const float inv = (float)((double)S / (sqrt(total) + (double)o.eps));
+  // X, zero beyond the matrix
+  const int k_runs = (int)X0.ld / 8;
+  for (int e = threadIdx.x; e < SMALL_ROWS * k_runs; e += THREADS) {
+    const int row = e / k_runs, col = e % k_runs * 8;
+    float v[8];
+    if (res.tall) {
 #pragma unroll
-    for (int k = 0; k < 8; ++k) {
-      const HiLo x = split(v[h][k] * inv);
-      hi[k] = x.hi, lo[k] = x.lo;
+      for (int k = 0; k < 8; ++k) {
+        const int i = col + k;
+        const bool in = i < s.rows && row < s.cols;
+        float u[8] = {};
+        load8(s.g, s.f32, in ? base + i * s.ld + row : 0, in ? 1 : 0, u);
+        v[k] = u[0];
+        if (mom) v[k] = momentum_u(s, in ? mom[i * s.cols + row] : 0.0f, u[0]);
+      }
+    } else {
+      const int n = row < s.rows ? s.cols - col : 0;
+      load8(s.g, s.f32, base + row * s.ld + col, n, v);
+      if (mom) {
+        float m[8];
+        load8(mom, true, row * s.cols + col, n, m);
+#pragma unroll
+        for (int k = 0; k < 8; ++k) v[k] = momentum_u(s, m[k], v[k]);
+      }
     }
-    _Float16* p = X.at + z * X.matrix +
-                  place<SPLIT>(X.ld, (int64_t)blockIdx.y * 64 + (t >> 3) + 32 * h,
-                               (int64_t)blockIdx.x * 64 + (t & 7) * 8);
-    *(f16x8*)p = hi;
-    *(f16x8*)(p + lo_at<SPLIT>(X)) = lo;
+    store_x<true>(X0, z, row, col, v, inv);
+  }
+  Args a = {};
+  a.unit_m = a.unit_n = 64;
+  a.res = res;
+  const int k_tiles = (int)X0.ld / TileOneX::BM;
+  for (int i = 0; i < o.n; ++i) {
+    const Planes& X = i & 1 ? X1 : X0;
+    __syncthreads();
+    a.unit_m = 64, a.units_m = a.units_n = a.units = a.count = 1, a.first = z;
+    a.P = a.Q = X, a.K = (int)X0.ld, a.C = A;
+    product<GRAM, true, TileOne>(a, 0, 1, 1, smem);
+    __syncthreads();
+    a.P = a.Q = A, a.K = SMALL_ROWS, a.C = B, a.alpha = o.c, a.beta = o.b, a.shift = 0.0f;
+    product<SQUARE, true, TileOne>(a, 0, 1, 1, smem);
+    __syncthreads();
+    a.unit_m = TileOneX::BM, a.units_m = a.units = a.count = k_tiles, a.first = z * k_tiles;
+    a.P = X, a.Q = B, a.C = i & 1 ? X0 : X1, a.beta = o.a;
+    if (i == o.n - 1)
+      product<RESULT, true, TileOneX>(a, 0, k_tiles, 1, smem);
+    else
+      product<UPDATE, true, TileOneX>(a, 0, k_tiles, 1, smem);
   }
 }
 
@@ -784,7 +885,7 @@ constexpr int64_t MAX_SIDE = (int64_t)1 << 20, MAX_SHORT = (int64_t)1 << 16, MAX
 // Sizes and the workspace of a stack of matrices
 struct Plan {
   int64_t batch;
-  int32_t r, k, tall;
+  int32_t r, k, tall, one;                  // one: ns_small_kernel's
   int32_t tile[3], tail[3];                 // rows of a tile of A, B and X; of its last round, or 0
   int64_t r_pad, k_pad;
   int32_t split, n_part;
@@ -838,9 +939,10 @@ bool make_plan(int64_t batch, int64_t m, int64_t n, int32_t out_dtype, Plan* p) 
   p->batch = batch, p->r = (int32_t)r, p->k = (int32_t)k, p->tall = m > n;
   p->split = out_dtype == AGRL_F32 || r <= SPLIT_ROWS;
   choose_tiles(p);
+  p->one = p->r <= SMALL_ROWS && p->k <= SMALL_K;
   int64_t pad = 128;
   for (int i = 0; i < 3; ++i) pad = p->tile[i] > pad ? p->tile[i] : pad;
-  p->r_pad = cdiv(r, pad) * pad;
+  p->r_pad = p->one ? 64 : cdiv(r, pad) * pad;
   p->k_pad = cdiv(k, pad) * pad;
   const int64_t per = cdiv(m * cdiv(n, (int64_t)8), (int64_t)NORM_THREADS);
   p->n_part = (int32_t)(per < NORM_GROUPS ? per : NORM_GROUPS);
@@ -861,7 +963,7 @@ bool make_plan(int64_t batch, int64_t m, int64_t n, int32_t out_dtype, Plan* p) 
   return true;
 }
 
-using Tile64 = Tile<2, 2, 2, 2, 9, 1>;
+using Tile64 = TileOne;
 using Tile128 = Tile<2, 2, 4, 4, 2, 2>;
 using Tile256 = Tile<2, 2, 8, 4, 3, 1>;
 
@@ -906,22 +1008,22 @@ void launch(const Plan& p, Args a, hipStream_t s) {
   }
 }
 
-struct Steps {
-  int32_t n;
-  float a, b, c, eps;
-};
-
 void run(const Plan& p, const Steps& o, const Source& src, const Result& res, uint8_t* ws,
          hipStream_t s) {
   double* part = (double*)(ws + p.part);
-  hipLaunchKernelGGL(ns_norm_kernel, dim3(p.n_part, (unsigned)p.batch), dim3(NORM_THREADS), 0, s,
-                     src, part);
   Planes X[2], A, B;
   const int64_t parts = p.split ? 2 : 1;      // interleaved
   for (int i = 0; i < 2; ++i)
     X[i] = Planes{(_Float16*)(ws + p.x[i]), parts * p.r_pad * p.k_pad, p.x_plane, p.k_pad};
   A = Planes{(_Float16*)(ws + p.a), parts * p.r_pad * p.r_pad, 0, p.r_pad};
   B = Planes{(_Float16*)(ws + p.b), parts * p.r_pad * p.r_pad, 0, p.r_pad};
+  if (p.one) {
+    hipLaunchKernelGGL(ns_small_kernel, dim3((unsigned)p.batch), dim3(64 * TileOne::WAVES), 0, s, src,
+                       o, res, X[0], X[1], A, B);
+    return;
+  }
+  hipLaunchKernelGGL(ns_norm_kernel, dim3(p.n_part, (unsigned)p.batch), dim3(NORM_THREADS), 0, s,
+                     src, part);
   const dim3 grid((unsigned)(p.k_pad / 64), (unsigned)(p.r_pad / 64), (unsigned)p.batch);
   if (p.split)
     hipLaunchKernelGGL(ns_start_kernel<true>, grid, dim3(PRE), 0, s, src, part, p.n_part, o.eps,

@@ -96,6 +96,20 @@ def test_larger_tiles(m, n, batch, out):
         _check(got[i], x[i], _off32(x[i]) if out == F32 else 0.0)
 
 
+# both sides of the sizes that one workgroup holds (64 rows, 256 columns), several to a stack
+@pytest.mark.parametrize("m,n", [(64, 256), (256, 64), (64, 257), (63, 129), (65, 256), (2, 200),
+                                 (255, 40)])
+@pytest.mark.parametrize("out", [BF, F32])
+def test_small_stacks(m, n, out):
+    import paper_2510_04206_amd as P
+    log(f"orthogonalize 5 x {m} x {n} -> {out}")
+    x = torch.stack([_matrix(m, n, kind, seed=i) for i, kind in
+                     enumerate(("flat", "steep", "few", "flat", "steep"))])
+    got = P.Orthogonalize(m, n, out_dtype=out, batch=5)(x.cuda())
+    for i in range(5):
+        _check(got[i], x[i], _off32(x[i]) if out == F32 else 0.0)
+
+
 @pytest.mark.parametrize("out", [BF, F32])
 def test_transposed_input_transposes_the_result(out):
     import paper_2510_04206_amd as P
@@ -171,7 +185,8 @@ def test_scales_zero_and_non_finite():
 
 @pytest.mark.parametrize("grad_dtype,param_dtype", [(F32, F32), (BF, F32), (F32, BF), (BF, BF)])
 @pytest.mark.parametrize("m,n,batch,nesterov", [(70, 200, None, True), (300, 128, None, False),
-                                                (96, 96, 3, True)])
+                                                (96, 96, 3, True), (50, 333, 2, True),
+                                                (201, 64, None, False), (1300, 1100, None, True)])
 def test_muon_steps(grad_dtype, param_dtype, m, n, batch, nesterov):
     """Three steps.  Momentum: one rounding of each term a step, 4 u of their sizes.  Parameter:
     lr scale O off by the bounds above, and u (bf16: 2^-9) of itself a step."""
