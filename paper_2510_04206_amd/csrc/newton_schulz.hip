@@ -66,7 +66,8 @@ __device__ __forceinline__ int64_t lo_at(const Planes& p) {
   return SPLIT ? 32 : p.lo;
 }
 
-enum { GRAM, SQUARE, UPDATE, RESULT };   // A = X X^T; B = bA + cAA + shift I; X = aX + BX, twice
+// A = X X^T; B = b A + c A A + shift I; X = beta X + B X, and the last of these
+enum { GRAM, SQUARE, UPDATE, RESULT };
 
 // What the last product writes: O, or the weight it updates.
 struct Result {
@@ -87,18 +88,20 @@ struct Args {
   int32_t sub_m_log, sub_n_log, halves_log;      // tiles of a unit down and across; units of a square
   Planes C;           // A, B or the next X
   float alpha, beta, shift;   // UPDATE: beta X + P Q; SQUARE: beta A + alpha P Q + shift I
+  int32_t keep_lo;            // UPDATE of one part: lo is read again
   Result res;         // RESULT: in place of C
 };
 
 // A tile of BM x BN by WM x WN waves, each BI x BJ blocks of 16 x 16; NST stages in LDS, each 128
 // bytes of every row: 64 k, or 32 k in two parts.
-template <int WM_, int WN_, int BI_, int BJ_, int NST_, int PER_CU_>
+template <int WM_, int WN_, int BI_, int BJ_, int NST_, int PER_CU_, bool EARLY_ = false>
 struct Tile {
+  static constexpr bool EARLY = EARLY_;          // the epilogue's inputs are read ahead of the products
   static constexpr int WM = WM_, WN = WN_, BI = BI_, BJ = BJ_, NST = NST_;
   static constexpr int PER_CU = PER_CU_;         // workgroups of a compute unit
   // registers: 256 per lane hold all of a tile up to 128 x 128, and no accumulator then moves
   // between the two register files
-  static constexpr int EU_WAVES = BI_ * BJ_ <= 16 ? 2 : 1;
+  static constexpr int EU_WAVES = BI_ * BJ_ <= 4 || PER_CU_ > 1 ? 2 : 1;
   static constexpr int BM = WM * BI * 16, BN = WN * BJ * 16, WAVES = WM * WN;
   static constexpr int P_BYTES = BM * 128, STAGE = (BM + BN) * 128;
   static constexpr int CP = BM / 8 / WAVES, CQ = BN / 8 / WAVES;   // 1 KiB copies of a wave
@@ -516,7 +519,7 @@ __device__ __forceinline__ void product(const Args& a, int item, const int end, 
     // (the wide tile's sums live in the accumulation registers on both sides of the loop:
     // otherwise the allocator moves them to and fro inside it)
     auto pin = [&]() {
-      if constexpr (T::EU_WAVES == 1)
+      if constexpr (T::EU_WAVES == 1 && !SPLIT)
 #pragma unroll
         for (int i = 0; i < BI; ++i)
 #pragma unroll
@@ -528,8 +531,9 @@ __device__ __forceinline__ void product(const Args& a, int item, const int end, 
     const int r0 = at.m0 + wm * BI * 16 + 4 * g, c0 = at.n0 + wn * BJ * 16 + fr;
     // What the epilogue adds to: a small tile reads it ahead of its products (a launch of few of
     // them is latency), a larger one half a tile at a time behind them.
-    constexpr bool OLD = MODE != GRAM, LO = SPLIT || TR, OLD_LO = OLD && LO;
-    constexpr int HALF_J = SMALL ? BJ : BJ / 2;
+    constexpr bool OLD = MODE == SQUARE || MODE == UPDATE || (MODE == RESULT && SPLIT);
+    constexpr bool LO = SPLIT || TR, OLD_LO = OLD && LO;
+    constexpr int HALF_J = T::EARLY ? BJ : BJ / 2;
     f16x4 oh[OLD ? BI : 1][HALF_J], ol[OLD_LO ? BI : 1][HALF_J];
     auto read_old = [&](auto j_c) {
       constexpr int j0 = decltype(j_c)::value;
@@ -543,7 +547,7 @@ __device__ __forceinline__ void product(const Args& a, int item, const int end, 
           if constexpr (OLD_LO) ol[i][j] = *(const f16x4*)(p + lo_at<SPLIT>(a.P));
         }
     };
-    if constexpr (OLD && SMALL) read_old(std::integral_constant<int, 0>{});
+    if constexpr (OLD && T::EARLY) read_old(std::integral_constant<int, 0>{});
     for (int s = 0; s < total; s += 2) {
       stage(std::integral_constant<int, 0>{});
       stage(std::integral_constant<int, 1>{});
@@ -553,7 +557,7 @@ __device__ __forceinline__ void product(const Args& a, int item, const int end, 
     if constexpr (OLD) {
       static_for<BJ / HALF_J>([&](auto half) {
         constexpr int j0 = decltype(half)::value * HALF_J;
-        if constexpr (!SMALL) read_old(std::integral_constant<int, j0>{});
+        if constexpr (!T::EARLY) read_old(std::integral_constant<int, j0>{});
 #pragma unroll
         for (int i = 0; i < BI; ++i)
 #pragma unroll
@@ -590,6 +594,7 @@ __device__ __forceinline__ void product(const Args& a, int item, const int end, 
       for (int i = 0; i < BI; i += 2)
 #pragma unroll
         for (int part = 0; part < (LO ? 2 : 1); ++part) {
+          if (MODE == UPDATE && !SPLIT && part && !a.keep_lo) continue;
           const u32x2 x = packed(val[i][j], part), y = packed(val[i + 1][j], part);
           // blocks i and i + 1: after the swap a lane holds 8 consecutive rows of one of them,
           // and a store covers 64 consecutive bytes of 16 columns
@@ -811,7 +816,7 @@ struct Steps {
 // A matrix of up to 64 rows and SMALL_K columns: everything in one workgroup, a launch for the whole
 // stack.  What the separate launches of such a matrix take is mostly their starts (4 of 6 to 9 us
 // each, seventeen of them); one compute unit's matrix cores are enough for its products.
-using TileOne = Tile<2, 2, 2, 2, 9, 1>;
+using TileOne = Tile<2, 2, 2, 2, 9, 1, true>;
 using TileOneX = Tile<2, 2, 4, 2, 4, 1>;      // B X: fewer, wider tiles, one after the other
 constexpr int SMALL_ROWS = 64, SMALL_K = 256;
 
@@ -897,14 +902,14 @@ struct Plan {
 // tile's start and end come on top.  Measured per stage for one part and two (for 128 x 128 also by
 // whether a compute unit has one workgroup or two):
 //   64 x 64   0.24 / 0.30               + 6   nine stages in flight: few, small matrices
-//   128       0.65 / 0.90, 0.95 / 1.30  + 6
+//   128       0.55 / 0.78, 0.95 / 1.30  + 6   one: four stages in flight, two: two each
 //   256 x 128 0.82                      + 10
 // e.g. B X of 1024 x 1024: 9.5, 18 and 24 us; of 8 of them 42, 32 and 29; of 4096 x 4096 254, 137
 // and 125.  In two parts: 16 and 36 us; 95 and 57; 557 and 342.
 double product_us(int tile, bool split, double items, double stages) {
   if (tile == 64) return ceil(items / 256) * stages * (split ? 0.30 : 0.24) + 6;
   if (tile == 256) return ceil(items / 256) * stages * 0.82 + 10;
-  if (items <= 256) return stages * (split ? 0.90 : 0.65) + 6;
+  if (items <= 256) return stages * (split ? 0.78 : 0.55) + 6;
   return ceil(items / 512) * stages * (split ? 1.30 : 0.95) + 6;
 }
 
@@ -965,6 +970,7 @@ bool make_plan(int64_t batch, int64_t m, int64_t n, int32_t out_dtype, Plan* p) 
 
 using Tile64 = TileOne;
 using Tile128 = Tile<2, 2, 4, 4, 2, 2>;
+using Tile128One = Tile<2, 2, 4, 4, 4, 1, true>;   // a launch of at most one to a compute unit
 using Tile256 = Tile<2, 2, 8, 4, 3, 1>;
 
 template <int MODE, class T>
@@ -1001,6 +1007,8 @@ void launch(const Plan& p, Args a, hipStream_t s) {
     if (!tile || a.count <= 0) continue;
     if (tile == 256)
       launch_tile<MODE, Tile256>(p, a, s);
+    else if (tile == 128 && p.tile[i] == 128 && a.count <= 256)
+      launch_tile<MODE, Tile128One>(p, a, s);
     else if (tile == 128)
       launch_tile<MODE, Tile128>(p, a, s);
     else
@@ -1035,13 +1043,21 @@ void run(const Plan& p, const Steps& o, const Source& src, const Result& res, ui
     Args a = {};
     a.P = a.Q = X[i & 1], a.K = (int32_t)p.k_pad, a.C = A;
     launch<GRAM>(p, a, s);
-    const float sigma = p.split || i < o.n - 2 ? 0.0f : -(o.b + o.c) * (i == o.n - 1 ? 1.0f : 0.5f);
+    // One part: X = (a - sigma) X + (B + sigma I) hi is the same step, but for the rounding of hi,
+    // which the second term carries.  Directions whose singular value is still small are spoilt by
+    // it times sigma and every later step's growth, those near 1 by it times |b + c + sigma| or so:
+    // sigma is 0 as long as there is growth to come, and a in the last step, which then needs no
+    // lo at all.  (256 x 1024, equal singular values: 1.7e-3 with 0 throughout, 1.2e-3 so; eight
+    // strong directions over 1e-3: 3.5e-4, and 1.0e-3.)
+    const bool last = i == o.n - 1, before = i == o.n - 2;
+    const float sigma = p.split ? 0.0f : last ? o.a : before ? -0.5f * (o.b + o.c) : 0.0f;
     a.P = a.Q = A, a.K = (int32_t)p.r_pad;
     a.C = B, a.alpha = o.c, a.beta = o.b, a.shift = sigma;
     launch<SQUARE>(p, a, s);
     a.P = X[i & 1], a.Q = B, a.C = X[(i + 1) & 1], a.beta = o.a - sigma;
+    a.keep_lo = !before;
     a.res = res;
-    if (i == o.n - 1)
+    if (last)
       launch<RESULT>(p, a, s);
     else
       launch<UPDATE>(p, a, s);
