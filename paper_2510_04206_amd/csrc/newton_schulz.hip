@@ -891,26 +891,32 @@ constexpr int64_t MAX_SIDE = (int64_t)1 << 20, MAX_SHORT = (int64_t)1 << 16, MAX
 struct Plan {
   int64_t batch;
   int32_t r, k, tall, one;                  // one: ns_small_kernel's
-  int32_t tile[3], tail[3];                 // rows of a tile of A, B and X; of its last round, or 0
+  int32_t tile[3], tail[3];                 // of KINDS, for A, B and X; the last round's, or -1
   int64_t r_pad, k_pad;
   int32_t split, n_part;
   int64_t x_plane, a_plane;                 // elements
   size_t part, x[2], a, b, total;           // bytes
 };
 
-// What a launch of `items` tiles takes, in microseconds: a round of workgroups lasts its stages, a
-// tile's start and end come on top.  Measured per stage for one part and two (for 128 x 128 also by
-// whether a compute unit has one workgroup or two):
-//   64 x 64   0.24 / 0.30               + 6   nine stages in flight: few, small matrices
-//   128       0.55 / 0.78, 0.95 / 1.30  + 6   one: four stages in flight, two: two each
-//   256 x 128 0.82                      + 10
-// e.g. B X of 1024 x 1024: 9.5, 18 and 24 us; of 8 of them 42, 32 and 29; of 4096 x 4096 254, 137
-// and 125.  In two parts: 16 and 36 us; 95 and 57; 557 and 342.
-double product_us(int tile, bool split, double items, double stages) {
-  if (tile == 64) return ceil(items / 256) * stages * (split ? 0.30 : 0.24) + 6;
-  if (tile == 256) return ceil(items / 256) * stages * 0.82 + 10;
-  if (items <= 256) return stages * (split ? 0.78 : 0.55) + 6;
-  return ceil(items / 512) * stages * (split ? 1.30 : 0.95) + 6;
+// The tiles that a launch can take, and what one takes: a round of workgroups lasts its stages, a
+// tile's start and end come on top.  Microseconds a stage measured for one part and two.
+struct Kind {
+  int rows, cols, round;      // round: workgroups that the chip holds
+  double one, two, fixed;
+};
+constexpr int K64 = 0, K128 = 1, K128_PAIR = 2, K256 = 3;
+constexpr Kind KINDS[] = {
+    {64, 64, 256, 0.24, 0.30, 6.0},       // nine stages in flight: few, small matrices
+    {128, 128, 256, 0.62, 1.00, 6.0},     // four stages in flight, one workgroup a compute unit
+    {128, 128, 512, 0.95, 1.30, 6.0},     // two stages, two workgroups
+    {256, 128, 256, 0.82, 0.0, 10.0},     // (its two-part sums would not fit the registers)
+};
+// e.g. B X of 1024 x 1024: 9.5 us with the first, 18 and 24 us with the third and fourth; of 8 of
+// them 42, 32 and 29; of 2048 x 2048 36 us, 26 with the second, 33, 37; of 4096 x 4096 254, 137
+// (third), 125.  In two parts: of 1024 x 1024 16 us, third 36; of 8 of them 95, 57; of 4096 x 4096
+// 557, 342.
+double launch_us(const Kind& k, bool split, double items, double stages) {
+  return ceil(items / k.round) * stages * (split ? k.two : k.one) + k.fixed;
 }
 
 // Each product takes the tile that is done first; where its last round would leave most of the
@@ -919,17 +925,19 @@ double product_us(int tile, bool split, double items, double stages) {
 void choose_tiles(Plan* p) {
   for (int i = 0; i < 3; ++i) {
     double best = 0.0;
-    for (int t = 64; t <= (p->split ? 128 : 256); t *= 2) {
-      const double r = (double)cdiv(p->r, t), k = (double)cdiv(p->k, t);
-      const double items = p->batch * (i == 2 ? r * k : r * (r + 1) / 2) * (t == 256 ? 2 : 1);
-      const double stages = (i == 0 ? p->k : p->r) / (p->split ? 32.0 : 64.0);
-      const double whole = floor(items / (t == 128 ? 512 : 256)) * (t == 128 ? 512 : 256);
-      for (int tail = 0; tail < t; tail = tail ? 2 * tail : 64) {
-        if (tail && (whole == 0 || whole == items)) continue;
-        const double subs = (double)t / tail * (t == 256 ? 128 : t) / tail;
-        const double us = tail ? product_us(t, p->split, whole, stages) +
-                                     product_us(tail, p->split, (items - whole) * subs, stages)
-                               : product_us(t, p->split, items, stages);
+    const double stages = (i == 0 ? p->k : p->r) / (p->split ? 32.0 : 64.0);
+    for (int t = K64; t <= (p->split ? K128_PAIR : K256); ++t) {
+      const Kind& k = KINDS[t];
+      const double r = (double)cdiv(p->r, k.rows), x = (double)cdiv(p->k, k.rows);
+      const double items = p->batch * (i == 2 ? r * x : r * (r + 1) / 2) * (k.rows / k.cols);
+      const double whole = floor(items / k.round) * k.round;
+      for (int tail = -1; tail < t; ++tail) {
+        if (tail >= 0 && (whole == 0 || whole == items || KINDS[tail].rows == k.rows)) continue;
+        double us = launch_us(k, p->split, tail < 0 ? items : whole, stages);
+        if (tail >= 0)
+          us += launch_us(KINDS[tail], p->split,
+                          (items - whole) * (k.rows / KINDS[tail].rows) * (k.cols / KINDS[tail].cols),
+                          stages);
         if (best == 0.0 || us < best) best = us, p->tile[i] = t, p->tail[i] = tail;
       }
     }
@@ -946,7 +954,7 @@ bool make_plan(int64_t batch, int64_t m, int64_t n, int32_t out_dtype, Plan* p) 
   choose_tiles(p);
   p->one = p->r <= SMALL_ROWS && p->k <= SMALL_K;
   int64_t pad = 128;
-  for (int i = 0; i < 3; ++i) pad = p->tile[i] > pad ? p->tile[i] : pad;
+  for (int i = 0; i < 3; ++i) pad = KINDS[p->tile[i]].rows > pad ? KINDS[p->tile[i]].rows : pad;
   p->r_pad = p->one ? 64 : cdiv(r, pad) * pad;
   p->k_pad = cdiv(k, pad) * pad;
   const int64_t per = cdiv(m * cdiv(n, (int64_t)8), (int64_t)NORM_THREADS);
@@ -969,8 +977,8 @@ bool make_plan(int64_t batch, int64_t m, int64_t n, int32_t out_dtype, Plan* p) 
 }
 
 using Tile64 = TileOne;
-using Tile128 = Tile<2, 2, 4, 4, 2, 2>;
-using Tile128One = Tile<2, 2, 4, 4, 4, 1, true>;   // a launch of at most one to a compute unit
+using Tile128 = Tile<2, 2, 4, 4, 4, 1, true>;
+using Tile128Pair = Tile<2, 2, 4, 4, 2, 2>;
 using Tile256 = Tile<2, 2, 8, 4, 3, 1>;
 
 template <int MODE, class T>
@@ -993,23 +1001,24 @@ template <int MODE>
 void launch(const Plan& p, Args a, hipStream_t s) {
   constexpr bool TR = MODE == UPDATE || MODE == RESULT;
   const int i = MODE == GRAM ? 0 : MODE == SQUARE ? 1 : 2;
-  a.unit_m = p.tile[i], a.unit_n = p.tile[i] == 256 ? 128 : p.tile[i];
+  const Kind& k = KINDS[p.tile[i]];
+  a.unit_m = k.rows, a.unit_n = k.cols;
   a.units_m = (int32_t)((TR ? p.k_pad : p.r_pad) / a.unit_m);
   a.units_n = (int32_t)(p.r_pad / a.unit_n);
-  a.halves_log = p.tile[i] == 256;
+  a.halves_log = k.rows == 2 * k.cols;
   a.units = TR ? a.units_m * a.units_n : a.units_m * (a.units_m + 1) / 2 * (a.unit_m / a.unit_n);
   const int32_t all = (int32_t)(a.units * p.batch);
-  const int32_t round = p.tile[i] == 128 ? 512 : 256;
+  const int32_t whole = p.tail[i] < 0 ? all : all / k.round * k.round;
   for (int part = 0; part < 2; ++part) {
+    a.first = part ? whole : 0;
+    a.count = part ? all - whole : whole;
+    if (a.count <= 0) continue;
     const int tile = part ? p.tail[i] : p.tile[i];
-    a.first = part ? all / round * round : 0;
-    a.count = (p.tail[i] && !part ? all / round * round : all) - a.first;
-    if (!tile || a.count <= 0) continue;
-    if (tile == 256)
+    if (tile == K256)
       launch_tile<MODE, Tile256>(p, a, s);
-    else if (tile == 128 && p.tile[i] == 128 && a.count <= 256)
-      launch_tile<MODE, Tile128One>(p, a, s);
-    else if (tile == 128)
+    else if (tile == K128_PAIR)
+      launch_tile<MODE, Tile128Pair>(p, a, s);
+    else if (tile == K128)
       launch_tile<MODE, Tile128>(p, a, s);
     else
       launch_tile<MODE, Tile64>(p, a, s);
