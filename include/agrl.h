@@ -18,7 +18,14 @@
  *                          token-level normalisation);
  *   agrl_policy_loss_bwd   dH and dW of that loss, recomputing the logits;
  *   agrl_sequence_mean_weights  per-token weights that turn the loss into the
- *                          sequence-level mean of App. B.2's GRPO objective.
+ *                          sequence-level mean of App. B.2's GRPO objective;
+ *
+ * and what stands on both sides of it in a training step:
+ *
+ *   agrl_token_norm_fwd    layer or RMS norm of the token rows that become H;
+ *   agrl_token_norm_bwd    its gradient, from the loss's dH;
+ *   agrl_orthogonalize     Newton-Schulz orthogonalisation of matrices;
+ *   agrl_muon_step         the optimiser step of weight matrices with it.
  *
  * Conventions for every entry point:
  *   - Array arguments are DEVICE pointers owned by the caller; the library
@@ -27,7 +34,8 @@
  *   - Calls only enqueue work on `stream` and return; they never synchronise.
  *     Argument errors are reported synchronously, before anything is
  *     launched, and leave every output untouched.
- *   - Row-major, contiguous.  H is [T, d]; W is [V, d] (the nn.Linear weight
+ *   - Row-major, contiguous (where a call has row and matrix strides in its
+ *     arguments: rows of consecutive elements).  H is [T, d]; W is [V, d] (the nn.Linear weight
  *     layout, logits = H W^T).  Row n of H is the hidden state that predicts
  *     token_id[n]; the caller shifts labels, the library never does.
  *   - Tokens with action_mask == 0 (environment observations, padding) are

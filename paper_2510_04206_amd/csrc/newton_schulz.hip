@@ -3,6 +3,24 @@
 //   X = G / (|G|_F + eps);  `steps` times: A = X X^T, B = b A + c A A, X = a X + B X
 //
 // on the side with fewer rows (r = min(m, n) rows of k = max(m, n); G^T for m > n).
+//
+// Matrix cores bound it.  A and A A are symmetric, so half of their tiles are formed and written
+// twice: 3 r^2 k + r^3 operations a step instead of 4 r^2 k + 2 r^3.  One workgroup per tile,
+// persistent, the K extent in stages of 128 bytes a row that the LDS copies keep in flight; which
+// tile and how many stages is chosen per product by the time it is expected to take (choose_tiles).
+// B X reads X transposed out of LDS, so X lies in memory once, and every product writes its result
+// as the next one's operand.  A step is three launches; two before the first make |G| and X.
+//
+// Measured (MI355X, five steps): 5120 x 5120 fp32 -> bf16 2.7 ms, 0.99 PFLOP/s of the operations
+// above (a 16384^3 library product in fp16 reaches 1.41); 14336 x 3584 with momentum and a bf16
+// weight 3.2 ms, 0.94; 8 x 1024 x 1024 fp32 -> fp32 0.77 ms, 0.67 PFLOP/s of fp16 products; 128 x
+// 512 114 us and 256 x 256 fp32 124 us, of which 17 launches' own 4 us each are two thirds.
+// What is left: in the large ones the compute units reach a tile's end together and move 256 KiB
+// each there (B X of 14336 x 3584: 13 to 17 of 60 us a tile), and the last round of tiles is not full
+// (A of 5120 x 5120: 420 tiles for 256 units); inside a tile the loop runs at 0.7 to 0.8 us per 256
+// x 128 stage of 64, 0.65 of what the units' clock (2.0 to 2.1 GHz under load) allows.  In two
+// parts the matrix cores are busy 40 to 55% of the time: a wave has 64 additions and 16 KiB of LDS
+// reads beside each 48 matrix instructions.
 #include <math.h>
 #include <stdio.h>
 
@@ -99,8 +117,8 @@ struct Tile {
   static constexpr bool EARLY = EARLY_;          // the epilogue's inputs are read ahead of the products
   static constexpr int WM = WM_, WN = WN_, BI = BI_, BJ = BJ_, NST = NST_;
   static constexpr int PER_CU = PER_CU_;         // workgroups of a compute unit
-  // registers: 256 per lane hold all of a tile up to 128 x 128, and no accumulator then moves
-  // between the two register files
+  // waves of a SIMD: with two, a lane has 256 registers, which hold a tile of 128 x 128 without a
+  // move between the two register files
   static constexpr int EU_WAVES = BI_ * BJ_ <= 4 || PER_CU_ > 1 ? 2 : 1;
   static constexpr int BM = WM * BI * 16, BN = WN * BJ * 16, WAVES = WM * WN;
   static constexpr int P_BYTES = BM * 128, STAGE = (BM + BN) * 128;
@@ -459,7 +477,7 @@ __device__ __forceinline__ void product(const Args& a, int item, const int end, 
         const f32x4 zero = {0.0f, 0.0f, 0.0f, 0.0f};
         terms[b % 3] = __builtin_amdgcn_mfma_f32_16x16x32_f16(
             fp[P][i][kp], fq[P][j][kq], term ? terms[b % 3] : zero, 0, 0, 0);
-        if constexpr (term < 2 && b > 1) 
+        if constexpr (term < 2 && b > 1)
           add(std::integral_constant<int, b - 2>{}, std::integral_constant<int, term>{});
       } else {
         acc[i][j] =
@@ -815,7 +833,8 @@ struct Steps {
 
 // A matrix of up to 64 rows and SMALL_K columns: everything in one workgroup, a launch for the whole
 // stack.  What the separate launches of such a matrix take is mostly their starts (4 of 6 to 9 us
-// each, seventeen of them); one compute unit's matrix cores are enough for its products.
+// each, seventeen of them); one compute unit's matrix cores are enough for its products: 64 x 64 57
+// us, in separate launches 110; 64 x 256 84, 105.
 using TileOne = Tile<2, 2, 2, 2, 9, 1, true>;
 using TileOneX = Tile<2, 2, 4, 2, 4, 1>;      // B X: fewer, wider tiles, one after the other
 constexpr int SMALL_ROWS = 64, SMALL_K = 256;
