@@ -11,16 +11,16 @@
 // B X reads X transposed out of LDS, so X lies in memory once, and every product writes its result
 // as the next one's operand.  A step is three launches; two before the first make |G| and X.
 //
-// Measured (MI355X, five steps): 5120 x 5120 fp32 -> bf16 2.7 ms, 0.99 PFLOP/s of the operations
-// above (a 16384^3 library product in fp16 reaches 1.41); 14336 x 3584 with momentum and a bf16
-// weight 3.2 ms, 0.94; 8 x 1024 x 1024 fp32 -> fp32 0.77 ms, 0.67 PFLOP/s of fp16 products; 128 x
-// 512 114 us and 256 x 256 fp32 124 us, of which 17 launches' own 4 us each are two thirds.
-// What is left: in the large ones the compute units reach a tile's end together and move 256 KiB
-// each there (B X of 14336 x 3584: 13 to 17 of 60 us a tile), and the last round of tiles is not full
-// (A of 5120 x 5120: 420 tiles for 256 units); inside a tile the loop runs at 0.7 to 0.8 us per 256
-// x 128 stage of 64, 0.65 of what the units' clock (2.0 to 2.1 GHz under load) allows.  In two
-// parts the matrix cores are busy 40 to 55% of the time: a wave has 64 additions and 16 KiB of LDS
-// reads beside each 48 matrix instructions.
+// Measured (MI355X, five steps): 5120 x 5120 fp32 -> bf16 2.5 ms, 1.06 PFLOP/s of the operations
+// above (a 16384^3 library product in fp16 reaches 1.41), 8192 x 8192 8.6 ms, 1.28; 14336 x 3584 with
+// momentum and a bf16 weight 3.0 ms, 0.99; 8 x 1024 x 1024 fp32 -> fp32 0.76 ms, 0.68 PFLOP/s of
+// fp16 products; 128 x 512 114 us and 256 x 256 fp32 124 us, of which 17 launches' own 4 us each are
+// two thirds.
+// What is left: the last round of tiles is not full (B X of 5120 x 5120: 400 tiles of 256 x 256 for
+// 256 units), at a tile's end all compute units move 512 KiB at once (20 of 140 us a tile there),
+// and a 256 x 256 stage of 64 takes 1.4 us where the matrix cores alone would take 1.0 at the clock
+// that the power limit leaves (2.0 to 2.1 GHz).  In two parts the matrix cores are busy 40 to 55% of
+// the time: a wave has 64 additions and 16 KiB of LDS reads beside each 48 matrix instructions.
 #include <math.h>
 #include <stdio.h>
 
@@ -121,6 +121,8 @@ struct Tile {
   // move between the two register files
   static constexpr int EU_WAVES = BI_ * BJ_ <= 4 || PER_CU_ > 1 ? 2 : 1;
   static constexpr int BM = WM * BI * 16, BN = WN * BJ * 16, WAVES = WM * WN;
+  // a register set of fragments holds a stage, or, for the largest tile, half of one
+  static constexpr bool HALVES = BI_ * BJ_ > 32;
   static constexpr int P_BYTES = BM * 128, STAGE = (BM + BN) * 128;
   static constexpr int CP = BM / 8 / WAVES, CQ = BN / 8 / WAVES;   // 1 KiB copies of a wave
 };
@@ -425,7 +427,8 @@ __device__ __forceinline__ void product(const Args& a, int item, const int end, 
   }
 
   // slice kk: the stage's k half, or its part
-  f16x8 fp[2][BI][2], fq[2][BJ][2];
+  constexpr int KK = T::HALVES ? 1 : 2;
+  f16x8 fp[2][BI][KK], fq[2][BJ][KK];
   auto read_p = [&](const uint8_t* st, int i, int kk) {
     if constexpr (TR) {
       const uint8_t* at = st + ta[i][SPLIT ? kk : 0] + (SPLIT ? 0 : kk * 32 * TROW);
@@ -507,8 +510,49 @@ __device__ __forceinline__ void product(const Args& a, int item, const int end, 
     if constexpr (COPY) advance();
     buf = next;
   };
+  // The largest tile: set h holds the stage's k half h, and the next half is read under a half's
+  // products.  The barrier stands between the halves.  The copies are spread over the second half:
+  // all at its start, they took LDS from the reads (8192 x 8192: 427 us for A, so 400).  Its sums
+  // fill the accumulation registers to the last, so the products are written with both sides tied
+  // (left to the allocator, half of the sums moved to and fro between the register files); what
+  // reads the sums behind the loop waits in pin().
+  auto half_stage = [&](auto half_c) {
+    constexpr int H = decltype(half_c)::value, PER = BI + BJ, N = BI * BJ;
+    static_assert(!T::HALVES || 4 * COPIES == N, "a copy at every fourth product of half a stage");
+    const int next = buf ^ 1;
+    if constexpr (H == 1) {
+      bf16k::wait_vmcnt<0>();
+      lds_barrier();
+      __builtin_amdgcn_sched_barrier(0);
+    }
+    const uint8_t* st = smem + (H == 1 ? next : buf) * T::STAGE;
+    const uint32_t into = lds0 + buf * T::STAGE;
+    static_for<N>([&](auto q_c) {
+      constexpr int q = decltype(q_c)::value, i = q / BJ, j = q % BJ;
+      asm volatile("v_mfma_f32_16x16x32_f16 %0, %1, %2, %0"
+                   : "+a"(acc[i][j])
+                   : "v"(fp[H][i][0]), "v"(fq[H][j][0]));
+      constexpr int r0 = reads_before(q, PER, N), r1 = reads_before(q + 1, PER, N);
+      static_for<r1 - r0>([&](auto n_c) {
+        constexpr int x = r0 + decltype(n_c)::value;
+        if constexpr (x < BJ)
+          fq[H ^ 1][x][0] = read_q(st, x, H ^ 1);
+        else
+          fp[H ^ 1][x - BJ][0] = read_p(st, x - BJ, H ^ 1);
+      });
+      if constexpr (H == 1 && q % 4 == 3) copy(into, std::integral_constant<int, q / 4>{});
+      __builtin_amdgcn_sched_barrier(0);
+    });
+    if constexpr (H == 1) {
+      advance();
+      buf = next;
+    }
+  };
   auto stage = [&](auto par_c) {
-    if (!SMALL || left > 0)
+    if constexpr (T::HALVES) {
+      half_stage(std::integral_constant<int, 0>{});
+      half_stage(std::integral_constant<int, 1>{});
+    } else if (!SMALL || left > 0)
       stage_with(par_c, std::true_type{});
     else if constexpr (SMALL)
       stage_with(par_c, std::false_type{});
@@ -523,7 +567,7 @@ __device__ __forceinline__ void product(const Args& a, int item, const int end, 
     bf16k::wait_vmcnt<0>();
   lds_barrier();
 #pragma unroll
-  for (int kk = 0; kk < 2; ++kk) {
+  for (int kk = 0; kk < KK; ++kk) {
 #pragma unroll
     for (int j = 0; j < BJ; ++j) fq[0][j][kk] = read_q(smem, j, kk);
 #pragma unroll
@@ -537,6 +581,8 @@ __device__ __forceinline__ void product(const Args& a, int item, const int end, 
     // (the wide tile's sums live in the accumulation registers on both sides of the loop:
     // otherwise the allocator moves them to and fro inside it)
     auto pin = [&]() {
+      // (a product written in assembly: no reader of its sum may follow within 18 cycles)
+      if constexpr (T::HALVES) asm volatile("s_nop 15\n\ts_nop 15" ::: "memory");
       if constexpr (T::EU_WAVES == 1 && !SPLIT)
 #pragma unroll
         for (int i = 0; i < BI; ++i)
@@ -548,95 +594,106 @@ __device__ __forceinline__ void product(const Args& a, int item, const int end, 
     // block (i, j) of a lane: column c = 16 j + (lane & 15), rows r .. r + 3, r = 16 i + 4 g
     const int r0 = at.m0 + wm * BI * 16 + 4 * g, c0 = at.n0 + wn * BJ * 16 + fr;
     // What the epilogue adds to: a small tile reads it ahead of its products (a launch of few of
-    // them is latency), a larger one half a tile at a time behind them.
+    // them is latency), a larger one half a tile at a time behind them, and the largest goes
+    // through its epilogue by quarters, the next one's read ahead of the stores.
     constexpr bool OLD = MODE == SQUARE || MODE == UPDATE || (MODE == RESULT && SPLIT);
     constexpr bool LO = SPLIT || TR, OLD_LO = OLD && LO;
-    constexpr int HALF_J = T::EARLY ? BJ : BJ / 2;
-    f16x4 oh[OLD ? BI : 1][HALF_J], ol[OLD_LO ? BI : 1][HALF_J];
+    constexpr int VAL_J = T::HALVES ? 1 : BJ;
+    constexpr int OLD_J = T::EARLY ? BJ : T::HALVES ? VAL_J : BJ / 2, SETS = T::HALVES ? 2 : 1;
+    f16x4 oh[SETS][OLD ? BI : 1][OLD_J], ol[SETS][OLD_LO ? BI : 1][OLD_J];
     auto read_old = [&](auto j_c) {
-      constexpr int j0 = decltype(j_c)::value;
+      constexpr int j0 = decltype(j_c)::value, set = j0 / OLD_J % SETS;
       const _Float16* const old = a.P.at + at.z * a.P.matrix;
 #pragma unroll
       for (int i = 0; i < BI; ++i)
 #pragma unroll
-        for (int j = 0; j < HALF_J; ++j) {
+        for (int j = 0; j < OLD_J; ++j) {
           const _Float16* p = old + place<SPLIT>(a.P.ld, c0 + 16 * (j0 + j), r0 + 16 * i);
-          oh[i][j] = *(const f16x4*)p;
-          if constexpr (OLD_LO) ol[i][j] = *(const f16x4*)(p + lo_at<SPLIT>(a.P));
+          oh[set][i][j] = *(const f16x4*)p;
+          if constexpr (OLD_LO) ol[set][i][j] = *(const f16x4*)(p + lo_at<SPLIT>(a.P));
         }
     };
     if constexpr (OLD && T::EARLY) read_old(std::integral_constant<int, 0>{});
+    if constexpr (T::HALVES) asm volatile("s_nop 7" ::: "memory");
     for (int s = 0; s < total; s += 2) {
       stage(std::integral_constant<int, 0>{});
       stage(std::integral_constant<int, 1>{});
     }
     pin();
-    f32x4 val[BI][BJ];
-    if constexpr (OLD) {
-      static_for<BJ / HALF_J>([&](auto half) {
-        constexpr int j0 = decltype(half)::value * HALF_J;
-        if constexpr (!T::EARLY) read_old(std::integral_constant<int, j0>{});
+    if constexpr (OLD && T::HALVES) read_old(std::integral_constant<int, 0>{});
+    static_for<BJ / VAL_J>([&](auto part_c) {
+      constexpr int v0 = decltype(part_c)::value * VAL_J;
+      const int cv = c0 + 16 * v0;
+      f32x4 val[BI][VAL_J];
+      if constexpr (OLD) {
+        static_for<VAL_J / OLD_J>([&](auto half) {
+          constexpr int h0 = decltype(half)::value * OLD_J, j0 = v0 + h0, set = j0 / OLD_J % SETS;
+          if constexpr (!T::EARLY && !T::HALVES) read_old(std::integral_constant<int, j0>{});
+#pragma unroll
+          for (int i = 0; i < BI; ++i)
+#pragma unroll
+            for (int j = 0; j < OLD_J; ++j)
+#pragma unroll
+              for (int q = 0; q < 4; ++q) {
+                const float o = (float)oh[set][i][j][q] +
+                                (OLD_LO ? (float)ol[set][OLD_LO ? i : 0][j][q] : 0.0f);
+                float v = acc[i][j0 + j][q] * (1.0f / S);
+                v = MODE == SQUARE ? fmaf(a.alpha, v, a.beta * o) : fmaf(a.beta, o, v);
+                if (MODE == SQUARE && r0 + 16 * i + q == c0 + 16 * (j0 + j)) v += a.shift * S;
+                val[i][h0 + j][q] = v;
+              }
+        });
+        if constexpr (T::HALVES && v0 + VAL_J < BJ)
+          read_old(std::integral_constant<int, v0 + VAL_J>{});
+      } else {
 #pragma unroll
         for (int i = 0; i < BI; ++i)
 #pragma unroll
-          for (int j = 0; j < HALF_J; ++j)
+          for (int j = 0; j < VAL_J; ++j) val[i][j] = acc[i][v0 + j] * (1.0f / S);
+      }
+      if constexpr (MODE == RESULT) {
+        const int end_m = a.res.tall ? a.res.rows : a.res.cols;
+        const int end_n = a.res.tall ? a.res.cols : a.res.rows;
+        if (at.m0 + BM <= end_m && at.n0 + BN <= end_n)
+          write_result<SPLIT, true>(a.res, val, at.z, r0, cv, lane);
+        else if (at.m0 < end_m && at.n0 < end_n)
+          write_result<SPLIT, false>(a.res, val, at.z, r0, cv, lane);
+      } else {
+        _Float16* const out = a.C.at + at.z * a.C.matrix;
 #pragma unroll
-            for (int q = 0; q < 4; ++q) {
-              const float o =
-                  (float)oh[i][j][q] + (OLD_LO ? (float)ol[OLD_LO ? i : 0][j][q] : 0.0f);
-              float v = acc[i][j0 + j][q] * (1.0f / S);
-              v = MODE == SQUARE ? fmaf(a.alpha, v, a.beta * o) : fmaf(a.beta, o, v);
-              if (MODE == SQUARE && r0 + 16 * i + q == c0 + 16 * (j0 + j)) v += a.shift * S;
-              val[i][j0 + j][q] = v;
-            }
-      });
-    } else {
+        for (int j = 0; j < VAL_J; ++j)
 #pragma unroll
-      for (int i = 0; i < BI; ++i)
-#pragma unroll
-        for (int j = 0; j < BJ; ++j) val[i][j] = acc[i][j] * (1.0f / S);
-    }
-    if constexpr (MODE == RESULT) {
-      const int end_m = a.res.tall ? a.res.rows : a.res.cols;
-      const int end_n = a.res.tall ? a.res.cols : a.res.rows;
-      if (at.m0 + BM <= end_m && at.n0 + BN <= end_n)
-        write_result<SPLIT, true>(a.res, val, at.z, r0, c0, lane);
-      else if (at.m0 < end_m && at.n0 < end_n)
-        write_result<SPLIT, false>(a.res, val, at.z, r0, c0, lane);
-      continue;
-    }
-    _Float16* const out = a.C.at + at.z * a.C.matrix;
-#pragma unroll
-    for (int j = 0; j < BJ; ++j)
-#pragma unroll
-      for (int i = 0; i < BI; i += 2)
-#pragma unroll
-        for (int part = 0; part < (LO ? 2 : 1); ++part) {
-          if (MODE == UPDATE && !SPLIT && part && !a.keep_lo) continue;
-          const u32x2 x = packed(val[i][j], part), y = packed(val[i + 1][j], part);
-          // blocks i and i + 1: after the swap a lane holds 8 consecutive rows of one of them,
-          // and a store covers 64 consecutive bytes of 16 columns
-          _Float16* p = out + part * lo_at<SPLIT>(a.C) +
-                        place<SPLIT>(a.C.ld, c0 + 16 * j,
-                                     r0 - 4 * g + 16 * (i + (g & 1)) + 8 * (g >> 1));
-          const auto s0 = __builtin_amdgcn_permlane16_swap(x[0], y[0], false, false);
-          const auto s1 = __builtin_amdgcn_permlane16_swap(x[1], y[1], false, false);
-          *(u32x4*)p = u32x4{s0[0], s1[0], s0[1], s1[1]};
-        }
-    if constexpr (!TR) {
-      if (at.below) {                                // (a diagonal square is written whole)
-#pragma unroll
-        for (int i = 0; i < BI; ++i)
-#pragma unroll
-          for (int j = 0; j < BJ; ++j)
+          for (int i = 0; i < BI; i += 2)
 #pragma unroll
             for (int part = 0; part < (LO ? 2 : 1); ++part) {
+              if (MODE == UPDATE && !SPLIT && part && !a.keep_lo) continue;
+              const u32x2 x = packed(val[i][j], part), y = packed(val[i + 1][j], part);
+              // blocks i and i + 1: after the swap a lane holds 8 consecutive rows of one of them,
+              // and a store covers 64 consecutive bytes of 16 columns
               _Float16* p = out + part * lo_at<SPLIT>(a.C) +
-                            place<SPLIT>(a.C.ld, r0 + 16 * i + (lane & 3), c0 + 16 * j - (lane & 3));
-              *(u32x2*)p = quad_transpose(packed(val[i][j], part), lane);
+                            place<SPLIT>(a.C.ld, cv + 16 * j,
+                                         r0 - 4 * g + 16 * (i + (g & 1)) + 8 * (g >> 1));
+              const auto s0 = __builtin_amdgcn_permlane16_swap(x[0], y[0], false, false);
+              const auto s1 = __builtin_amdgcn_permlane16_swap(x[1], y[1], false, false);
+              *(u32x4*)p = u32x4{s0[0], s1[0], s0[1], s1[1]};
             }
+        if constexpr (!TR) {
+          if (at.below) {                            // (a diagonal square is written whole)
+#pragma unroll
+            for (int i = 0; i < BI; ++i)
+#pragma unroll
+              for (int j = 0; j < VAL_J; ++j)
+#pragma unroll
+                for (int part = 0; part < (LO ? 2 : 1); ++part) {
+                  _Float16* p =
+                      out + part * lo_at<SPLIT>(a.C) +
+                      place<SPLIT>(a.C.ld, r0 + 16 * i + (lane & 3), cv + 16 * j - (lane & 3));
+                  *(u32x2*)p = quad_transpose(packed(val[i][j], part), lane);
+                }
+          }
+        }
       }
-    }
+    });
   }
   // no copy outlives the workgroup's LDS, and what was written can be read behind a barrier
   asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
@@ -906,59 +963,93 @@ __global__ void __launch_bounds__(64 * TileOne::WAVES)
 // ---------------------------------------------------------------------------
 constexpr int64_t MAX_SIDE = (int64_t)1 << 20, MAX_SHORT = (int64_t)1 << 16, MAX_BATCH = 65535;
 
+// A launch of a product: `units` of the product's numbering (see Args) by tile `tile`.
+struct Part {
+  int32_t tile, units;
+};
+constexpr int PARTS = 3;
+
 // Sizes and the workspace of a stack of matrices
 struct Plan {
   int64_t batch;
   int32_t r, k, tall, one;                  // one: ns_small_kernel's
-  int32_t tile[3], tail[3];                 // of KINDS, for A, B and X; the last round's, or -1
+  Part part_of[3][PARTS];                   // of A, B and X; the first one's tile is the unit
   int64_t r_pad, k_pad;
   int32_t split, n_part;
   int64_t x_plane, a_plane;                 // elements
   size_t part, x[2], a, b, total;           // bytes
 };
 
-// The tiles that a launch can take, and what one takes: a round of workgroups lasts its stages, a
-// tile's start and end come on top.  Microseconds a stage measured for one part and two.
+// The tiles that a launch can take, and the time of one, in microseconds: a round of workgroups
+// lasts its stages and its end, a launch's start comes on top.  Fitted to launches that were
+// measured; in two parts a last round that fills part of the chip runs faster (the compute units
+// in it share less power and bandwidth), which the wide tiles' own figures hold already.
 struct Kind {
   int rows, cols, round;      // round: workgroups that the chip holds
-  double one, two, fixed;
+  double one, two, start;     // a stage of one part, of two; a launch
+  double end[2];              // a round's end in A and A A, and in B X
+  double part;                // what of a round's time is left as its share of the chip goes to 0
 };
-constexpr int K64 = 0, K128 = 1, K128_PAIR = 2, K256 = 3;
+constexpr int K64 = 0, K128 = 1, K128_PAIR = 2, K256 = 3, K256_SQUARE = 4;
 constexpr Kind KINDS[] = {
-    {64, 64, 256, 0.24, 0.30, 6.0},       // nine stages in flight: few, small matrices
-    {128, 128, 256, 0.62, 1.00, 6.0},     // four stages in flight, one workgroup a compute unit
-    {128, 128, 512, 0.95, 1.30, 6.0},     // two stages, two workgroups
-    {256, 128, 256, 0.82, 0.0, 10.0},     // (its two-part sums would not fit the registers)
+    {64, 64, 256, 0.24, 0.30, 6.0, {0.0, 0.0}, 1.0},      // nine stages in flight: few, small matrices
+    {128, 128, 256, 0.62, 1.00, 6.0, {0.0, 0.0}, 0.7},    // four, one workgroup a compute unit
+    {128, 128, 512, 0.95, 1.30, 6.0, {0.0, 0.0}, 1.0},    // two, two workgroups
+    {256, 128, 256, 0.79, 0.0, 6.0, {3.0, 14.0}, 1.0},    // (the sums of two parts would not fit
+    {256, 256, 256, 1.20, 0.0, 4.0, {18.0, 10.0}, 1.0},   // the registers of these two)
 };
 // e.g. B X of 1024 x 1024: 9.5 us with the first, 18 and 24 us with the third and fourth; of 8 of
 // them 42, 32 and 29; of 2048 x 2048 36 us, 26 with the second, 33, 37; of 4096 x 4096 254, 137
-// (third), 125.  In two parts: of 1024 x 1024 16 us, third 36; of 8 of them 95, 57; of 4096 x 4096
-// 557, 342.
-double launch_us(const Kind& k, bool split, double items, double stages) {
-  return ceil(items / k.round) * stages * (split ? k.two : k.one) + k.fixed;
+// (third), 125 to 135 and, with the fifth, 114.  In two parts: of 1024 x 1024 16 us, third 36; of
+// 8 of them 95, 57; of 4096 x 4096 557, 342; five steps of 2048 x 2048 900 us with the third, 797
+// with the second where it fits.
+double launch_us(const Kind& k, bool split, bool update, int64_t items, double stages) {
+  const int64_t whole = items / k.round, rest = items % k.round;
+  const double part = split ? k.part : 1.0;
+  const double rounds = whole + (rest ? part + (1.0 - part) * rest / k.round : 0.0);
+  return rounds * (stages * (split ? k.two : k.one) + k.end[update]) + k.start;
 }
 
 // Each product takes the tile that is done first; where its last round would leave most of the
-// chip idle, that round's tiles go to a launch of smaller ones (B X of 5120 x 5120: 800 tiles of
-// 256 x 128 are three rounds of 256 and 32 tiles more).
+// chip idle, that round's units go to a launch of smaller tiles, and so on (B X of 14336 x 3584: 784
+// tiles of 256 x 256 are three rounds of 256 and 16 units more, which go by 64 x 64).  The time of
+// `units` of unit kind `of` by tile t and smaller ones; out: the launches, `left` of them at most.
+double plan_parts(bool split, bool update, double stages, int of, int t, int64_t units, int left,
+                  Part* out) {
+  const Kind& k = KINDS[t];
+  const int64_t per = (int64_t)(KINDS[of].rows / k.rows) * (KINDS[of].cols / k.cols);
+  double best = launch_us(k, split, update, units * per, stages);
+  out[0] = Part{t, (int32_t)units};
+  if (left > 1) out[1].units = 0;
+  const int64_t whole = units * per / k.round * k.round / per;
+  if (left == 1 || whole == 0 || whole == units) return best;
+  const double first = launch_us(k, split, update, whole * per, stages);
+  for (int next = K64; next < t; ++next) {
+    if (KINDS[next].rows * KINDS[next].cols >= k.rows * k.cols) continue;
+    Part rest[PARTS] = {};
+    const double us =
+        first + plan_parts(split, update, stages, of, next, units - whole, left - 1, rest);
+    if (us >= best) continue;
+    best = us;
+    out[0].units = (int32_t)whole;
+    for (int i = 1; i < left; ++i) out[i] = rest[i - 1];
+  }
+  return best;
+}
+
 void choose_tiles(Plan* p) {
   for (int i = 0; i < 3; ++i) {
     double best = 0.0;
     const double stages = (i == 0 ? p->k : p->r) / (p->split ? 32.0 : 64.0);
-    for (int t = K64; t <= (p->split ? K128_PAIR : K256); ++t) {
+    for (int t = K64; t <= (p->split ? K128_PAIR : K256_SQUARE); ++t) {
       const Kind& k = KINDS[t];
-      const double r = (double)cdiv(p->r, k.rows), x = (double)cdiv(p->k, k.rows);
-      const double items = p->batch * (i == 2 ? r * x : r * (r + 1) / 2) * (k.rows / k.cols);
-      const double whole = floor(items / k.round) * k.round;
-      for (int tail = -1; tail < t; ++tail) {
-        if (tail >= 0 && (whole == 0 || whole == items || KINDS[tail].rows == k.rows)) continue;
-        double us = launch_us(k, p->split, tail < 0 ? items : whole, stages);
-        if (tail >= 0)
-          us += launch_us(KINDS[tail], p->split,
-                          (items - whole) * (k.rows / KINDS[tail].rows) * (k.cols / KINDS[tail].cols),
-                          stages);
-        if (best == 0.0 || us < best) best = us, p->tile[i] = t, p->tail[i] = tail;
-      }
+      const int64_t r = cdiv(p->r, k.rows), x = cdiv(p->k, k.rows);
+      const int64_t units = p->batch * (i == 2 ? r * x : r * (r + 1) / 2) * (k.rows / k.cols);
+      Part parts[PARTS] = {};
+      const double us = plan_parts(p->split, i == 2, stages, t, t, units, PARTS, parts);
+      if (t > K64 && us >= best) continue;
+      best = us;
+      for (int j = 0; j < PARTS; ++j) p->part_of[i][j] = parts[j];
     }
   }
 }
@@ -973,7 +1064,8 @@ bool make_plan(int64_t batch, int64_t m, int64_t n, int32_t out_dtype, Plan* p) 
   choose_tiles(p);
   p->one = p->r <= SMALL_ROWS && p->k <= SMALL_K;
   int64_t pad = 128;
-  for (int i = 0; i < 3; ++i) pad = KINDS[p->tile[i]].rows > pad ? KINDS[p->tile[i]].rows : pad;
+  for (const auto& parts : p->part_of)
+    if (KINDS[parts[0].tile].rows > pad) pad = KINDS[parts[0].tile].rows;
   p->r_pad = p->one ? 64 : cdiv(r, pad) * pad;
   p->k_pad = cdiv(k, pad) * pad;
   const int64_t per = cdiv(m * cdiv(n, (int64_t)8), (int64_t)NORM_THREADS);
@@ -999,6 +1091,7 @@ using Tile64 = TileOne;
 using Tile128 = Tile<2, 2, 4, 4, 4, 1, true>;
 using Tile128Pair = Tile<2, 2, 4, 4, 2, 2>;
 using Tile256 = Tile<2, 2, 8, 4, 3, 1>;
+using Tile256Square = Tile<2, 2, 8, 8, 2, 1>;
 
 template <int MODE, class T>
 void launch_tile(const Plan& p, Args a, hipStream_t s) {
@@ -1020,20 +1113,22 @@ template <int MODE>
 void launch(const Plan& p, Args a, hipStream_t s) {
   constexpr bool TR = MODE == UPDATE || MODE == RESULT;
   const int i = MODE == GRAM ? 0 : MODE == SQUARE ? 1 : 2;
-  const Kind& k = KINDS[p.tile[i]];
+  const Kind& k = KINDS[p.part_of[i][0].tile];
   a.unit_m = k.rows, a.unit_n = k.cols;
   a.units_m = (int32_t)((TR ? p.k_pad : p.r_pad) / a.unit_m);
   a.units_n = (int32_t)(p.r_pad / a.unit_n);
   a.halves_log = k.rows == 2 * k.cols;
   a.units = TR ? a.units_m * a.units_n : a.units_m * (a.units_m + 1) / 2 * (a.unit_m / a.unit_n);
   const int32_t all = (int32_t)(a.units * p.batch);
-  const int32_t whole = p.tail[i] < 0 ? all : all / k.round * k.round;
-  for (int part = 0; part < 2; ++part) {
-    a.first = part ? whole : 0;
-    a.count = part ? all - whole : whole;
-    if (a.count <= 0) continue;
-    const int tile = part ? p.tail[i] : p.tile[i];
-    if (tile == K256)
+  for (int j = 0; j < PARTS && a.first < all; ++j) {
+    const Part* const part = &p.part_of[i][j];
+    const int tile = part->tile;
+    // (the padding may hold more units than were counted: the last launch takes all that is left)
+    const bool last = j == PARTS - 1 || part[1].units == 0;
+    a.count = last || part->units > all - a.first ? all - a.first : part->units;
+    if (tile == K256_SQUARE)
+      launch_tile<MODE, Tile256Square>(p, a, s);
+    else if (tile == K256)
       launch_tile<MODE, Tile256>(p, a, s);
     else if (tile == K128_PAIR)
       launch_tile<MODE, Tile128Pair>(p, a, s);
@@ -1041,6 +1136,7 @@ void launch(const Plan& p, Args a, hipStream_t s) {
       launch_tile<MODE, Tile128>(p, a, s);
     else
       launch_tile<MODE, Tile64>(p, a, s);
+    a.first += a.count;
   }
 }
 
