@@ -803,14 +803,27 @@ __device__ __forceinline__ void source_run(const Source& s, int64_t base, float*
   for (int k = 0; k < 8; ++k) sum[k & 1] = fma((double)u[k], (double)u[k], sum[k & 1]);
 }
 
+// S / (|u| + eps) as factor 2^exponent: in one fp32 number it would be infinite for a norm below
+// 1.2e-35, which a zero matrix with a small eps has (and 0 times it NaN), and short of bits for one
+// beyond 3e41.  The exponent is applied first: |u| 2^exponent is at most 1.
+struct Scale {
+  float factor;
+  int exponent;
+};
+__device__ __forceinline__ Scale scale_of(double sum_of_squares, float eps) {
+  int e;
+  const double m = frexp(sqrt(sum_of_squares) + (double)eps, &e);
+  return Scale{(float)((double)S / m), -e};
+}
+
 // Eight neighbours of a row of X, scaled.
 template <bool SPLIT>
 __device__ __forceinline__ void store_x(const Planes& X, int64_t z, int64_t row, int64_t col,
-                                        const float (&v)[8], float inv) {
+                                        const float (&v)[8], const Scale& by) {
   f16x8 hi, lo;
 #pragma unroll
   for (int k = 0; k < 8; ++k) {
-    const HiLo x = split(v[k] * inv);
+    const HiLo x = split(ldexpf(v[k], by.exponent) * by.factor);
     hi[k] = x.hi, lo[k] = x.lo;
   }
   _Float16* p = X.at + z * X.matrix + place<SPLIT>(X.ld, row, col);
@@ -865,7 +878,7 @@ __global__ void __launch_bounds__(PRE)
     }
   }
   const double total = block_sum<PRE>(t < n_part ? part[z * n_part + t] : 0.0, red);
-  const float inv = (float)((double)S / (sqrt(total) + (double)eps));
+  const Scale by = scale_of(total, eps);
   if (tall) {
 #pragma unroll
     for (int h = 0; h < 2; ++h)
@@ -880,7 +893,7 @@ __global__ void __launch_bounds__(PRE)
 #pragma unroll
   for (int h = 0; h < 2; ++h)
     store_x<SPLIT>(X, z, (int64_t)blockIdx.y * 64 + (t >> 3) + 32 * h,
-                   (int64_t)blockIdx.x * 64 + (t & 7) * 8, v[h], inv);
+                   (int64_t)blockIdx.x * 64 + (t & 7) * 8, v[h], by);
 }
 
 struct Steps {
@@ -909,7 +922,7 @@ __global__ void __launch_bounds__(64 * TileOne::WAVES)
   for (int e = threadIdx.x; e < s.rows * runs; e += THREADS)
     source_run(s, base, mom, e / runs, e % runs, sum);
   const double total = block_sum<THREADS>(sum[0] + sum[1], red);
-  const float inv = (float)((double)S / (sqrt(total) + (double)o.eps));
+  const Scale by = scale_of(total, o.eps);
   // X, zero beyond the matrix
   const int k_runs = (int)X0.ld / 8;
   for (int e = threadIdx.x; e < SMALL_ROWS * k_runs; e += THREADS) {
@@ -935,7 +948,7 @@ __global__ void __launch_bounds__(64 * TileOne::WAVES)
         for (int k = 0; k < 8; ++k) v[k] = momentum_u(s, m[k], v[k]);
       }
     }
-    store_x<true>(X0, z, row, col, v, inv);
+    store_x<true>(X0, z, row, col, v, by);
   }
   Args a = {};
   a.unit_m = a.unit_n = 64;
