@@ -297,6 +297,7 @@ __global__ void __launch_bounds__(Shape<TEAM>::BLOCK) norm_fwd_kernel(FwdArgs a)
           mean = base + off;
           ss = fmaf(-(float)a.d * off, off, ss);
         }
+        ss = ss < 0.0f ? 0.0f : ss;    // (a constant row's rounds to either side of 0; NaN stays)
       } else {
 #pragma unroll
         for (int c = 0; c < NC; ++c)
