@@ -332,8 +332,9 @@ int agrl_token_logprob_noalloc(int64_t T, int64_t max_act, int32_t d, int32_t V,
  * Outputs: y, mean[T] (layer; NULL: not written), rstd[T] (NULL: not written).
  * x, y and the parameters may start at any element.  y may be x itself (the
  * same pointer and stride); arrays that overlap in another way are not
- * supported.  A constant row has y = bias up to rounding (layer).  A NaN
- * or infinite element makes its own row NaN and no other.
+ * supported.  A constant row has y = bias up to rounding (layer).  A row with a
+ * NaN or infinite element, or whose sum (layer) or sum of squares passes fp32's
+ * range (elements around 1e19), is NaN as a whole, its rstd too; no other row is.
  */
 enum { AGRL_NORM_LAYER = 0, AGRL_NORM_RMS = 1 };
 int agrl_token_norm_fwd(int64_t T, int32_t d, int32_t kind, int32_t dtype, int32_t w_dtype,

@@ -313,7 +313,10 @@ __global__ void __launch_bounds__(Shape<TEAM>::BLOCK) norm_fwd_kernel(FwdArgs a)
         }
       }
       par ^= 1;    // (the next row's partial sums go to the other half: one barrier a row)
-      const float rstd = 1.0f / sqrtf(fmaf(ss, inv_d, a.eps));
+      // infinite: an infinite element (RMS), or squares beyond fp32's range.  1 / sqrt would be 0 and
+      // the row a finite one, its bias
+      const float var = fmaf(ss, inv_d, a.eps);
+      const float rstd = var < INFINITY ? 1.0f / sqrtf(var) : NAN;
       X* y = (X*)a.y + r * a.ld_y;
 #pragma unroll
       for (int c = 0; c < NC; ++c) {
