@@ -255,8 +255,11 @@ class _Stack(_Owned):
 
 class Orthogonalize(_Stack):
     """Newton-Schulz orthogonalisation of [m, n] matrices (agrl_orthogonalize), a stack of them
-    with ``batch``.  Holds the workspace and the output; the result's type sets the products'
-    precision.  ``__call__`` takes fp32 or bf16 and returns the output."""
+    with ``batch``.  Holds the workspace and the output.  ``__call__`` takes fp32 or bf16 and
+    returns the output.  The result's type sets the products' precision: fp32 as fp32 products;
+    bf16, of more than 128 rows and columns, operands of 11 bits, which leave up to 2e-3 of the
+    result's norm, a few times more where entries repeat (include/agrl.h).  coeffs of three zeros and
+    eps=0 select the defaults."""
 
     def __init__(self, m: int, n: int, out_dtype: torch.dtype = torch.bfloat16,
                  batch: Optional[int] = None, steps: int = 5, coeffs=None, eps: float = 1e-7,
@@ -276,7 +279,8 @@ class Orthogonalize(_Stack):
 class MuonStep(_Stack):
     """One step of the orthogonalised-momentum optimiser for [m, n] weights, or a stack of them
     (agrl_muon_step).  Holds the workspace; the caller holds the weight and the fp32 momentum,
-    which ``__call__`` updates in place."""
+    which ``__call__`` updates in place.  The weight's type sets the products' precision, as the
+    result's does for Orthogonalize.  scale=0 selects sqrt(max(1, m / n))."""
 
     def __init__(self, m: int, n: int, param_dtype: torch.dtype = torch.float32,
                  batch: Optional[int] = None, momentum: float = 0.95, nesterov: bool = True,

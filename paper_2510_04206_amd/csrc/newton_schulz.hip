@@ -42,16 +42,20 @@ typedef _Float16 f16x8 __attribute__((ext_vector_type(8)));
 typedef _Float16 f16x4 __attribute__((ext_vector_type(4)));
 
 // What the matrix cores multiply is fp16 (11 bits), scaled by S so that entries far below the
-// largest keep their bits: |X|, |A|, |B| stay below about 4 for coefficients that keep the
-// singular values bounded, and fp16 reaches 65504 = 16 S.
+// largest keep their bits: |X|, |A|, |B| stay below about 4 for the default coefficients, and fp16
+// reaches 65504 = 16 S.
 //
 // The iterate X is held in two fp16 numbers, hi + lo (22 bits and the scale's range, the state
 // that the term a X carries on), whose hi is the operand.  For a bf16 result the products take
-// hi alone: the rounding of the operands to 11 bits leaves 2e-4 to 1.6e-3 relative in the result
-// (the more, the flatter the singular values), which the result's own rounding (1.7e-3) covers.
-// For an fp32 result every operand is hi + lo and a product is three (hi hi + hi lo + lo hi),
-// which is as exact as fp32 products.  Matrices of few rows take that way too: there the
-// roundings average over few entries (33 x 65: 2.0e-3) and the time is latency.
+// hi alone.  Of the result's norm, the rounding of the operands to 11 bits leaves 2e-4 to 2e-3 where
+// it averages over many unequal entries, as in gradients (the more, the flatter the singular
+// values), as much as the result's own rounding (1.7e-3).  Where entries repeat it adds up: over
+// 1 to 256 equal blocks of one value 5e-3 at the median, 2.6e-2 at most (emulated); the recursion of a
+// singular value, with every rounding 2^-11 and of the worst sign, gives 6.2e-2 to first order.
+// For an fp32 result every operand is hi + lo and a product is three (hi hi + hi lo + lo hi): 0.2 to
+// 1.4 times what fp32 products are off by on noise, at most 9e-6 on the blocks, where those reach
+// 1e-3.  Matrices of few rows take that way too: there the roundings average over few entries (33 x
+// 65: 2.0e-3) and the time is latency.
 constexpr float S = 4096.0f;
 constexpr int SPLIT_ROWS = 128;
 
