@@ -23,27 +23,43 @@ def _row_stride(t: torch.Tensor) -> int:
     return t.stride(-2) if t.shape[-2] > 1 else max(t.shape[-1], 1)
 
 
+def _capturing(stream) -> bool:
+    with torch.cuda.stream(stream):
+        return torch.cuda.is_current_stream_capturing()
+
+
 class _Owned:
-    """Buffers of a handle and the stream they were made on.  A call on another stream first
-    waits for that one (once per stream), and the allocator is told of the use."""
+    """Buffers of a handle and the order of its calls.  They share the workspace and the outputs,
+    so a call on another stream than the last one's first waits for all that stream was given,
+    and the allocator is told of the use.  Calls under capture wait for nothing outside it: whoever
+    captures has synchronised before, and orders the replays and the handle's other calls."""
 
     def __init__(self, device):
         self.device = torch.device(device)
-        self._made_on = torch.cuda.current_stream(self.device)
-        self._seen = {self._made_on.cuda_stream}
+        self._last = torch.cuda.current_stream(self.device)
+        self._raw = self._last.cuda_stream
+        self._told = {self._raw}
+        self._buffers = ()
 
-    def _on(self, stream, buffers):
-        raw = (torch._C._cuda_getCurrentRawStream(self._made_on.device_index) if stream is None
+    def _keep(self, *buffers):
+        self._buffers = tuple(b for b in buffers if b is not None)
+
+    def _on(self, stream):
+        raw = (torch._C._cuda_getCurrentRawStream(self._last.device_index) if stream is None
                else stream.cuda_stream)
-        # (a capture cannot wait for work outside it; whoever captures has synchronised before)
-        if raw in self._seen or torch.cuda.is_current_stream_capturing():
+        if raw == self._raw:
             return
         use = stream if stream is not None else torch.cuda.current_stream(self.device)
-        use.wait_stream(self._made_on)
-        for b in buffers:
-            if b is not None:
+        if _capturing(use):
+            return
+        if _capturing(self._last):
+            raise RuntimeError("agrl: the stream of this handle's last call is being captured")
+        use.wait_stream(self._last)
+        if raw not in self._told:
+            for b in self._buffers:
                 b.record_stream(use)
-        self._seen.add(raw)
+            self._told.add(raw)
+        self._last, self._raw = use, raw
 
 
 def task_adv_norm(traj_id: torch.Tensor, action_mask: torch.Tensor, traj_task: torch.Tensor,
@@ -194,6 +210,7 @@ class TokenNorm(_Owned):
             self.dweight = new(self.d)
             if bias_grad or (bias_grad is None and kind == "layer"):
                 self.dbias = new(self.d)
+        self._keep(self.y, self.mean, self.rstd, self.workspace, self.dx, self.dweight, self.dbias)
 
     def _check(self, x, weight, action_mask):
         _need(x, "x", (self.T, self.d), (self.dtype,))
@@ -207,7 +224,7 @@ class TokenNorm(_Owned):
         par = weight if weight is not None else bias
         if bias is not None:
             _need(bias, "bias", (self.d,), (par.dtype,))
-        self._on(stream, (self.y, self.mean, self.rstd))
+        self._on(stream)
         B.agrl_token_norm_fwd(self.T, self.d, self.kind, _CODES[self.dtype],
                               B.AGRL_F32 if par is None else _CODES[par.dtype], x, _row_stride(x),
                               weight, bias, action_mask, self.eps, self.y, self.d, self.mean,
@@ -219,7 +236,7 @@ class TokenNorm(_Owned):
             raise ValueError("agrl: this TokenNorm was made with grads=False")
         self._check(x, weight, action_mask)
         _need(dy, "dy", (self.T, self.d), _CODES)
-        self._on(stream, (self.mean, self.rstd, self.workspace, self.dx, self.dweight, self.dbias))
+        self._on(stream)
         B.agrl_token_norm_bwd(self.T, self.d, self.kind, _CODES[self.dtype],
                               B.AGRL_F32 if weight is None else _CODES[weight.dtype],
                               _CODES[dy.dtype], x, _row_stride(x), weight, action_mask, dy,
@@ -247,6 +264,7 @@ class _Stack(_Owned):
         self.ns = B.agrl_ns_options(steps=int(steps), a=a, b=b, c=c, eps=eps)
         self.ws_bytes = B.agrl_orthogonalize_workspace_size(self.count, self.m, self.n, self.code)
         self.workspace = torch.empty(max(self.ws_bytes, 1), dtype=torch.uint8, device=self.device)
+        self._keep(self.workspace)
 
     @staticmethod
     def _strides(t):
@@ -266,10 +284,11 @@ class Orthogonalize(_Stack):
                  device="cuda"):
         super().__init__(m, n, out_dtype, batch, steps, coeffs, eps, device)
         self.out = torch.empty(self.shape, dtype=out_dtype, device=self.device)
+        self._keep(self.workspace, self.out)
 
     def __call__(self, g, stream=None):
         _need(g, "g", self.shape, _CODES)
-        self._on(stream, (self.workspace, self.out))
+        self._on(stream)
         B.agrl_orthogonalize(self.count, self.m, self.n, _CODES[g.dtype], g, *self._strides(g),
                              self.code, self.ns, self.workspace, self.ws_bytes, self.out, self.n,
                              self.m * self.n, stream)
@@ -294,7 +313,7 @@ class MuonStep(_Stack):
         _need(param, "param", self.shape, (self.dtype,))
         _need(grad, "grad", self.shape, _CODES)
         _need(momentum, "momentum", self.shape, (torch.float32,))
-        self._on(stream, (self.workspace,))
+        self._on(stream)
         B.agrl_muon_step(self.count, self.m, self.n, _CODES[grad.dtype], grad, *self._strides(grad),
                          self.code, param, *self._strides(param), momentum, float(lr), self.mu,
                          self.nesterov, self.weight_decay, self.scale, self.ns, self.workspace,
