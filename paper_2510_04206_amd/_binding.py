@@ -113,7 +113,7 @@ def _ptr(t: Optional[torch.Tensor]):
         raise ValueError("agrl: arrays must be GPU tensors (the ABI takes device pointers)")
     if not t.is_contiguous():
         raise ValueError("agrl: arrays must be contiguous (the ABI takes plain pointers)")
-    return ctypes.c_void_p(t.data_ptr())
+    return t.data_ptr()
 
 
 def _rows(t: Optional[torch.Tensor]):

@@ -29,14 +29,16 @@ def _capturing(stream) -> bool:
 
 
 class _Owned:
-    """Buffers of a handle and the order of its calls.  They share the workspace and the outputs,
-    so a call on another stream than the last one's first waits for all that stream was given,
-    and the allocator is told of the use.  Calls under capture wait for nothing outside it: whoever
-    captures has synchronised before, and orders the replays and the handle's other calls."""
+    """Buffers of a handle, its device and the order of its calls.  They share the workspace and the
+    outputs, so a call on another stream than the last one's first waits for all that stream was
+    given, and the allocator is told of the use.  Calls under capture wait for nothing outside it:
+    whoever captures has synchronised before, and orders the replays and the handle's other calls.
+    The work goes to the handle's device, whichever is current."""
 
     def __init__(self, device):
-        self.device = torch.device(device)
-        self._last = torch.cuda.current_stream(self.device)
+        self._last = torch.cuda.current_stream(torch.device(device))
+        self._index = self._last.device_index
+        self.device = torch.device("cuda", self._index)
         self._raw = self._last.cuda_stream
         self._told = {self._raw}
         self._buffers = ()
@@ -44,9 +46,33 @@ class _Owned:
     def _keep(self, *buffers):
         self._buffers = tuple(b for b in buffers if b is not None)
 
+    def _need(self, t, name, shape, dtypes):
+        if t.shape != shape or t.dtype not in dtypes:
+            _need(t, name, shape, dtypes)
+        if t.device != self.device:
+            self._same_device(t, name)
+
+    def _same_device(self, t, name):
+        raise ValueError(f"agrl: {name} is on {t.device}, the handle on {self.device}")
+
+    def _away(self, stream) -> bool:
+        """Whether the handle's device is not the current one; if it is, the call is put in order."""
+        if torch.cuda.current_device() != self._index:
+            return True
+        self._on(stream)
+        return False
+
+    def _there(self, call, *args):
+        with torch.cuda.device(self._index):
+            return call(*args)
+
     def _on(self, stream):
-        raw = (torch._C._cuda_getCurrentRawStream(self._last.device_index) if stream is None
-               else stream.cuda_stream)
+        if stream is None:
+            raw = torch._C._cuda_getCurrentRawStream(self._index)
+        else:
+            raw = stream.cuda_stream
+            if stream.device_index != self._index:
+                raise ValueError(f"agrl: the stream is {stream.device}'s, the handle on {self.device}")
         if raw == self._raw:
             return
         use = stream if stream is not None else torch.cuda.current_stream(self.device)
@@ -213,18 +239,19 @@ class TokenNorm(_Owned):
         self._keep(self.y, self.mean, self.rstd, self.workspace, self.dx, self.dweight, self.dbias)
 
     def _check(self, x, weight, action_mask):
-        _need(x, "x", (self.T, self.d), (self.dtype,))
+        self._need(x, "x", (self.T, self.d), (self.dtype,))
         if weight is not None:
-            _need(weight, "weight", (self.d,), _CODES)
+            self._need(weight, "weight", (self.d,), _CODES)
         if action_mask is not None:
-            _need(action_mask, "action_mask", (self.T,), (torch.uint8,))
+            self._need(action_mask, "action_mask", (self.T,), (torch.uint8,))
 
     def forward(self, x, weight=None, bias=None, action_mask=None, stream=None):
         self._check(x, weight, action_mask)
         par = weight if weight is not None else bias
         if bias is not None:
-            _need(bias, "bias", (self.d,), (par.dtype,))
-        self._on(stream)
+            self._need(bias, "bias", (self.d,), (par.dtype,))
+        if self._away(stream):
+            return self._there(self.forward, x, weight, bias, action_mask, stream)
         B.agrl_token_norm_fwd(self.T, self.d, self.kind, _CODES[self.dtype],
                               B.AGRL_F32 if par is None else _CODES[par.dtype], x, _row_stride(x),
                               weight, bias, action_mask, self.eps, self.y, self.d, self.mean,
@@ -235,8 +262,9 @@ class TokenNorm(_Owned):
         if self.dx is None:
             raise ValueError("agrl: this TokenNorm was made with grads=False")
         self._check(x, weight, action_mask)
-        _need(dy, "dy", (self.T, self.d), _CODES)
-        self._on(stream)
+        self._need(dy, "dy", (self.T, self.d), _CODES)
+        if self._away(stream):
+            return self._there(self.backward, x, weight, dy, action_mask, accumulate, stream)
         B.agrl_token_norm_bwd(self.T, self.d, self.kind, _CODES[self.dtype],
                               B.AGRL_F32 if weight is None else _CODES[weight.dtype],
                               _CODES[dy.dtype], x, _row_stride(x), weight, action_mask, dy,
@@ -287,8 +315,9 @@ class Orthogonalize(_Stack):
         self._keep(self.workspace, self.out)
 
     def __call__(self, g, stream=None):
-        _need(g, "g", self.shape, _CODES)
-        self._on(stream)
+        self._need(g, "g", self.shape, _CODES)
+        if self._away(stream):
+            return self._there(self, g, stream)
         B.agrl_orthogonalize(self.count, self.m, self.n, _CODES[g.dtype], g, *self._strides(g),
                              self.code, self.ns, self.workspace, self.ws_bytes, self.out, self.n,
                              self.m * self.n, stream)
@@ -310,10 +339,11 @@ class MuonStep(_Stack):
         self.weight_decay, self.scale = float(weight_decay), float(scale)
 
     def __call__(self, param, grad, momentum, lr: float, stream=None):
-        _need(param, "param", self.shape, (self.dtype,))
-        _need(grad, "grad", self.shape, _CODES)
-        _need(momentum, "momentum", self.shape, (torch.float32,))
-        self._on(stream)
+        self._need(param, "param", self.shape, (self.dtype,))
+        self._need(grad, "grad", self.shape, _CODES)
+        self._need(momentum, "momentum", self.shape, (torch.float32,))
+        if self._away(stream):
+            return self._there(self, param, grad, momentum, lr, stream)
         B.agrl_muon_step(self.count, self.m, self.n, _CODES[grad.dtype], grad, *self._strides(grad),
                          self.code, param, *self._strides(param), momentum, float(lr), self.mu,
                          self.nesterov, self.weight_decay, self.scale, self.ns, self.workspace,
