@@ -394,6 +394,8 @@ size_t agrl_orthogonalize_workspace_size(int64_t batch, int64_t m, int64_t n, in
  *   dtype            type of G: AGRL_BF16 or AGRL_F32; rows ld_g >= n elements apart,
  *                    matrices stride_g apart (not read for batch 1)
  *   out_dtype        type of O: AGRL_BF16 or AGRL_F32; ld_o, stride_o likewise
+ *                    (any strides that keep O's rows apart: matrix after matrix, or
+ *                    rows of the matrices in turn, ld_o >= (batch - 1) stride_o + n)
  *   ns               NULL or options (zero-initialised: the defaults)
  *   workspace        256-byte aligned, agrl_orthogonalize_workspace_size bytes
  * G and O may start at any element and must not overlap.

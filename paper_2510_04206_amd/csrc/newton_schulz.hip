@@ -1224,6 +1224,14 @@ int start(const char* fn, const Plan& p, const agrl_ns_options* opt, const Sourc
   return hip_status(hipGetLastError());
 }
 
+// Whether no two rows of a stack share an element: the matrices follow each other, or their rows
+// take turns (a stack that is a view of [m, batch, n]).  128 bits: strides are the caller's.
+bool rows_apart(int64_t batch, int64_t m, int64_t n, int64_t ld, int64_t stride) {
+  typedef __int128 wide;
+  return (wide)stride >= (wide)(m - 1) * ld + n ||
+         (stride >= n && (wide)ld >= (wide)(batch - 1) * stride + n);
+}
+
 int check(const char* fn, int64_t batch, int64_t m, int64_t n, int32_t in_dtype, int64_t ld_in,
           int64_t stride_in, int32_t out_dtype, int64_t ld_out, int64_t stride_out, Plan* p) {
   if ((in_dtype != AGRL_BF16 && in_dtype != AGRL_F32) ||
@@ -1231,9 +1239,9 @@ int check(const char* fn, int64_t batch, int64_t m, int64_t n, int32_t in_dtype,
     return fail(AGRL_E_DTYPE, fn, "dtype must be AGRL_BF16 or AGRL_F32");
   if (batch < 0 || m < 0 || n < 0) return fail(AGRL_E_SHAPE, fn, "negative size");
   if (ld_in < n || ld_out < n) return fail(AGRL_E_SHAPE, fn, "a row stride is smaller than n");
-  if (batch > 1 && (stride_in < 0 || stride_out < m * ld_out))
-    return fail(AGRL_E_SHAPE, fn, "a matrix stride is too small");
   if (batch == 0 || m == 0 || n == 0) return AGRL_OK;
+  if (batch > 1 && (stride_in < 0 || !rows_apart(batch, m, n, ld_out, stride_out)))
+    return fail(AGRL_E_SHAPE, fn, "a matrix stride is negative, or rows that are written overlap");
   if (!make_plan(batch, m, n, out_dtype, p)) return fail(AGRL_E_SHAPE, fn, "sizes too large");
   return AGRL_OK;
 }
