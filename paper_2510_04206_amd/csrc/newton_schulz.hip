@@ -27,9 +27,12 @@
 #include "../../include/agrl.h"
 #include "common.hpp"
 #include "gemm.hpp"
+#include "ns_plan.hpp"
 
 namespace agrl {
 namespace {
+
+using namespace ns;
 
 int fail(int code, const char* fn, const char* what) {
   char buf[200];
@@ -57,7 +60,6 @@ typedef _Float16 f16x4 __attribute__((ext_vector_type(4)));
 // 1e-3.  Matrices of few rows take that way too: there the roundings average over few entries (33 x
 // 65: 2.0e-3) and the time is latency.
 constexpr float S = 4096.0f;
-constexpr int SPLIT_ROWS = 128;
 
 struct HiLo {
   _Float16 hi, lo;
@@ -732,8 +734,7 @@ struct Source {
   float mu;
   int32_t nesterov;
 };
-constexpr int NORM_GROUPS = 256;   // workgroups of a matrix's sum of squares, at most
-constexpr int NORM_THREADS = 1024, PRE = 256;
+constexpr int PRE = 256;
 
 typedef f32x4 f32x4_any __attribute__((aligned(4)));
 typedef u32x4 u32x4_any __attribute__((aligned(2)));
@@ -911,7 +912,6 @@ struct Steps {
 // us, in separate launches 110; 64 x 256 84, 105.
 using TileOne = Tile<2, 2, 2, 2, 9, 1, true>;
 using TileOneX = Tile<2, 2, 4, 2, 4, 1>;      // B X: fewer, wider tiles, one after the other
-constexpr int SMALL_ROWS = 64, SMALL_K = 256;
 
 __global__ void __launch_bounds__(64 * TileOne::WAVES)
     ns_small_kernel(Source s, Steps o, Result res, Planes X0, Planes X1, Planes A, Planes B) {
@@ -978,132 +978,6 @@ __global__ void __launch_bounds__(64 * TileOne::WAVES)
 }
 
 // ---------------------------------------------------------------------------
-constexpr int64_t MAX_SIDE = (int64_t)1 << 20, MAX_SHORT = (int64_t)1 << 16, MAX_BATCH = 65535;
-
-// A launch of a product: `units` of the product's numbering (see Args) by tile `tile`.
-struct Part {
-  int32_t tile, units;
-};
-constexpr int PARTS = 3;
-
-// Sizes and the workspace of a stack of matrices
-struct Plan {
-  int64_t batch;
-  int32_t r, k, tall, one;                  // one: ns_small_kernel's
-  Part part_of[3][PARTS];                   // of A, B and X; the first one's tile is the unit
-  int64_t r_pad, k_pad;
-  int32_t split, n_part;
-  int64_t x_plane, a_plane;                 // elements
-  size_t part, x[2], a, b, total;           // bytes
-};
-
-// The tiles that a launch can take, and the time of one, in microseconds: a round of workgroups
-// lasts its stages and its end, a launch's start comes on top.  Fitted to launches that were
-// measured; in two parts a last round that fills part of the chip runs faster (the compute units
-// in it share less power and bandwidth), which the wide tiles' own figures hold already.
-struct Kind {
-  int rows, cols, round;      // round: workgroups that the chip holds
-  double one, two, start;     // a stage of one part, of two; a launch
-  double end[2];              // a round's end in A and A A, and in B X
-  double part;                // what of a round's time is left as its share of the chip goes to 0
-};
-constexpr int K64 = 0, K128 = 1, K128_PAIR = 2, K256 = 3, K256_SQUARE = 4;
-constexpr Kind KINDS[] = {
-    {64, 64, 256, 0.24, 0.30, 6.0, {0.0, 0.0}, 1.0},      // nine stages in flight: few, small matrices
-    {128, 128, 256, 0.62, 1.00, 6.0, {0.0, 0.0}, 0.7},    // four, one workgroup a compute unit
-    {128, 128, 512, 0.95, 1.30, 6.0, {0.0, 0.0}, 1.0},    // two, two workgroups
-    {256, 128, 256, 0.79, 0.0, 6.0, {3.0, 14.0}, 1.0},    // (the sums of two parts would not fit
-    {256, 256, 256, 1.20, 0.0, 4.0, {18.0, 10.0}, 1.0},   // the registers of these two)
-};
-// e.g. B X of 1024 x 1024: 9.5 us with the first, 18 and 24 us with the third and fourth; of 8 of
-// them 42, 32 and 29; of 2048 x 2048 36 us, 26 with the second, 33, 37; of 4096 x 4096 254, 137
-// (third), 125 to 135 and, with the fifth, 114.  In two parts: of 1024 x 1024 16 us, third 36; of
-// 8 of them 95, 57; of 4096 x 4096 557, 342; five steps of 2048 x 2048 900 us with the third, 797
-// with the second where it fits.
-double launch_us(const Kind& k, bool split, bool update, int64_t items, double stages) {
-  const int64_t whole = items / k.round, rest = items % k.round;
-  const double part = split ? k.part : 1.0;
-  const double rounds = whole + (rest ? part + (1.0 - part) * rest / k.round : 0.0);
-  return rounds * (stages * (split ? k.two : k.one) + k.end[update]) + k.start;
-}
-
-// Each product takes the tile that is done first; where its last round would leave most of the
-// chip idle, that round's units go to a launch of smaller tiles, and so on (B X of 14336 x 3584: 784
-// tiles of 256 x 256 are three rounds of 256 and 16 units more, which go by 64 x 64).  The time of
-// `units` of unit kind `of` by tile t and smaller ones; out: the launches, `left` of them at most.
-double plan_parts(bool split, bool update, double stages, int of, int t, int64_t units, int left,
-                  Part* out) {
-  const Kind& k = KINDS[t];
-  const int64_t per = (int64_t)(KINDS[of].rows / k.rows) * (KINDS[of].cols / k.cols);
-  double best = launch_us(k, split, update, units * per, stages);
-  out[0] = Part{t, (int32_t)units};
-  if (left > 1) out[1].units = 0;
-  const int64_t whole = units * per / k.round * k.round / per;
-  if (left == 1 || whole == 0 || whole == units) return best;
-  const double first = launch_us(k, split, update, whole * per, stages);
-  for (int next = K64; next < t; ++next) {
-    if (KINDS[next].rows * KINDS[next].cols >= k.rows * k.cols) continue;
-    Part rest[PARTS] = {};
-    const double us =
-        first + plan_parts(split, update, stages, of, next, units - whole, left - 1, rest);
-    if (us >= best) continue;
-    best = us;
-    out[0].units = (int32_t)whole;
-    for (int i = 1; i < left; ++i) out[i] = rest[i - 1];
-  }
-  return best;
-}
-
-void choose_tiles(Plan* p) {
-  for (int i = 0; i < 3; ++i) {
-    double best = 0.0;
-    const double stages = (i == 0 ? p->k : p->r) / (p->split ? 32.0 : 64.0);
-    for (int t = K64; t <= (p->split ? K128_PAIR : K256_SQUARE); ++t) {
-      const Kind& k = KINDS[t];
-      const int64_t r = cdiv(p->r, k.rows), x = cdiv(p->k, k.rows);
-      const int64_t units = p->batch * (i == 2 ? r * x : r * (r + 1) / 2) * (k.rows / k.cols);
-      Part parts[PARTS] = {};
-      const double us = plan_parts(p->split, i == 2, stages, t, t, units, PARTS, parts);
-      if (t > K64 && us >= best) continue;
-      best = us;
-      for (int j = 0; j < PARTS; ++j) p->part_of[i][j] = parts[j];
-    }
-  }
-}
-
-bool make_plan(int64_t batch, int64_t m, int64_t n, int32_t out_dtype, Plan* p) {
-  if (batch <= 0 || batch > MAX_BATCH || m <= 0 || n <= 0 || m > MAX_SIDE || n > MAX_SIDE)
-    return false;
-  const int64_t r = m < n ? m : n, k = m < n ? n : m;
-  if (r > MAX_SHORT) return false;
-  p->batch = batch, p->r = (int32_t)r, p->k = (int32_t)k, p->tall = m > n;
-  p->split = out_dtype == AGRL_F32 || r <= SPLIT_ROWS;
-  choose_tiles(p);
-  p->one = p->r <= SMALL_ROWS && p->k <= SMALL_K;
-  int64_t pad = 128;
-  for (const auto& parts : p->part_of)
-    if (KINDS[parts[0].tile].rows > pad) pad = KINDS[parts[0].tile].rows;
-  p->r_pad = p->one ? 64 : cdiv(r, pad) * pad;
-  p->k_pad = cdiv(k, pad) * pad;
-  const int64_t per = cdiv(m * cdiv(n, (int64_t)8), (int64_t)NORM_THREADS);
-  p->n_part = (int32_t)(per < NORM_GROUPS ? per : NORM_GROUPS);
-  p->x_plane = batch * p->r_pad * p->k_pad;
-  p->a_plane = batch * p->r_pad * p->r_pad;
-  size_t at = 0;
-  auto take = [&](size_t bytes) {
-    const size_t here = at;
-    at += (bytes + 255) / 256 * 256;
-    return here;
-  };
-  p->part = take((size_t)batch * p->n_part * sizeof(double));
-  for (int i = 0; i < 2; ++i) p->x[i] = take((size_t)p->x_plane * 4);
-  const size_t a_bytes = (size_t)p->a_plane * (p->split ? 4 : 2);
-  p->a = take(a_bytes);
-  p->b = take(a_bytes);
-  p->total = at;
-  return true;
-}
-
 using Tile64 = TileOne;
 using Tile128 = Tile<2, 2, 4, 4, 4, 1, true>;
 using Tile128Pair = Tile<2, 2, 4, 4, 2, 2>;
@@ -1128,32 +1002,22 @@ void launch_tile(const Plan& p, Args a, hipStream_t s) {
 
 template <int MODE>
 void launch(const Plan& p, Args a, hipStream_t s) {
-  constexpr bool TR = MODE == UPDATE || MODE == RESULT;
-  const int i = MODE == GRAM ? 0 : MODE == SQUARE ? 1 : 2;
-  const Kind& k = KINDS[p.part_of[i][0].tile];
-  a.unit_m = k.rows, a.unit_n = k.cols;
-  a.units_m = (int32_t)((TR ? p.k_pad : p.r_pad) / a.unit_m);
-  a.units_n = (int32_t)(p.r_pad / a.unit_n);
-  a.halves_log = k.rows == 2 * k.cols;
-  a.units = TR ? a.units_m * a.units_n : a.units_m * (a.units_m + 1) / 2 * (a.unit_m / a.unit_n);
-  const int32_t all = (int32_t)(a.units * p.batch);
-  for (int j = 0; j < PARTS && a.first < all; ++j) {
-    const Part* const part = &p.part_of[i][j];
-    const int tile = part->tile;
-    // (the padding may hold more units than were counted: the last launch takes all that is left)
-    const bool last = j == PARTS - 1 || part[1].units == 0;
-    a.count = last || part->units > all - a.first ? all - a.first : part->units;
-    if (tile == K256_SQUARE)
+  Launch parts[PARTS];
+  const int n = product_launches(p, MODE == GRAM ? 0 : MODE == SQUARE ? 1 : 2, parts);
+  for (int j = 0; j < n; ++j) {
+    const Launch& l = parts[j];
+    a.unit_m = l.unit_m, a.unit_n = l.unit_n, a.units_m = l.units_m, a.units_n = l.units_n;
+    a.units = l.units, a.first = l.first, a.count = l.count, a.halves_log = l.halves_log;
+    if (l.tile == K256_SQUARE)
       launch_tile<MODE, Tile256Square>(p, a, s);
-    else if (tile == K256)
+    else if (l.tile == K256)
       launch_tile<MODE, Tile256>(p, a, s);
-    else if (tile == K128_PAIR)
+    else if (l.tile == K128_PAIR)
       launch_tile<MODE, Tile128Pair>(p, a, s);
-    else if (tile == K128)
+    else if (l.tile == K128)
       launch_tile<MODE, Tile128>(p, a, s);
     else
       launch_tile<MODE, Tile64>(p, a, s);
-    a.first += a.count;
   }
 }
 
