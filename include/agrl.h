@@ -32,6 +32,8 @@
  *     allocates no memory.  Scalars and `opt` are host values.  `stream` is a
  *     hipStream_t passed as void* (NULL = the null stream).
  *   - Calls only enqueue work on `stream` and return; they never synchronise.
+ *     Calls that share a workspace or an output are ordered by the caller when
+ *     they are on different streams.
  *     Argument errors are reported synchronously, before anything is
  *     launched, and leave every output untouched.
  *   - Row-major, contiguous (where a call has row and matrix strides in its

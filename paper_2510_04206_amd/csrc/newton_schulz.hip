@@ -11,16 +11,19 @@
 // B X reads X transposed out of LDS, so X lies in memory once, and every product writes its result
 // as the next one's operand.  A step is three launches; two before the first make |G| and X.
 //
-// Measured (MI355X, five steps): 5120 x 5120 fp32 -> bf16 2.5 ms, 1.06 PFLOP/s of the operations
+// Measured (MI355X, five steps): 5120 x 5120 fp32 -> bf16 2.5 ms, 1.07 PFLOP/s of the operations
 // above (a 16384^3 library product in fp16 reaches 1.41), 8192 x 8192 8.6 ms, 1.28; 14336 x 3584 with
-// momentum and a bf16 weight 3.0 ms, 0.99; 8 x 1024 x 1024 fp32 -> fp32 0.76 ms, 0.68 PFLOP/s of
-// fp16 products; 128 x 512 114 us and 256 x 256 fp32 124 us, of which 17 launches' own 4 us each are
-// two thirds.
+// momentum and a bf16 weight 3.0 ms, 1.00, with an fp32 weight 8.3 ms, 1.08 PFLOP/s of fp16 products;
+// 8 x 1024 x 1024 fp32 -> fp32 0.75 ms, 0.69 of the same; 128 x 512 114 us and 256 x 256 fp32 124 us,
+// of which 17 launches' own 4 us each are 60 and 55%.
 // What is left: the last round of tiles is not full (B X of 5120 x 5120: 400 tiles of 256 x 256 for
-// 256 units), at a tile's end all compute units move 512 KiB at once (20 of 140 us a tile there),
-// and a 256 x 256 stage of 64 takes 1.4 us where the matrix cores alone would take 1.0 at the clock
-// that the power limit leaves (2.0 to 2.1 GHz).  In two parts the matrix cores are busy 40 to 55% of
-// the time: a wave has 64 additions and 16 KiB of LDS reads beside each 48 matrix instructions.
+// 256 units: matrix cores busy 0.47 of its time, 0.55 in 14336 x 3584's), at a tile's end all compute
+// units move 512 KiB at once (20 of 140 us a tile there), and a 256 x 256 stage of 64 takes 1.4 us
+// where the matrix cores alone would take 1.0 at the clock that the power limit leaves (1.9 to 2.1
+// GHz).  In two parts, 8 x 1024 x 1024, they are busy 0.2 (A A) to 0.4 (B X) of the time; a wave waits a
+// third of its cycles for memory or a barrier and another third to issue, without bank conflicts and
+// with LDS 0.13 busy at most: which of the three dependent products of a block, the 64 additions
+// beside each 48 and the last round's 32 tiles of 288 weighs most has not been measured.
 #include <math.h>
 #include <stdio.h>
 

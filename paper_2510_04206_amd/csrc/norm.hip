@@ -21,10 +21,13 @@
 // cancellation.  One LDS exchange and one barrier per row and team.
 //
 // Measured (MI355X; a copy of 2 GiB moves 4.9 TB/s): forward of 65536 x 5120 bf16 RMS with a third
-// of the rows live 190 us, 4.7 TB/s; of 3823 x 1001, no row aligned, 7.8 us; backward of 32768 x
+// of the rows live 190 us, 4.7 TB/s; of 3823 x 1001, no row aligned, 7.4 us, where a copy's rate would
+// take 3.1 (a row a team: nothing is loaded ahead, and the parameters come first); backward of 32768 x
 // 3584 bf16 with fp32 dy, a third live, 117 us, 4.0 TB/s (5 us of it the second launch, which
-// adds the workgroups' partial sums); of 65536 x 4096, all live, dy bf16, 294 us, 5.5 TB/s.  Small
-// calls are one or two launches: one row of 256 takes 3 us on the GPU.
+// adds the workgroups' partial sums); of 65536 x 4096, all live, dy bf16, 294 us, 5.5 TB/s.  Past d =
+// 8192 the backward's sums do not fit the 128 registers that 1024 lanes leave each and go to
+// scratch memory: 16384 x 12288 725 us, 2.2 TB/s (of 16384 x 8192 205 us, 5.2).  Small calls are
+// one or two launches: one row of 256 takes 2.3 us on the GPU.
 #include <math.h>
 #include <stdio.h>
 
