@@ -55,18 +55,15 @@ class _Owned:
     def _same_device(self, t, name):
         raise ValueError(f"agrl: {name} is on {t.device}, the handle on {self.device}")
 
-    def _away(self, stream) -> bool:
-        """Whether the handle's device is not the current one; if it is, the call is put in order."""
-        if torch.cuda.current_device() != self._index:
-            return True
-        self._on(stream)
-        return False
-
     def _there(self, call, *args):
         with torch.cuda.device(self._index):
             return call(*args)
 
-    def _on(self, stream):
+    def _order(self, stream):
+        """Puts a call on `stream` (None: the current one) behind the handle's last one.  Returns the
+        stream, or None if the handle's device is not the current one."""
+        if torch.cuda.current_device() != self._index:
+            return None
         if stream is None:
             raw = torch._C._cuda_getCurrentRawStream(self._index)
         else:
@@ -74,10 +71,10 @@ class _Owned:
             if stream.device_index != self._index:
                 raise ValueError(f"agrl: the stream is {stream.device}'s, the handle on {self.device}")
         if raw == self._raw:
-            return
+            return self._last
         use = stream if stream is not None else torch.cuda.current_stream(self.device)
         if _capturing(use):
-            return
+            return use
         if _capturing(self._last):
             raise RuntimeError("agrl: the stream of this handle's last call is being captured")
         use.wait_stream(self._last)
@@ -86,6 +83,7 @@ class _Owned:
                 b.record_stream(use)
             self._told.add(raw)
         self._last, self._raw = use, raw
+        return use
 
 
 def task_adv_norm(traj_id: torch.Tensor, action_mask: torch.Tensor, traj_task: torch.Tensor,
@@ -250,12 +248,13 @@ class TokenNorm(_Owned):
         par = weight if weight is not None else bias
         if bias is not None:
             self._need(bias, "bias", (self.d,), (par.dtype,))
-        if self._away(stream):
+        on = self._order(stream)
+        if on is None:
             return self._there(self.forward, x, weight, bias, action_mask, stream)
         B.agrl_token_norm_fwd(self.T, self.d, self.kind, _CODES[self.dtype],
                               B.AGRL_F32 if par is None else _CODES[par.dtype], x, _row_stride(x),
                               weight, bias, action_mask, self.eps, self.y, self.d, self.mean,
-                              self.rstd, stream)
+                              self.rstd, on)
         return self.y, self.mean, self.rstd
 
     def backward(self, x, weight, dy, action_mask=None, accumulate: bool = False, stream=None):
@@ -263,14 +262,15 @@ class TokenNorm(_Owned):
             raise ValueError("agrl: this TokenNorm was made with grads=False")
         self._check(x, weight, action_mask)
         self._need(dy, "dy", (self.T, self.d), _CODES)
-        if self._away(stream):
+        on = self._order(stream)
+        if on is None:
             return self._there(self.backward, x, weight, dy, action_mask, accumulate, stream)
         B.agrl_token_norm_bwd(self.T, self.d, self.kind, _CODES[self.dtype],
                               B.AGRL_F32 if weight is None else _CODES[weight.dtype],
                               _CODES[dy.dtype], x, _row_stride(x), weight, action_mask, dy,
                               _row_stride(dy), self.mean, self.rstd, int(accumulate),
                               self.workspace, self.ws_bytes, self.dx, self.d, self.dweight,
-                              self.dbias, stream)
+                              self.dbias, on)
         return self.dx, self.dweight, self.dbias
 
 
@@ -316,11 +316,12 @@ class Orthogonalize(_Stack):
 
     def __call__(self, g, stream=None):
         self._need(g, "g", self.shape, _CODES)
-        if self._away(stream):
+        on = self._order(stream)
+        if on is None:
             return self._there(self, g, stream)
         B.agrl_orthogonalize(self.count, self.m, self.n, _CODES[g.dtype], g, *self._strides(g),
                              self.code, self.ns, self.workspace, self.ws_bytes, self.out, self.n,
-                             self.m * self.n, stream)
+                             self.m * self.n, on)
         return self.out
 
 
@@ -342,10 +343,11 @@ class MuonStep(_Stack):
         self._need(param, "param", self.shape, (self.dtype,))
         self._need(grad, "grad", self.shape, _CODES)
         self._need(momentum, "momentum", self.shape, (torch.float32,))
-        if self._away(stream):
+        on = self._order(stream)
+        if on is None:
             return self._there(self, param, grad, momentum, lr, stream)
         B.agrl_muon_step(self.count, self.m, self.n, _CODES[grad.dtype], grad, *self._strides(grad),
                          self.code, param, *self._strides(param), momentum, float(lr), self.mu,
                          self.nesterov, self.weight_decay, self.scale, self.ns, self.workspace,
-                         self.ws_bytes, stream)
+                         self.ws_bytes, on)
         return param
