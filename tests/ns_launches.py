@@ -1,7 +1,7 @@
 """Sizes that take every launch that the Newton-Schulz products can take, and the plans behind them.
 
 A launch's class is (product 0 A, 1 A A, 2 B X; parts 1 or 2; the unit's tile; the launch's own tile;
-the how manieth of the product it is; whether its workgroups run on from tile to tile).
+its place among the launches of the product; whether its workgroups run on from tile to tile).
 """
 import os
 import subprocess
