@@ -25,7 +25,15 @@
  *   agrl_token_norm_fwd    layer or RMS norm of the token rows that become H;
  *   agrl_token_norm_bwd    its gradient, from the loss's dH;
  *   agrl_orthogonalize     Newton-Schulz orthogonalisation of matrices;
- *   agrl_muon_step         the optimiser step of weight matrices with it.
+ *   agrl_muon_step         the optimiser step of weight matrices with it;
+ *
+ * and what stands between the packed token ids and that norm and knows of the packing:
+ *
+ *   agrl_token_embed_fwd   rows of the embedding, scaled;
+ *   agrl_token_embed_bwd   its gradient, added up by token id;
+ *   agrl_rotate_heads      query and key heads turned by their tokens' positions (and back);
+ *   agrl_attention_fwd     causal attention within each sequence of the stream;
+ *   agrl_attention_bwd     its gradients.
  *
  * Conventions for every entry point:
  *   - Array arguments are DEVICE pointers owned by the caller; the library
@@ -434,6 +442,112 @@ int agrl_muon_step(int64_t batch, int64_t m, int64_t n, int32_t grad_dtype, cons
                    int32_t nesterov, float weight_decay, float scale, const agrl_ns_options* ns,
                    void* workspace, size_t ws_bytes, void* stream);
 
+/*
+ * Embedding of a packed stream: y[n] = scale * weight[token_id[n]].
+ *   T, d, V           tokens, row length (<= 2^20), rows of the embedding
+ *   w_dtype, dtype    type of weight and of y: AGRL_BF16 or AGRL_F32; y is rounded once
+ *   weight[V, d]      contiguous; token_id[T] int32
+ *   live_mask[T]      uint8; NULL: every token is live.  A token with mask 0 is not read (nor
+ *                     its id); its y is +0
+ *   scale             finite
+ *   y[T, d]           rows ld_y >= d elements apart
+ * weight and y may start at any element.  A live token_id outside [0, V) sets bit 1 of the
+ * device error word and makes its row NaN.
+ */
+int agrl_token_embed_fwd(int64_t T, int32_t d, int32_t V, int32_t w_dtype, int32_t dtype,
+                         const void* weight, const int32_t* token_id, const uint8_t* live_mask,
+                         float scale, void* y, int64_t ld_y, void* stream);
+
+/* Bytes of workspace for agrl_token_embed_bwd; 0 for invalid sizes.  Host-only. */
+size_t agrl_token_embed_bwd_workspace_size(int64_t T, int32_t d, int32_t V);
+
+/*
+ * Gradient of the embedding: dweight[v] = scale * sum of dy[n] over the live tokens n with
+ * token_id[n] = v, in the tokens' order, in fp32.
+ *   dy[T, d]          in dy_dtype, rows ld_dy >= d elements apart, from any element
+ *   accumulate        0: every row of dweight is written (0 where no token has its id); 1: the
+ *                     sums are added, rows without a token are not touched.  A tied head's
+ *                     gradient: agrl_policy_loss_bwd first, then this with accumulate 1
+ *   workspace         256-byte aligned, agrl_token_embed_bwd_workspace_size bytes
+ *   dweight[V, d]     fp32, contiguous, 4-byte aligned
+ * A live token_id outside [0, V) sets bit 1 of the device error word and adds nothing.  T = 0
+ * writes zeros (accumulate 0) or nothing.
+ */
+int agrl_token_embed_bwd(int64_t T, int32_t d, int32_t V, int32_t dy_dtype,
+                         const int32_t* token_id, const uint8_t* live_mask, const void* dy,
+                         int64_t ld_dy, float scale, int32_t accumulate, void* workspace,
+                         size_t ws_bytes, float* dweight, void* stream);
+
+/*
+ * Heads [T, n_head, d] in the two calls below: `ld` elements between tokens, `head` between
+ * heads, the d elements of a head adjacent, from any element.  Inputs may have any strides that are
+ * not negative (0 repeats a head or a token); the heads of an output must not overlap.
+ *
+ * Rotation by position: of each head's first `rot` elements (even, <= d) the pairs
+ * (i, i + rot / 2), or (2 i, 2 i + 1) with interleaved = 1, are turned by the angle
+ * position * base^(-2 i / rot):  (p, q) -> (p cos - q sin, p sin + q cos).  Elements from rot on are
+ * copied.  inverse = 1 turns back, which is the gradient of the rotation.
+ *   T, n_head, d      d <= 512 (AGRL_E_UNSUPPORTED above)
+ *   dtype             type of x and y: AGRL_BF16 or AGRL_F32; angles are formed in 64 bits, the
+ *                     rest in 32, y is rounded once
+ *   position[T]       int32, any value; NULL: the token's number
+ *   base              finite, > 0
+ *   y                 may be x itself (the same strides); arrays that overlap in another way
+ *                     are not supported
+ */
+int agrl_rotate_heads(int64_t T, int32_t n_head, int32_t d, int32_t rot, int32_t dtype,
+                      const void* x, int64_t ld_x, int64_t head_x, const int32_t* position,
+                      double base, int32_t interleaved, int32_t inverse, void* y, int64_t ld_y,
+                      int64_t head_y, void* stream);
+
+/*
+ * Causal attention within each sequence of a packed stream of T tokens:
+ *   S = scale q k^T over the keys of the token's sequence up to the token itself,
+ *   o = softmax(S) v,  lse = log sum exp S
+ *   n_head, n_kv      query heads; key heads, a divisor: query head h reads key head h / (n_head / n_kv)
+ *   d                 head size, <= 128 (AGRL_E_UNSUPPORTED above)
+ *   dtype             type of q, k, v and o: AGRL_BF16 or AGRL_F32
+ *   q [T, n_head, d]; k, v [T, n_kv, d]
+ *   seq_start[n_seq + 1]  int32: sequence i is the tokens seq_start[i] .. seq_start[i + 1] - 1; it may
+ *                     be empty.  Tokens before the first offset and from the last one on belong to no
+ *                     sequence: their values do not matter, their o is +0 and their lse 0.  n_seq = 0:
+ *                     no token belongs to one.  Offsets that decrease or leave [0, T] set bit 32 of
+ *                     the device error word; what o holds is then unspecified
+ *   scale             finite, > 0
+ * Outputs: o [T, n_head, d]; lse [n_head, T] fp32 (NULL: not written; the backward needs it).
+ * Products of bf16 inputs and all sums are fp32, P is rounded to `dtype` before it meets v, o once.
+ * No token of another sequence and no later one of its own reaches a row, not even a NaN or
+ * infinite one; an element of v that is not finite makes what counts it NaN or infinite.
+ */
+int agrl_attention_fwd(int64_t T, int32_t n_seq, int32_t n_head, int32_t n_kv, int32_t d,
+                       int32_t dtype, const void* q, int64_t ld_q, int64_t head_q, const void* k,
+                       int64_t ld_k, int64_t head_k, const void* v, int64_t ld_v, int64_t head_v,
+                       const int32_t* seq_start, float scale, void* o, int64_t ld_o,
+                       int64_t head_o, float* lse, void* stream);
+
+/* Bytes of workspace for agrl_attention_bwd; 0 for invalid sizes.  Host-only. */
+size_t agrl_attention_bwd_workspace_size(int64_t T, int32_t n_head, int32_t n_kv, int32_t d,
+                                         int32_t dtype);
+
+/*
+ * Gradients of agrl_attention_fwd.  With P = exp(S - lse), D = sum over d of dout o and
+ * dS = P (dout v^T - D):  dv = P^T dout, dq = scale dS k, dk = scale dS^T q; dk and dv are the sums over
+ * the query heads that share a key head (in a fixed order).
+ *   o, lse            as the forward left them; dout [T, n_head, d] in `dtype`
+ *   workspace         256-byte aligned, agrl_attention_bwd_workspace_size bytes
+ * Outputs in `dtype`: dq [T, n_head, d], dk and dv [T, n_kv, d] (+0 on tokens of no sequence); they may be
+ * parts of one array [T, n_head + 2 n_kv, d].  P and dS are rounded to `dtype` before they
+ * meet dout, k and q; sums are fp32.
+ */
+int agrl_attention_bwd(int64_t T, int32_t n_seq, int32_t n_head, int32_t n_kv, int32_t d,
+                       int32_t dtype, const void* q, int64_t ld_q, int64_t head_q, const void* k,
+                       int64_t ld_k, int64_t head_k, const void* v, int64_t ld_v, int64_t head_v,
+                       const int32_t* seq_start, float scale, const void* o, int64_t ld_o,
+                       int64_t head_o, const float* lse, const void* dout, int64_t ld_do,
+                       int64_t head_do, void* workspace, size_t ws_bytes, void* dq, int64_t ld_dq,
+                       int64_t head_dq, void* dk, int64_t ld_dk, int64_t head_dk, void* dv,
+                       int64_t ld_dv, int64_t head_dv, void* stream);
+
 /* Text for a status code (static storage). */
 const char* agrl_status_string(int status);
 
@@ -443,7 +557,7 @@ const char* agrl_last_error(void);
 /*
  * Synchronises `stream`, then reads and clears the current device's error
  * word into *code (0 = no fault; bits: 1 token id, 2 trajectory id, 4 task
- * id, 8 group id, 16 more action tokens than max_act).
+ * id, 8 group id, 16 more action tokens than max_act, 32 sequence offsets).
  */
 int agrl_get_device_error(void* stream, int32_t* code);
 

@@ -23,10 +23,11 @@ AGRL_NORM_RMS = 1
 AGRL_NOALLOC_SCRATCH_BYTES = 64 << 20     # include/agrl.h
 ERROR_BITS = {1: "token id out of range", 2: "trajectory id out of range",
               4: "task id out of range", 8: "group id out of range",
-              16: "more action tokens than max_act"}
+              16: "more action tokens than max_act", 32: "sequence offsets out of order or range"}
 
 _c_i64, _c_i32, _c_f32, _c_p, _c_sz = (ctypes.c_int64, ctypes.c_int32, ctypes.c_float,
                                        ctypes.c_void_p, ctypes.c_size_t)
+_HEADS = [_c_p, _c_i64, _c_i64]      # [T, n_head, d]: address, distance of rows, of heads
 
 
 class agrl_options(ctypes.Structure):
@@ -80,6 +81,19 @@ _SIGS = {
     "agrl_muon_step": (_c_i32, [_c_i64, _c_i64, _c_i64, _c_i32, _c_p, _c_i64, _c_i64, _c_i32,
                                 _c_p, _c_i64, _c_i64, _c_p, _c_f32, _c_f32, _c_i32, _c_f32, _c_f32,
                                 _c_p, _c_p, _c_sz, _c_p]),
+    "agrl_token_embed_fwd": (_c_i32, [_c_i64, _c_i32, _c_i32, _c_i32, _c_i32, _c_p, _c_p, _c_p, _c_f32,
+                                      _c_p, _c_i64, _c_p]),
+    "agrl_token_embed_bwd_workspace_size": (_c_sz, [_c_i64, _c_i32, _c_i32]),
+    "agrl_token_embed_bwd": (_c_i32, [_c_i64, _c_i32, _c_i32, _c_i32, _c_p, _c_p, _c_p, _c_i64, _c_f32,
+                                      _c_i32, _c_p, _c_sz, _c_p, _c_p]),
+    "agrl_rotate_heads": (_c_i32, [_c_i64, _c_i32, _c_i32, _c_i32, _c_i32, *_HEADS, _c_p,
+                                   ctypes.c_double, _c_i32, _c_i32, *_HEADS, _c_p]),
+    "agrl_attention_fwd": (_c_i32, [_c_i64, _c_i32, _c_i32, _c_i32, _c_i32, _c_i32, *_HEADS, *_HEADS,
+                                    *_HEADS, _c_p, _c_f32, *_HEADS, _c_p, _c_p]),
+    "agrl_attention_bwd_workspace_size": (_c_sz, [_c_i64, _c_i32, _c_i32, _c_i32, _c_i32]),
+    "agrl_attention_bwd": (_c_i32, [_c_i64, _c_i32, _c_i32, _c_i32, _c_i32, _c_i32, *_HEADS, *_HEADS,
+                                    *_HEADS, _c_p, _c_f32, *_HEADS, _c_p, *_HEADS, _c_p, _c_sz,
+                                    *_HEADS, *_HEADS, *_HEADS, _c_p]),
     "agrl_status_string": (ctypes.c_char_p, [_c_i32]),
     "agrl_last_error": (ctypes.c_char_p, []),
     "agrl_get_device_error": (_c_i32, [_c_p, _c_p]),
@@ -126,6 +140,15 @@ def _rows(t: Optional[torch.Tensor]):
     if t.stride(-1) != 1 and t.shape[-1] > 1:
         raise ValueError("agrl: the elements of a row must be adjacent")
     return t.data_ptr()
+
+
+def _heads(t: Optional[torch.Tensor]):
+    """Address, distance of rows and distance of heads of a [T, n_head, d] tensor (1 token or 1 head has no
+    neighbour: 0)."""
+    p = _rows(t)
+    if p is None:
+        return None, 0, 0
+    return p, t.stride(0) if t.shape[0] > 1 else 0, t.stride(1) if t.shape[1] > 1 else 0
 
 
 def _stream(stream) -> ctypes.c_void_p:
@@ -263,6 +286,50 @@ def agrl_muon_step(batch, m, n, grad_dtype, grad, ld_grad, stride_grad, param_dt
         batch, m, n, grad_dtype, _rows(grad), ld_grad, stride_grad, param_dtype, _rows(param),
         ld_param, stride_param, _ptr(momentum), lr, mu, nesterov, weight_decay, scale, _ns(ns),
         _ptr(workspace), ws_bytes, _stream(stream)))
+
+
+def agrl_token_embed_fwd(T, d, V, w_dtype, dtype, weight, token_id, live_mask, scale, y, ld_y,
+                         stream=None) -> None:
+    _check("agrl_token_embed_fwd", lib().agrl_token_embed_fwd(
+        T, d, V, w_dtype, dtype, _ptr(weight), _ptr(token_id), _ptr(live_mask), scale, _rows(y), ld_y,
+        _stream(stream)))
+
+
+def agrl_token_embed_bwd_workspace_size(T, d, V) -> int:
+    return int(lib().agrl_token_embed_bwd_workspace_size(T, d, V))
+
+
+def agrl_token_embed_bwd(T, d, V, dy_dtype, token_id, live_mask, dy, ld_dy, scale, accumulate, workspace,
+                         ws_bytes, dweight, stream=None) -> None:
+    _check("agrl_token_embed_bwd", lib().agrl_token_embed_bwd(
+        T, d, V, dy_dtype, _ptr(token_id), _ptr(live_mask), _rows(dy), ld_dy, scale, accumulate,
+        _ptr(workspace), ws_bytes, _ptr(dweight), _stream(stream)))
+
+
+def agrl_rotate_heads(T, n_head, d, rot, dtype, x, position, base, interleaved, inverse, y,
+                      stream=None) -> None:
+    _check("agrl_rotate_heads", lib().agrl_rotate_heads(
+        T, n_head, d, rot, dtype, *_heads(x), _ptr(position), base, interleaved, inverse, *_heads(y),
+        _stream(stream)))
+
+
+def agrl_attention_fwd(T, n_seq, n_head, n_kv, d, dtype, q, k, v, seq_start, scale, o, lse,
+                       stream=None) -> None:
+    _check("agrl_attention_fwd", lib().agrl_attention_fwd(
+        T, n_seq, n_head, n_kv, d, dtype, *_heads(q), *_heads(k), *_heads(v), _ptr(seq_start), scale,
+        *_heads(o), _ptr(lse), _stream(stream)))
+
+
+def agrl_attention_bwd_workspace_size(T, n_head, n_kv, d, dtype) -> int:
+    return int(lib().agrl_attention_bwd_workspace_size(T, n_head, n_kv, d, dtype))
+
+
+def agrl_attention_bwd(T, n_seq, n_head, n_kv, d, dtype, q, k, v, seq_start, scale, o, lse, do, workspace,
+                       ws_bytes, dq, dk, dv, stream=None) -> None:
+    _check("agrl_attention_bwd", lib().agrl_attention_bwd(
+        T, n_seq, n_head, n_kv, d, dtype, *_heads(q), *_heads(k), *_heads(v), _ptr(seq_start), scale,
+        *_heads(o), _ptr(lse), *_heads(do), _ptr(workspace), ws_bytes, *_heads(dq), *_heads(dk),
+        *_heads(dv), _stream(stream)))
 
 
 def agrl_get_device_error(stream=None) -> int:

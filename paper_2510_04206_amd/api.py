@@ -352,3 +352,162 @@ class MuonStep(_Stack):
                          self.nesterov, self.weight_decay, self.scale, self.ns, self.workspace,
                          self.ws_bytes, on)
         return param
+
+
+class TokenEmbedding(_Owned):
+    """Embedding of T packed token ids, rows of a [V, d] weight (agrl_token_embed_*).
+
+    ``forward`` returns y [T, d] = scale weight[token_id], in ``dtype`` whatever the weight's type (w_dtype,
+    by default the same).  ``backward`` adds up dy's rows by id, in the tokens' order, into ``dweight`` [V, d]
+    fp32: its own, or the one given (a tied head's: ``dweight=loss.dW`` and accumulate=True).  Tokens whose
+    live_mask is 0 are not read: y is +0 there, dy goes nowhere.  grads=False leaves the backward out.
+    """
+
+    def __init__(self, T: int, V: int, d: int, dtype: torch.dtype, w_dtype: Optional[torch.dtype] = None,
+                 scale: float = 1.0, grads: bool = True, dweight: Optional[torch.Tensor] = None,
+                 device="cuda"):
+        super().__init__(device)
+        self.w_dtype = dtype if w_dtype is None else w_dtype
+        for t in (dtype, self.w_dtype):
+            if t not in _CODES:
+                raise TypeError(f"unsupported dtype {t}")
+        self.T, self.V, self.d, self.dtype, self.scale = int(T), int(V), int(d), dtype, float(scale)
+        self.y = torch.empty((self.T, self.d), dtype=dtype, device=self.device)
+        self.dweight = self.workspace = None
+        self.ws_bytes = 0
+        if grads:
+            self.ws_bytes = B.agrl_token_embed_bwd_workspace_size(self.T, self.d, self.V)
+            self.workspace = torch.empty(max(self.ws_bytes, 1), dtype=torch.uint8, device=self.device)
+            if dweight is not None:
+                self._need(dweight, "dweight", (self.V, self.d), (torch.float32,))
+            self.dweight = dweight if dweight is not None else torch.empty(
+                (self.V, self.d), dtype=torch.float32, device=self.device)
+        self._keep(self.y, self.workspace, self.dweight)
+
+    def _check(self, token_id, live_mask):
+        self._need(token_id, "token_id", (self.T,), (torch.int32,))
+        if live_mask is not None:
+            self._need(live_mask, "live_mask", (self.T,), (torch.uint8,))
+
+    def forward(self, weight, token_id, live_mask=None, stream=None):
+        self._need(weight, "weight", (self.V, self.d), (self.w_dtype,))
+        self._check(token_id, live_mask)
+        on = self._order(stream)
+        if on is None:
+            return self._there(self.forward, weight, token_id, live_mask, stream)
+        B.agrl_token_embed_fwd(self.T, self.d, self.V, _CODES[self.w_dtype], _CODES[self.dtype], weight,
+                               token_id, live_mask, self.scale, self.y, self.d, on)
+        return self.y
+
+    def backward(self, token_id, dy, live_mask=None, accumulate: bool = False, stream=None):
+        if self.dweight is None:
+            raise ValueError("agrl: this TokenEmbedding was made with grads=False")
+        self._check(token_id, live_mask)
+        self._need(dy, "dy", (self.T, self.d), _CODES)
+        on = self._order(stream)
+        if on is None:
+            return self._there(self.backward, token_id, dy, live_mask, accumulate, stream)
+        B.agrl_token_embed_bwd(self.T, self.d, self.V, _CODES[dy.dtype], token_id, live_mask, dy,
+                               _row_stride(dy), self.scale, int(accumulate), self.workspace,
+                               self.ws_bytes, self.dweight, on)
+        return self.dweight
+
+
+class TokenRotation(_Owned):
+    """Rotation of [T, n_head, d] heads by their tokens' positions (agrl_rotate_heads): the first ``rot``
+    elements (all by default) in pairs, half a rotated part apart or neighbours (``interleaved``).
+
+    ``__call__`` returns the handle's output, or ``out`` (x itself rotates in place; a view of a fused
+    projection's heads does).  position [T] int32; None: the row's number.  inverse=True turns
+    back: the gradient of the rotation.
+    """
+
+    def __init__(self, T: int, n_head: int, d: int, dtype: torch.dtype, rot: Optional[int] = None,
+                 base: float = 10000.0, interleaved: bool = False, output: bool = True, device="cuda"):
+        super().__init__(device)
+        if dtype not in _CODES:
+            raise TypeError(f"unsupported dtype {dtype}")
+        self.T, self.n_head, self.d, self.dtype = int(T), int(n_head), int(d), dtype
+        self.shape = (self.T, self.n_head, self.d)
+        self.rot, self.base = self.d if rot is None else int(rot), float(base)
+        self.interleaved = int(bool(interleaved))
+        self.out = torch.empty(self.shape, dtype=dtype, device=self.device) if output else None
+        self._keep(self.out)
+
+    def __call__(self, x, position=None, inverse: bool = False, out=None, stream=None):
+        self._need(x, "x", self.shape, (self.dtype,))
+        if position is not None:
+            self._need(position, "position", (self.T,), (torch.int32,))
+        if out is None:
+            if self.out is None:
+                raise ValueError("agrl: this TokenRotation was made with output=False: name out")
+            out = self.out
+        else:
+            self._need(out, "out", self.shape, (self.dtype,))
+        on = self._order(stream)
+        if on is None:
+            return self._there(self, x, position, inverse, out, stream)
+        B.agrl_rotate_heads(self.T, self.n_head, self.d, self.rot, _CODES[self.dtype], x, position,
+                            self.base, self.interleaved, int(bool(inverse)), out, on)
+        return out
+
+
+class PackedAttention(_Owned):
+    """Causal attention within each sequence of a packed stream of T tokens, n_head query heads over n_kv
+    key heads (agrl_attention_*).
+
+    ``forward(q, k, v, seq_start)`` returns (o [T, n_head, d], lse [n_head, T] fp32); ``backward(q, k, v,
+    seq_start, do)`` reads the o and lse of the last forward and returns (dq, dk, dv), three views of
+    ``dqkv`` [T, n_head + 2 n_kv, d], the gradient of a fused projection's output.  seq_start
+    [n_seq + 1] int32: sequence i is the tokens seq_start[i] .. seq_start[i + 1] - 1; tokens outside
+    are not read and get +0.  q, k and v may be views with any strides of rows and heads.
+    scale=None: 1 / sqrt(d).  grads=False leaves the backward out.
+    """
+
+    def __init__(self, T: int, n_head: int, n_kv: int, d: int, dtype: torch.dtype,
+                 scale: Optional[float] = None, grads: bool = True, device="cuda"):
+        super().__init__(device)
+        if dtype not in _CODES:
+            raise TypeError(f"unsupported dtype {dtype}")
+        self.T, self.n_head, self.n_kv, self.d, self.dtype = int(T), int(n_head), int(n_kv), int(d), dtype
+        self.scale = self.d ** -0.5 if scale is None else float(scale)
+        new = lambda *n, dt=torch.float32: torch.empty(n, dtype=dt, device=self.device)  # noqa: E731
+        self.o = new(self.T, self.n_head, self.d, dt=dtype)
+        self.lse = new(self.n_head, self.T)
+        self.dqkv = self.dq = self.dk = self.dv = self.workspace = None
+        self.ws_bytes = 0
+        if grads:
+            self.ws_bytes = B.agrl_attention_bwd_workspace_size(self.T, self.n_head, self.n_kv, self.d,
+                                                                _CODES[dtype])
+            self.workspace = new(max(self.ws_bytes, 1), dt=torch.uint8)
+            self.dqkv = new(self.T, self.n_head + 2 * self.n_kv, self.d, dt=dtype)
+            self.dq, self.dk, self.dv = self.dqkv.split((self.n_head, self.n_kv, self.n_kv), 1)
+        self._keep(self.o, self.lse, self.workspace, self.dqkv)
+
+    def _check(self, q, k, v, seq_start):
+        self._need(q, "q", (self.T, self.n_head, self.d), (self.dtype,))
+        self._need(k, "k", (self.T, self.n_kv, self.d), (self.dtype,))
+        self._need(v, "v", (self.T, self.n_kv, self.d), (self.dtype,))
+        self._need(seq_start, "seq_start", (max(seq_start.numel(), 1),), (torch.int32,))
+
+    def forward(self, q, k, v, seq_start, stream=None):
+        self._check(q, k, v, seq_start)
+        on = self._order(stream)
+        if on is None:
+            return self._there(self.forward, q, k, v, seq_start, stream)
+        B.agrl_attention_fwd(self.T, seq_start.numel() - 1, self.n_head, self.n_kv, self.d,
+                             _CODES[self.dtype], q, k, v, seq_start, self.scale, self.o, self.lse, on)
+        return self.o, self.lse
+
+    def backward(self, q, k, v, seq_start, do, stream=None):
+        if self.dqkv is None:
+            raise ValueError("agrl: this PackedAttention was made with grads=False")
+        self._check(q, k, v, seq_start)
+        self._need(do, "do", (self.T, self.n_head, self.d), (self.dtype,))
+        on = self._order(stream)
+        if on is None:
+            return self._there(self.backward, q, k, v, seq_start, do, stream)
+        B.agrl_attention_bwd(self.T, seq_start.numel() - 1, self.n_head, self.n_kv, self.d,
+                             _CODES[self.dtype], q, k, v, seq_start, self.scale, self.o, self.lse, do,
+                             self.workspace, self.ws_bytes, self.dq, self.dk, self.dv, on)
+        return self.dq, self.dk, self.dv

@@ -1,0 +1,895 @@
+// Causal attention within each sequence of a packed stream, forward and backward (gfx950).
+//
+//   S = scale q k^T over the keys of the row's sequence up to the row itself, P = softmax(S),
+//   o = P v, lse = log sum exp S;  with do given and D = sum do o of each row and head:
+//   P = exp(S - lse), dv = P^T do, dS = P (do v^T - D), dq = scale dS k, dk = scale dS^T q
+//
+// Query head h reads key head h / (n_head / n_kv); dk and dv are the sums over those heads.
+//
+// Tiles are cut from the stream as it lies: a row's keys start at its sequence's first token, so a tile
+// that holds several sequences masks, one that holds a part of one reads a contiguous range of
+// keys, and nothing is padded or planned ahead.
+//
+// Every product is formed with its long side in the rows of a 32 x 32 matrix-core block and the wave's own 32
+// queries (or keys, in the kernel of dk and dv) in the columns, S^T = K Q^T.  A lane then
+// holds 16 values of one column: maximum and sum of a softmax are its own but for one exchange
+// with the other half-wave, and the block of P, converted, is the operand of the next product as it
+// lies (its contraction index may come in any order, so the other operand is read in the order
+// the accumulator has: two transposing LDS reads of four rows each).
+//
+// bf16: v_mfma_f32_32x32x16_bf16, fp32: v_mfma_f32_32x32x2_f32; the same loops on 16-byte fragments.
+#include <math.h>
+
+#include <type_traits>
+
+#include "rows.hpp"
+
+namespace agrl {
+namespace {
+
+typedef __bf16 bf16x4 __attribute__((ext_vector_type(4)));
+typedef __attribute__((address_space(3))) bf16x4 lds_bf16x4;
+typedef uint16_t u16x2 __attribute__((ext_vector_type(2)));
+
+constexpr float LOG2E = 1.44269504088896341f, LN2 = 0.693147180559945309f;
+
+// [T, n_head, d]: rows `ld`, heads `hs` elements apart
+struct Heads {
+  const void* p;
+  int64_t ld, hs;
+};
+struct HeadsOut {
+  void* p;
+  int64_t ld, hs;
+};
+
+template <typename T>
+struct Mma;
+template <>
+struct Mma<uint16_t> {
+  static constexpr int E = 8;        // elements of a 16-byte fragment
+  static constexpr int K = 16;       // contraction of a fragment pair
+  static __device__ __forceinline__ f32x16 mma(u32x4 a, u32x4 b, f32x16 c) {
+    return __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, a),
+                                                   __builtin_bit_cast(bf16x8, b), c, 0, 0, 0);
+  }
+  static __device__ __forceinline__ uint32_t pack(float lo, float hi) {
+    return __builtin_bit_cast(uint32_t, __builtin_convertvector(f32x2{lo, hi}, bf16x2));
+  }
+  // accumulator rows 8 s .. 8 s + 7 as a fragment
+  static __device__ __forceinline__ u32x4 frag(const f32x16& c, int s) {
+    return u32x4{pack(c[8 * s], c[8 * s + 1]), pack(c[8 * s + 2], c[8 * s + 3]),
+                 pack(c[8 * s + 4], c[8 * s + 5]), pack(c[8 * s + 6], c[8 * s + 7])};
+  }
+  // largest magnitude bits: at least LIMIT if an element is infinite or NaN
+  static __device__ __forceinline__ uint32_t magnitude(uint32_t m, u32x4 f) {
+#pragma unroll
+    for (int k = 0; k < 4; ++k)
+      m = __builtin_bit_cast(uint32_t, __builtin_elementwise_max(__builtin_bit_cast(u16x2, m),
+                                                                 __builtin_bit_cast(u16x2, f[k] & 0x7fff7fffu)));
+    return m;
+  }
+  static __device__ __forceinline__ bool odd(uint32_t m) {
+    return (m & 0xffffu) >= 0x7f80u || m >= 0x7f800000u;
+  }
+  // the fragment with 0 for infinite and NaN elements, and 1 there and 0 elsewhere
+  static __device__ __forceinline__ void split(u32x4 f, u32x4& sane, u32x4& ind) {
+#pragma unroll
+    for (int k = 0; k < 4; ++k) {
+      const uint32_t lo = (f[k] & 0x7f80u) == 0x7f80u ? 0xffffu : 0u;
+      const uint32_t hi = (f[k] & 0x7f800000u) == 0x7f800000u ? 0xffff0000u : 0u;
+      sane[k] = f[k] & ~(lo | hi);
+      ind[k] = (lo | hi) & 0x3f803f80u;
+    }
+  }
+};
+template <>
+struct Mma<float> {
+  static constexpr int E = 4;
+  static constexpr int K = 8;
+  static __device__ __forceinline__ f32x16 mma(u32x4 a, u32x4 b, f32x16 c) {
+#pragma unroll
+    for (int j = 0; j < 4; ++j)
+      c = __builtin_amdgcn_mfma_f32_32x32x2f32(__uint_as_float(a[j]), __uint_as_float(b[j]), c, 0, 0, 0);
+    return c;
+  }
+  static __device__ __forceinline__ u32x4 frag(const f32x16& c, int s) {
+    return u32x4{__float_as_uint(c[4 * s]), __float_as_uint(c[4 * s + 1]), __float_as_uint(c[4 * s + 2]),
+                 __float_as_uint(c[4 * s + 3])};
+  }
+  static __device__ __forceinline__ uint32_t magnitude(uint32_t m, u32x4 f) {
+#pragma unroll
+    for (int k = 0; k < 4; ++k) m = max(m, f[k] & 0x7fffffffu);
+    return m;
+  }
+  static __device__ __forceinline__ bool odd(uint32_t m) { return m >= 0x7f800000u; }
+  static __device__ __forceinline__ void split(u32x4 f, u32x4& sane, u32x4& ind) {
+#pragma unroll
+    for (int k = 0; k < 4; ++k) {
+      const bool bad = (f[k] & 0x7f800000u) == 0x7f800000u;
+      sane[k] = bad ? 0u : f[k];
+      ind[k] = bad ? 0x3f800000u : 0u;
+    }
+  }
+};
+
+// A tile of rows of DP elements in LDS.  16-byte chunk c of row r sits at c ^ sw(r): the 16 rows that a
+// pass of row-wise fragment reads touches lie in 16 distinct bank groups, and so do the four
+// rows of a transposing read (its 64-byte windows).
+template <typename T, int DP>
+struct Tile {
+  using M = Mma<T>;
+  static constexpr int ROW = DP * (int)sizeof(T);    // bytes
+  static constexpr int CPR = ROW / 16;               // chunks of a row
+  static constexpr int NS = DP / M::K;               // fragments along a row
+  static constexpr int ND = DP / 32;                 // 32-column blocks
+  static constexpr int NP = 32 / M::K;               // fragments along 32 rows
+
+  static __device__ __forceinline__ int sw(int r) {
+    return CPR == 8 ? ((r >> 1) & 1) << 2 | ((r >> 2) & 3) : (r & 3) << 2 | ((r >> 2) & 3);
+  }
+
+  // Lane's byte offsets of its row-wise and transposing reads (the rest is XORs and immediates)
+  struct Lane {
+    int row, tr;
+    __device__ __forceinline__ Lane() {
+      const int l = threadIdx.x & 63, r = l & 31, h = l >> 5;
+      row = r * ROW + ((sw(r) ^ h) << 4);
+      if constexpr (sizeof(T) == 2) {
+        // 16-lane group g: columns 16 (g & 1) .., rows 4 h ..; lane s of it points at row s >> 2, columns 4 (s & 3)
+        const int s = l & 15, q = s >> 2, k = 4 * h + q, c = ((l >> 4) & 1) * 2 + ((s & 3) >> 1);
+        tr = k * ROW + ((c ^ sw(k)) << 4) + (s & 1) * 8;
+      } else {
+        tr = 4 * h * ROW + (((r >> 2) ^ sw(4 * h)) << 4) + (r & 3) * 4;
+      }
+    }
+  };
+  // row operand: rows 32 b .., fragment s
+  static __device__ __forceinline__ u32x4 rows(const uint8_t* p, const Lane& L, int b, int s) {
+    return *(const u32x4*)(p + b * 32 * ROW + (L.row ^ (s << 5)));
+  }
+  // transposed operand: columns 32 c .. of the tile are the rows, fragment s of the rows 32 b ..
+  static __device__ __forceinline__ u32x4 cols(const uint8_t* p, const Lane& L, int b, int s, int c) {
+    if constexpr (sizeof(T) == 2) {
+      const uint8_t* q = p + (b * 32 + s * 16) * ROW;
+      const bf16x4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4bf16((lds_bf16x4*)(q + (L.tr ^ (c << 6))));
+      const bf16x4 hi =
+          __builtin_amdgcn_ds_read_tr16_b64_v4bf16((lds_bf16x4*)(q + 8 * ROW + (L.tr ^ (c << 6) ^ 32)));
+      const u32x2 a = __builtin_bit_cast(u32x2, lo), d = __builtin_bit_cast(u32x2, hi);
+      return u32x4{a.x, a.y, d.x, d.y};
+    } else {
+      u32x4 v;
+#pragma unroll
+      for (int j = 0; j < 4; ++j)
+        v[j] = *(const uint32_t*)(p + (b * 32 + s * 8 + j) * ROW +
+                                  (L.tr ^ (j << 6) ^ ((s & 1) << 5) ^ (c << 7)));
+      return v;
+    }
+  }
+};
+
+// R rows of a head, from global memory through registers into LDS by NT lanes.  Rows from `end` on are 0.
+template <typename T, int DP, int R, int NT, bool FULL>
+struct Stage {
+  using TL = Tile<T, DP>;
+  static constexpr int N = R * TL::CPR / NT, STEP = NT / TL::CPR;
+  static_assert(N >= 1 && NT % TL::CPR == 0, "whole chunks a lane");
+  u32x4 v[N];
+  __device__ __forceinline__ void load(const T* base, int64_t ld, int row0, int end, int d) {
+    const int r0 = threadIdx.x / TL::CPR, col = (threadIdx.x & (TL::CPR - 1)) * TL::M::E;
+    const T* p = base + (int64_t)(row0 + r0) * ld + col;
+#pragma unroll
+    for (int i = 0; i < N; ++i, p += STEP * ld) {
+      v[i] = u32x4{0, 0, 0, 0};
+      if (row0 + r0 + i * STEP < end) v[i] = chunk(p, d - col);
+    }
+  }
+  static __device__ __forceinline__ u32x4 chunk(const T* p, int n) {
+    if (FULL || n >= TL::M::E) return sizeof(T) == 2 ? (u32x4) * (const u32x4_a2*)p : (u32x4) * (const u32x4_a4*)p;
+    u32x4 w = {0, 0, 0, 0};
+#pragma unroll
+    for (int k = 0; k < TL::M::E - 1; ++k)
+      if (k < n) {
+        if constexpr (sizeof(T) == 2)
+          w[k >> 1] |= (uint32_t)p[k] << (16 * (k & 1));
+        else
+          w[k] = __float_as_uint(p[k]);
+      }
+    return w;
+  }
+  __device__ __forceinline__ void store(uint8_t* lds) const {
+    const int r0 = threadIdx.x / TL::CPR, c = threadIdx.x & (TL::CPR - 1);
+#pragma unroll
+    for (int i = 0; i < N; ++i) {
+      const int r = r0 + i * STEP;
+      *(u32x4*)(lds + r * TL::ROW + ((c ^ TL::sw(r)) << 4)) = v[i];
+    }
+  }
+};
+
+// A column operand held in registers: 32 rows of a head, lane's row r, as fragments
+template <typename T, int DP, bool FULL, int NS>
+__device__ __forceinline__ void hold(u32x4 (&f)[NS], const T* row, bool live, int d) {
+  using M = Mma<T>;
+  static_assert(NS == Tile<T, DP>::NS, "a whole row");
+  const int h = (threadIdx.x & 63) >> 5;
+#pragma unroll
+  for (int s = 0; s < NS; ++s) {
+    f[s] = u32x4{0, 0, 0, 0};
+    if (live) f[s] = Stage<T, DP, 32, 64, FULL>::chunk(row + (2 * s + h) * M::E, d - (2 * s + h) * M::E);
+  }
+}
+
+// ------------------------------------------------------------------ sequences
+// The number of offsets that are at most n, by one wave: 64 probes a step
+__device__ __forceinline__ int offsets_upto(const int32_t* start, int n_seq, int n) {
+  const int lane = threadIdx.x & 63;
+  int lo = 0, hi = n_seq + 1;
+  while (hi - lo > 64) {
+    const int step = (hi - lo + 63) >> 6, i = lo + (lane + 1) * step - 1;
+    const int c = __popcll(__ballot(i < hi && start[min(i, hi - 1)] <= n));
+    lo += c * step;
+    hi = min(hi, lo + step);
+  }
+  const int i = lo + lane;
+  return lo + __popcll(__ballot(i < hi && start[min(i, n_seq)] <= n));
+}
+
+// A lane's token n and its sequence [begin, end); live: there is one
+struct Place {
+  int begin, end;
+  bool live;
+  // first, last: the wave's tokens' range (all lanes); n within it
+  __device__ __forceinline__ Place(const int32_t* start, int n_seq, int T, int first, int last, int n) {
+    int lo = offsets_upto(start, n_seq, first), hi = offsets_upto(start, n_seq, last);
+    while (lo < hi) {
+      const int mid = (lo + hi) >> 1;
+      if (start[mid] <= n)
+        lo = mid + 1;
+      else
+        hi = mid;
+    }
+    live = n < T && lo >= 1 && lo <= n_seq;
+    begin = end = n;
+    if (live) {
+      begin = min(max(start[lo - 1], 0), n);     // (offsets out of order stay within the stream)
+      end = min(max(start[lo], n + 1), T);
+    }
+  }
+};
+
+__device__ __forceinline__ int wave_min(int v) {
+#pragma unroll
+  for (int o = 32; o; o >>= 1) v = min(v, __shfl_xor(v, o));
+  return __builtin_amdgcn_readfirstlane(v);
+}
+__device__ __forceinline__ int wave_max(int v) { return -wave_min(-v); }
+
+// Offsets that decrease or leave [0, T] set the error word's bit; the grid's workgroups share them.
+__device__ __forceinline__ void check_offsets(const int32_t* start, int n_seq, int T, int* err) {
+  for (int64_t i = (int64_t)blockIdx.x * blockDim.x + threadIdx.x; i <= n_seq;
+       i += (int64_t)gridDim.x * blockDim.x) {
+    const int s = start[i];
+    if (s < 0 || s > T || (i > 0 && start[i - 1] > s)) set_error(err, ERR_SEQ_START);
+  }
+}
+
+// ------------------------------------------------------------------ products
+// acc += X^T p over the tile's 32 rows of block b; `ok`: which of the lane's 16 rows count.  In masked blocks
+// p is 0 where a row does not count, but 0 times an infinite or NaN element of X is not: there such
+// elements are taken out, and a second product with ones in their places finds who did count them.
+template <typename T, int DP, bool MASKED, int ND, int NP>
+__device__ __forceinline__ void add_cols(f32x16 (&acc)[ND], const uint8_t* x,
+                                         const typename Tile<T, DP>::Lane& L, int b, const u32x4 (&p)[NP],
+                                         uint32_t ok) {
+  using TL = Tile<T, DP>;
+  using M = Mma<T>;
+  if constexpr (MASKED) {
+    uint32_t m = 0;
+#pragma unroll
+    for (int c = 0; c < TL::ND; ++c)
+#pragma unroll
+      for (int s = 0; s < TL::NP; ++s) m = M::magnitude(m, TL::cols(x, L, b, s, c));
+    if (__any(M::odd(m))) {
+      f32x16 counts;
+#pragma unroll
+      for (int r = 0; r < 16; ++r) counts[r] = ok >> r & 1 ? 1.0f : 0.0f;
+#pragma unroll
+      for (int c = 0; c < TL::ND; ++c) {
+        f32x16 hit = {};
+#pragma unroll
+        for (int s = 0; s < TL::NP; ++s) {
+          u32x4 sane, ind;
+          M::split(TL::cols(x, L, b, s, c), sane, ind);
+          acc[c] = M::mma(sane, p[s], acc[c]);
+          hit = M::mma(ind, M::frag(counts, s), hit);
+        }
+#pragma unroll
+        for (int r = 0; r < 16; ++r) acc[c][r] = hit[r] > 0.0f ? NAN : acc[c][r];
+      }
+      return;
+    }
+  }
+#pragma unroll
+  for (int c = 0; c < TL::ND; ++c)
+#pragma unroll
+    for (int s = 0; s < TL::NP; ++s) acc[c] = M::mma(TL::cols(x, L, b, s, c), p[s], acc[c]);
+}
+
+// acc = X f over the tile's 32 rows of block b
+template <typename T, int DP, int NS>
+__device__ __forceinline__ f32x16 mul_rows(const uint8_t* x, const typename Tile<T, DP>::Lane& L, int b,
+                                           const u32x4 (&f)[NS]) {
+  f32x16 acc = {};
+#pragma unroll
+  for (int s = 0; s < NS; ++s) acc = Mma<T>::mma(Tile<T, DP>::rows(x, L, b, s), f[s], acc);
+  return acc;
+}
+
+// row of accumulator element r within its block
+__device__ __forceinline__ int acc_row(int r) { return 8 * (r >> 2) + (r & 3) + 4 * ((threadIdx.x & 63) >> 5); }
+
+__device__ __forceinline__ float other_half(float v) {
+  const auto r = __builtin_amdgcn_permlane32_swap(__float_as_uint(v), __float_as_uint(v), false, false);
+  return __uint_as_float(threadIdx.x & 32 ? r[0] : r[1]);
+}
+
+// The column's DP values times f to a row of the output, eight (fp32: four) adjacent ones a lane
+template <typename T, int DP, bool FULL, int ND>
+__device__ __forceinline__ void put_row(T* row, const f32x16 (&acc)[ND], float f, bool zero, bool live, int d) {
+  const int h = (threadIdx.x & 63) >> 5;
+#pragma unroll
+  for (int c = 0; c < ND; ++c) {
+    if constexpr (sizeof(T) == 2) {
+#pragma unroll
+      for (int g = 0; g < 4; g += 2) {
+        uint32_t w[4];
+#pragma unroll
+        for (int k = 0; k < 4; ++k)
+          w[k] = zero ? 0u : Mma<T>::pack(acc[c][4 * g + 2 * k] * f, acc[c][4 * g + 2 * k + 1] * f);
+        const auto a = __builtin_amdgcn_permlane32_swap(w[0], w[2], false, false);
+        const auto b = __builtin_amdgcn_permlane32_swap(w[1], w[3], false, false);
+        const u32x4 v = {a[0], b[0], a[1], b[1]};
+        const int col = 32 * c + 8 * (g + h);
+        if (!live) continue;
+        if (FULL || col + 8 <= d) {
+          *(u32x4_a2*)(row + col) = v;
+        } else {
+#pragma unroll
+          for (int k = 0; k < 7; ++k)
+            if (col + k < d) row[col + k] = (T)(v[k >> 1] >> (16 * (k & 1)));
+        }
+      }
+    } else {
+#pragma unroll
+      for (int g = 0; g < 4; ++g) {
+        f32x4 v;
+#pragma unroll
+        for (int k = 0; k < 4; ++k) v[k] = zero ? 0.0f : acc[c][4 * g + k] * f;
+        const int col = 32 * c + 8 * g + 4 * h;
+        typedef f32x4 f32x4_a4 __attribute__((aligned(4)));
+        if (!live) continue;
+        if (FULL || col + 4 <= d) {
+          *(f32x4_a4*)(row + col) = v;
+        } else {
+#pragma unroll
+          for (int k = 0; k < 3; ++k)
+            if (col + k < d) row[col + k] = v[k];
+        }
+      }
+    }
+  }
+}
+
+// ------------------------------------------------------------------ forward
+constexpr int WAVES = 4, THREADS = 64 * WAVES, BM = 32 * WAVES;   // own rows of a workgroup
+template <typename T>
+constexpr int BN = sizeof(T) == 2 ? 64 : 32;                      // rows of a tile that goes through LDS
+
+struct AttArgs {
+  int32_t T, n_seq, n_head, n_kv, rep, d;
+  Heads q, k, v;
+  const int32_t* start;
+  float scale;
+  HeadsOut o;
+  float* lse;
+  int* err;
+  // backward
+  Heads dout;
+  const float *lse2, *delta;     // [n_head, T]: lse in powers of 2, sum do o
+  HeadsOut dq, dk, dv;
+};
+
+// What a wave's 32 columns need: its range of the other side
+struct Span {
+  int lo, hi;              // [lo, hi): rows that some column counts
+  int full_lo, full_hi;    // [full_lo, full_hi): rows that every column counts
+};
+// the workgroup's range
+__device__ __forceinline__ void join(const Span& s, int (&lds)[2][WAVES], int& lo, int& hi) {
+  const int wave = threadIdx.x >> 6;
+  if ((threadIdx.x & 63) == 0) {
+    lds[0][wave] = s.lo;
+    lds[1][wave] = s.hi;
+  }
+  __syncthreads();
+  lo = 0x7fffffff;
+  hi = 0;
+#pragma unroll
+  for (int w = 0; w < WAVES; ++w) {
+    lo = min(lo, lds[0][w]);
+    hi = max(hi, lds[1][w]);
+  }
+  lo = __builtin_amdgcn_readfirstlane(lo);
+  hi = __builtin_amdgcn_readfirstlane(hi);
+}
+
+// Queries in the columns: a row of the stream counts the keys begin .. itself
+__device__ __forceinline__ Span query_span(const Place& at, int n) {
+  const int lo = wave_min(at.live ? at.begin : 0x7fffffff), last = wave_max(at.live ? n : -1);
+  const bool all = __all(at.live);
+  const int full_lo = wave_max(at.begin), full_hi = wave_min(n) + 1;
+  return Span{lo, last + 1, full_lo, all ? full_hi : 0};
+}
+
+template <typename T, int DP, bool FULL>
+__global__ void __launch_bounds__(THREADS, sizeof(T) == 2 ? 2 : 1) att_fwd_kernel(AttArgs a) {
+  using TL = Tile<T, DP>;
+  using M = Mma<T>;
+  constexpr int R = BN<T>, NB = R / 32;
+  __shared__ __align__(16) uint8_t lds_k[2][R * TL::ROW], lds_v[2][R * TL::ROW];
+  __shared__ int lds_span[2][WAVES];
+  if (a.err) check_offsets(a.start, a.n_seq, a.T, a.err);
+  // the longest ranges first; a key head's query heads on one XCD (8 in turn) as far as the numbers allow
+  const int tiles = (a.T + BM - 1) / BM;
+  const int tile = tiles - 1 - blockIdx.x / a.n_head, j = blockIdx.x % a.n_head;
+  const int kv = j % a.n_kv, head = kv * a.rep + j / a.n_kv;
+  const int wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6), lane = threadIdx.x & 63;
+  const int first = tile * BM + wave * 32, n = first + (lane & 31);
+  const Place at(a.start, a.n_seq, a.T, first, first + 31, n);
+  const Span span = query_span(at, n);
+  const uint32_t len = at.live ? n - at.begin + 1 : 0;
+  int lo, hi;
+  join(span, lds_span, lo, hi);
+
+  const typename TL::Lane L;
+  u32x4 q[TL::NS];
+  hold<T, DP, FULL>(q, (const T*)a.q.p + head * a.q.hs + (int64_t)n * a.q.ld, at.live, a.d);
+  const T* kp = (const T*)a.k.p + kv * a.k.hs;
+  const T* vp = (const T*)a.v.p + kv * a.v.hs;
+  const float sl2 = a.scale * LOG2E;
+  f32x16 o[TL::ND] = {};
+  float m = -INFINITY, l = 0.0f;
+  Stage<T, DP, R, THREADS, FULL> sk, sv;
+  const int kt0 = lo / R * R;
+  if (lo < hi) {
+    sk.load(kp, a.k.ld, kt0, a.T, a.d);
+    sv.load(vp, a.v.ld, kt0, a.T, a.d);
+    sk.store(lds_k[0]);
+    sv.store(lds_v[0]);
+  }
+  __syncthreads();
+  int buf = 0;
+  for (int k0 = kt0; k0 < hi; k0 += R, buf ^= 1) {
+    const bool more = k0 + R < hi;
+    if (more) {
+      sk.load(kp, a.k.ld, k0 + R, a.T, a.d);
+      sv.load(vp, a.v.ld, k0 + R, a.T, a.d);
+    }
+    auto step = [&](auto masked_c) {
+      constexpr bool MASKED = decltype(masked_c)::value;
+      f32x16 s[NB];
+      uint32_t ok[NB];
+      float top = -INFINITY;
+#pragma unroll
+      for (int b = 0; b < NB; ++b) {
+        s[b] = mul_rows<T, DP>(lds_k[buf], L, b, q);
+        ok[b] = 0;
+        if constexpr (MASKED) {
+#pragma unroll
+          for (int r = 0; r < 16; ++r) {
+            const bool in = (uint32_t)(k0 + 32 * b + acc_row(r) - at.begin) < len;
+            ok[b] |= in ? 1u << r : 0u;
+            s[b][r] = in ? s[b][r] : -INFINITY;
+          }
+        }
+#pragma unroll
+        for (int r = 0; r < 16; ++r) top = fmaxf(top, s[b][r]);
+      }
+      top = fmaxf(top, other_half(top)) * sl2;
+      // a column's reference moves only when the maximum has left it 2^8 behind: any reference gives the same
+      // quotient (and a column's own, so no other row's values change its roundings)
+      const bool far = top > m + 8.0f;
+      if (__any(far)) {
+        const float to = far ? top : m;
+        const float f = far ? __builtin_amdgcn_exp2f(m - to) : 1.0f;
+        l *= f;
+#pragma unroll
+        for (int c = 0; c < TL::ND; ++c) o[c] *= f;
+        m = to;
+      }
+      const float ref = m == -INFINITY ? 0.0f : m;
+#pragma unroll
+      for (int b = 0; b < NB; ++b) {
+        u32x4 p[TL::NP];
+#pragma unroll
+        for (int r = 0; r < 16; ++r) {
+          s[b][r] = __builtin_amdgcn_exp2f(fmaf(s[b][r], sl2, -ref));
+          l += s[b][r];
+        }
+#pragma unroll
+        for (int i = 0; i < TL::NP; ++i) p[i] = M::frag(s[b], i);
+        add_cols<T, DP, MASKED>(o, lds_v[buf], L, b, p, ok[b]);
+      }
+    };
+    if (k0 + R > span.lo && k0 < span.hi) {
+      if (k0 >= span.full_lo && k0 + R <= span.full_hi)
+        step(std::false_type{});
+      else
+        step(std::true_type{});
+    }
+    if (more) {
+      sk.store(lds_k[buf ^ 1]);
+      sv.store(lds_v[buf ^ 1]);
+    }
+    __syncthreads();
+  }
+  l += other_half(l);
+  if (a.lse && n < a.T && lane < 32)
+    a.lse[(int64_t)head * a.T + n] = at.live ? LN2 * (m + __builtin_amdgcn_logf(l)) : 0.0f;
+  put_row<T, DP, FULL>((T*)a.o.p + head * a.o.hs + (int64_t)n * a.o.ld, o, 1.0f / l, !at.live, n < a.T, a.d);
+}
+
+// ------------------------------------------------------------------ backward
+// lse in powers of 2 and D = sum do o, [n_head, T].  A wave takes a token's heads in turn, 16 lanes a head.
+struct DeltaArgs {
+  int32_t T, n_head, d;
+  Heads o, dout;
+  const float* lse;
+  float *lse2, *delta;
+};
+template <typename T>
+__global__ void __launch_bounds__(256) att_delta_kernel(DeltaArgs a) {
+  const int l = threadIdx.x & 15, team = threadIdx.x >> 4;
+  for (int64_t i = (int64_t)blockIdx.x * 16 + team; i < (int64_t)a.T * a.n_head; i += (int64_t)gridDim.x * 16) {
+    const int n = (int)(i / a.n_head), h = (int)(i - (int64_t)n * a.n_head);
+    const T* o = (const T*)a.o.p + (int64_t)n * a.o.ld + h * a.o.hs;
+    const T* g = (const T*)a.dout.p + (int64_t)n * a.dout.ld + h * a.dout.hs;
+    float sum = 0.0f;
+    for (int c = l * CH; c < a.d; c += 16 * CH) {
+      Chunk<T> x, y;
+      if (c + CH <= a.d) {
+        x.load(o + c);
+        y.load(g + c);
+      } else {
+        x.load_some(o + c, a.d - c);
+        y.load_some(g + c, a.d - c);
+      }
+#pragma unroll
+      for (int k = 0; k < CH; ++k) sum = fmaf(x.get(k), y.get(k), sum);
+    }
+    sum = dpp_add<0xb1>(sum);
+    sum = dpp_add<0x4e>(sum);
+    sum = dpp_add<0x141>(sum);
+    sum = dpp_add<0x140>(sum);
+    if (l == 0) {
+      a.delta[(int64_t)h * a.T + n] = sum;
+      a.lse2[(int64_t)h * a.T + n] = a.lse[(int64_t)h * a.T + n] * LOG2E;
+    }
+  }
+}
+
+// dq: queries in the columns as in the forward; dS^T is the operand that meets K^T.
+template <typename T, int DP, bool FULL>
+__global__ void __launch_bounds__(THREADS, sizeof(T) == 2 ? 2 : 1) att_dq_kernel(AttArgs a) {
+  using TL = Tile<T, DP>;
+  using M = Mma<T>;
+  constexpr int R = BN<T>, NB = R / 32;
+  __shared__ __align__(16) uint8_t lds_k[2][R * TL::ROW], lds_v[2][R * TL::ROW];
+  __shared__ int lds_span[2][WAVES];
+  if (a.err) check_offsets(a.start, a.n_seq, a.T, a.err);
+  const int tiles = (a.T + BM - 1) / BM;
+  const int tile = tiles - 1 - blockIdx.x / a.n_head, j = blockIdx.x % a.n_head;
+  const int kv = j % a.n_kv, head = kv * a.rep + j / a.n_kv;
+  const int wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6), lane = threadIdx.x & 63;
+  const int first = tile * BM + wave * 32, n = first + (lane & 31);
+  const Place at(a.start, a.n_seq, a.T, first, first + 31, n);
+  const Span span = query_span(at, n);
+  const uint32_t len = at.live ? n - at.begin + 1 : 0;
+  int lo, hi;
+  join(span, lds_span, lo, hi);
+
+  const typename TL::Lane L;
+  u32x4 q[TL::NS], g[TL::NS];
+  hold<T, DP, FULL>(q, (const T*)a.q.p + head * a.q.hs + (int64_t)n * a.q.ld, at.live, a.d);
+  hold<T, DP, FULL>(g, (const T*)a.dout.p + head * a.dout.hs + (int64_t)n * a.dout.ld, at.live, a.d);
+  const float lse2 = at.live ? a.lse2[(int64_t)head * a.T + n] : 0.0f;
+  const float delta = at.live ? a.delta[(int64_t)head * a.T + n] : 0.0f;
+  const T* kp = (const T*)a.k.p + kv * a.k.hs;
+  const T* vp = (const T*)a.v.p + kv * a.v.hs;
+  const float sl2 = a.scale * LOG2E;
+  f32x16 dq[TL::ND] = {};
+  Stage<T, DP, R, THREADS, FULL> sk, sv;
+  const int kt0 = lo / R * R;
+  if (lo < hi) {
+    sk.load(kp, a.k.ld, kt0, a.T, a.d);
+    sv.load(vp, a.v.ld, kt0, a.T, a.d);
+    sk.store(lds_k[0]);
+    sv.store(lds_v[0]);
+  }
+  __syncthreads();
+  int buf = 0;
+  for (int k0 = kt0; k0 < hi; k0 += R, buf ^= 1) {
+    const bool more = k0 + R < hi;
+    if (more) {
+      sk.load(kp, a.k.ld, k0 + R, a.T, a.d);
+      sv.load(vp, a.v.ld, k0 + R, a.T, a.d);
+    }
+    auto step = [&](auto masked_c) {
+      constexpr bool MASKED = decltype(masked_c)::value;
+#pragma unroll
+      for (int b = 0; b < NB; ++b) {
+        f32x16 s = mul_rows<T, DP>(lds_k[buf], L, b, q);
+        const f32x16 dp = mul_rows<T, DP>(lds_v[buf], L, b, g);
+        uint32_t ok = 0;
+#pragma unroll
+        for (int r = 0; r < 16; ++r) {
+          s[r] = __builtin_amdgcn_exp2f(fmaf(s[r], sl2, -lse2)) * (dp[r] - delta);
+          if constexpr (MASKED) {
+            const bool in = (uint32_t)(k0 + 32 * b + acc_row(r) - at.begin) < len;
+            ok |= in ? 1u << r : 0u;
+            s[r] = in && len > 1 ? s[r] : 0.0f;      // (a row's only key: P is 1 whatever the scores are)
+          }
+        }
+        u32x4 p[TL::NP];
+#pragma unroll
+        for (int i = 0; i < TL::NP; ++i) p[i] = M::frag(s, i);
+        add_cols<T, DP, MASKED>(dq, lds_k[buf], L, b, p, ok);
+      }
+    };
+    if (k0 + R > span.lo && k0 < span.hi) {
+      if (k0 >= span.full_lo && k0 + R <= span.full_hi)
+        step(std::false_type{});
+      else
+        step(std::true_type{});
+    }
+    if (more) {
+      sk.store(lds_k[buf ^ 1]);
+      sv.store(lds_v[buf ^ 1]);
+    }
+    __syncthreads();
+  }
+  put_row<T, DP, FULL>((T*)a.dq.p + head * a.dq.hs + (int64_t)n * a.dq.ld, dq, a.scale, !at.live, n < a.T, a.d);
+}
+
+// dk and dv: keys in the columns, the rows of Q and do go through LDS, head after head of the group.
+template <typename T, int DP, bool FULL>
+__global__ void __launch_bounds__(THREADS, 1) att_dkv_kernel(AttArgs a) {
+  using TL = Tile<T, DP>;
+  using M = Mma<T>;
+  constexpr int R = BN<T>, NB = R / 32;
+  __shared__ __align__(16) uint8_t lds_q[2][R * TL::ROW], lds_g[2][R * TL::ROW];
+  __shared__ __align__(16) float lds_s[2][2][R];     // lse and D of the tile's rows
+  __shared__ int lds_span[2][WAVES];
+  const int tile = blockIdx.x / a.n_kv, kv = blockIdx.x % a.n_kv;
+  const int wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6), lane = threadIdx.x & 63;
+  const int first = tile * BM + wave * 32, n = first + (lane & 31);
+  const Place at(a.start, a.n_seq, a.T, first, first + 31, n);
+  // a key is counted by the rows from itself to its sequence's end
+  const Span span = {wave_min(at.live ? n : 0x7fffffff), wave_max(at.live ? at.end : 0),
+                     wave_max(n), __all(at.live) ? wave_min(at.end) : 0};
+  const uint32_t len = at.live ? at.end - n : 0;
+  const bool head_of = at.live && at.begin == n;     // the sequence's first token
+  int lo, hi;
+  join(span, lds_span, lo, hi);
+
+  const typename TL::Lane L;
+  u32x4 k[TL::NS], v[TL::NS];
+  hold<T, DP, FULL>(k, (const T*)a.k.p + kv * a.k.hs + (int64_t)n * a.k.ld, at.live, a.d);
+  hold<T, DP, FULL>(v, (const T*)a.v.p + kv * a.v.hs + (int64_t)n * a.v.ld, at.live, a.d);
+  const float sl2 = a.scale * LOG2E;
+  f32x16 dk[TL::ND] = {}, dv[TL::ND] = {};
+  Stage<T, DP, R, THREADS, FULL> sq, sg;
+  float stat = 0.0f;
+  const int t0 = lo / R * R, per = lo < hi ? (hi - t0 + R - 1) / R : 0, steps = per * a.rep;
+  auto load = [&](int i) {
+    const int head = kv * a.rep + i / per, q0 = t0 + (i - i / per * per) * R;
+    sq.load((const T*)a.q.p + head * a.q.hs, a.q.ld, q0, a.T, a.d);
+    sg.load((const T*)a.dout.p + head * a.dout.hs, a.dout.ld, q0, a.T, a.d);
+    const int r = q0 + (threadIdx.x & (R - 1));
+    if (threadIdx.x < 2 * R && r < a.T)
+      stat = (threadIdx.x < R ? a.lse2 : a.delta)[(int64_t)head * a.T + r];
+  };
+  auto store = [&](int buf) {
+    sq.store(lds_q[buf]);
+    sg.store(lds_g[buf]);
+    if (threadIdx.x < 2 * R) lds_s[buf][threadIdx.x / R][threadIdx.x & (R - 1)] = stat;
+  };
+  if (steps > 0) {
+    load(0);
+    store(0);
+  }
+  __syncthreads();
+  int buf = 0;
+  for (int i = 0; i < steps; ++i, buf ^= 1) {
+    const int q0 = t0 + (i % per) * R;
+    if (i + 1 < steps) load(i + 1);
+    auto step = [&](auto masked_c) {
+      constexpr bool MASKED = decltype(masked_c)::value;
+#pragma unroll
+      for (int b = 0; b < NB; ++b) {
+        f32x16 s = mul_rows<T, DP>(lds_q[buf], L, b, k);
+        f32x16 ds = mul_rows<T, DP>(lds_g[buf], L, b, v);
+        uint32_t ok = 0;
+#pragma unroll
+        for (int g = 0; g < 4; ++g) {
+          const f32x4 z = *(const f32x4*)&lds_s[buf][0][32 * b + acc_row(4 * g)];
+          const f32x4 del = *(const f32x4*)&lds_s[buf][1][32 * b + acc_row(4 * g)];
+#pragma unroll
+          for (int e = 0; e < 4; ++e) {
+            const int r = 4 * g + e;
+            s[r] = __builtin_amdgcn_exp2f(fmaf(s[r], sl2, -z[e]));
+            ds[r] = s[r] * (ds[r] - del[e]);
+            if constexpr (MASKED) {
+              const uint32_t after = q0 + 32 * b + acc_row(r) - n;
+              const bool in = after < len;
+              ok |= in ? 1u << r : 0u;
+              s[r] = in ? s[r] : 0.0f;
+              ds[r] = in && !(head_of && after == 0) ? ds[r] : 0.0f;   // (the first row's only key)
+            }
+          }
+        }
+        u32x4 p[TL::NP], dp[TL::NP];
+#pragma unroll
+        for (int i2 = 0; i2 < TL::NP; ++i2) {
+          p[i2] = M::frag(s, i2);
+          dp[i2] = M::frag(ds, i2);
+        }
+        add_cols<T, DP, MASKED>(dv, lds_g[buf], L, b, p, ok);
+        add_cols<T, DP, MASKED>(dk, lds_q[buf], L, b, dp, ok);
+      }
+    };
+    if (q0 + R > span.lo && q0 < span.hi) {
+      if (q0 >= span.full_lo && q0 + R <= span.full_hi)
+        step(std::false_type{});
+      else
+        step(std::true_type{});
+    }
+    if (i + 1 < steps) store(buf ^ 1);
+    __syncthreads();
+  }
+  put_row<T, DP, FULL>((T*)a.dk.p + kv * a.dk.hs + (int64_t)n * a.dk.ld, dk, a.scale, !at.live, n < a.T, a.d);
+  put_row<T, DP, FULL>((T*)a.dv.p + kv * a.dv.hs + (int64_t)n * a.dv.ld, dv, 1.0f, !at.live, n < a.T, a.d);
+}
+
+constexpr int32_t ATT_MAX_D = 128;
+constexpr int64_t ATT_MAX_T = ((int64_t)1 << 31) - 65536;
+
+int att_check(const char* fn, int64_t T, int32_t n_seq, int32_t n_head, int32_t n_kv, int32_t d, int32_t dtype,
+              float scale) {
+  if (dtype != AGRL_BF16 && dtype != AGRL_F32)
+    return fail(AGRL_E_DTYPE, fn, "dtype must be AGRL_BF16 or AGRL_F32");
+  if (T < 0 || T > ATT_MAX_T || n_seq < 0 || n_seq == 0x7fffffff)
+    return fail(AGRL_E_SHAPE, fn, "bad T or n_seq");
+  if (n_head <= 0 || n_kv <= 0 || n_head % n_kv || d <= 0)
+    return fail(AGRL_E_SHAPE, fn, "n_head must be a multiple of n_kv, d positive");
+  if (cdiv(T, (int64_t)BM) * n_head >= 0x7fffffff) return fail(AGRL_E_SHAPE, fn, "T n_head is too large");
+  if (d > ATT_MAX_D) return fail(AGRL_E_UNSUPPORTED, fn, "d is larger than 128");
+  if (!(scale > 0.0f) || !isfinite(scale)) return fail(AGRL_E_FLAGS, fn, "scale must be finite and > 0");
+  return AGRL_OK;
+}
+int att_strides(const char* fn, int64_t ld, int64_t hs) {
+  return ld < 0 || hs < 0 ? fail(AGRL_E_SHAPE, fn, "a stride is negative") : AGRL_OK;
+}
+
+// f(element type, padded head size, whether it is the head size)
+template <class F>
+void att_pick(int32_t dtype, int32_t d, F&& f) {
+  auto with = [&](auto z) {
+    if (d == 128)
+      f(z, std::integral_constant<int, 128>{}, std::true_type{});
+    else if (d == 64)
+      f(z, std::integral_constant<int, 64>{}, std::true_type{});
+    else if (d > 64)
+      f(z, std::integral_constant<int, 128>{}, std::false_type{});
+    else
+      f(z, std::integral_constant<int, 64>{}, std::false_type{});
+  };
+  if (dtype == AGRL_BF16)
+    with(uint16_t{});
+  else
+    with(float{});
+}
+
+}  // namespace
+}  // namespace agrl
+
+extern "C" int agrl_attention_fwd(int64_t T, int32_t n_seq, int32_t n_head, int32_t n_kv, int32_t d,
+                                  int32_t dtype, const void* q, int64_t ld_q, int64_t head_q,
+                                  const void* k, int64_t ld_k, int64_t head_k, const void* v,
+                                  int64_t ld_v, int64_t head_v, const int32_t* seq_start, float scale,
+                                  void* o, int64_t ld_o, int64_t head_o, float* lse, void* stream) {
+  using namespace agrl;
+  const char* fn = "agrl_attention_fwd";
+  int rc = att_check(fn, T, n_seq, n_head, n_kv, d, dtype, scale);
+  if (!rc) rc = att_strides(fn, ld_q, head_q);
+  if (!rc) rc = att_strides(fn, ld_k, head_k);
+  if (!rc) rc = att_strides(fn, ld_v, head_v);
+  if (rc) return rc;
+  if (!heads_apart(T, n_head, d, ld_o, head_o)) return fail(AGRL_E_SHAPE, fn, "the heads of o overlap");
+  if (T == 0) return AGRL_OK;
+  if (!q || !k || !v || !o || !seq_start) return fail(AGRL_E_NULL, fn, "q, k, v, o or seq_start is NULL");
+  AttArgs a = {};
+  a.T = (int32_t)T, a.n_seq = n_seq, a.n_head = n_head, a.n_kv = n_kv, a.rep = n_head / n_kv, a.d = d;
+  a.q = {q, ld_q, head_q}, a.k = {k, ld_k, head_k}, a.v = {v, ld_v, head_v};
+  a.start = seq_start, a.scale = scale, a.o = {o, ld_o, head_o}, a.lse = lse, a.err = device_error_ptr();
+  att_pick(dtype, d, [&](auto z, auto dp, auto full) {
+    hipLaunchKernelGGL((att_fwd_kernel<decltype(z), decltype(dp)::value, decltype(full)::value>),
+                       dim3((unsigned)(cdiv(T, (int64_t)BM) * n_head)), dim3(THREADS), 0, (hipStream_t)stream, a);
+  });
+  return hip_status(hipGetLastError());
+}
+
+extern "C" size_t agrl_attention_bwd_workspace_size(int64_t T, int32_t n_head, int32_t n_kv, int32_t d,
+                                                    int32_t dtype) {
+  using namespace agrl;
+  if ((dtype != AGRL_BF16 && dtype != AGRL_F32) || T <= 0 || T > ATT_MAX_T || n_head <= 0 || n_kv <= 0 ||
+      n_head % n_kv || d <= 0 || d > ATT_MAX_D || cdiv(T, (int64_t)BM) * n_head >= 0x7fffffff)
+    return 0;
+  return (size_t)T * n_head * 2 * sizeof(float);
+}
+
+extern "C" int agrl_attention_bwd(int64_t T, int32_t n_seq, int32_t n_head, int32_t n_kv, int32_t d,
+                                  int32_t dtype, const void* q, int64_t ld_q, int64_t head_q,
+                                  const void* k, int64_t ld_k, int64_t head_k, const void* v,
+                                  int64_t ld_v, int64_t head_v, const int32_t* seq_start, float scale,
+                                  const void* o, int64_t ld_o, int64_t head_o, const float* lse,
+                                  const void* dout, int64_t ld_do, int64_t head_do, void* workspace,
+                                  size_t ws_bytes, void* dq, int64_t ld_dq, int64_t head_dq, void* dk,
+                                  int64_t ld_dk, int64_t head_dk, void* dv, int64_t ld_dv,
+                                  int64_t head_dv, void* stream) {
+  using namespace agrl;
+  const char* fn = "agrl_attention_bwd";
+  int rc = att_check(fn, T, n_seq, n_head, n_kv, d, dtype, scale);
+  if (!rc) rc = att_strides(fn, ld_q, head_q);
+  if (!rc) rc = att_strides(fn, ld_k, head_k);
+  if (!rc) rc = att_strides(fn, ld_v, head_v);
+  if (!rc) rc = att_strides(fn, ld_o, head_o);
+  if (!rc) rc = att_strides(fn, ld_do, head_do);
+  if (rc) return rc;
+  if (!heads_apart(T, n_head, d, ld_dq, head_dq) || !heads_apart(T, n_kv, d, ld_dk, head_dk) ||
+      !heads_apart(T, n_kv, d, ld_dv, head_dv))
+    return fail(AGRL_E_SHAPE, fn, "the heads of dq, dk or dv overlap");
+  if (T == 0) return AGRL_OK;
+  if (!q || !k || !v || !seq_start || !o || !lse || !dout)
+    return fail(AGRL_E_NULL, fn, "q, k, v, seq_start, o, lse or dout is NULL");
+  if (!dq || !dk || !dv) return fail(AGRL_E_NULL, fn, "dq, dk or dv is NULL");
+  if (!workspace || ws_bytes < agrl_attention_bwd_workspace_size(T, n_head, n_kv, d, dtype))
+    return fail(AGRL_E_WORKSPACE, fn, "workspace missing or too small");
+  if ((uintptr_t)workspace % 256 != 0)
+    return fail(AGRL_E_UNSUPPORTED, fn, "workspace must be 256-byte aligned");
+  hipStream_t s = (hipStream_t)stream;
+  float* lse2 = (float*)workspace;
+  float* delta = lse2 + T * n_head;
+  const DeltaArgs de = {(int32_t)T, n_head, d, {o, ld_o, head_o}, {dout, ld_do, head_do}, lse, lse2, delta};
+  const int64_t need = cdiv(T * n_head, (int64_t)16), most = (int64_t)device_cu_count() * 16;
+  const dim3 dgrid((unsigned)(need < most ? need : most));
+  if (dtype == AGRL_BF16)
+    hipLaunchKernelGGL(att_delta_kernel<uint16_t>, dgrid, dim3(256), 0, s, de);
+  else
+    hipLaunchKernelGGL(att_delta_kernel<float>, dgrid, dim3(256), 0, s, de);
+  AttArgs a = {};
+  a.T = (int32_t)T, a.n_seq = n_seq, a.n_head = n_head, a.n_kv = n_kv, a.rep = n_head / n_kv, a.d = d;
+  a.q = {q, ld_q, head_q}, a.k = {k, ld_k, head_k}, a.v = {v, ld_v, head_v};
+  a.start = seq_start, a.scale = scale, a.err = device_error_ptr();
+  a.dout = {dout, ld_do, head_do}, a.lse2 = lse2, a.delta = delta;
+  a.dq = {dq, ld_dq, head_dq}, a.dk = {dk, ld_dk, head_dk}, a.dv = {dv, ld_dv, head_dv};
+  const int64_t tiles = cdiv(T, (int64_t)BM);
+  att_pick(dtype, d, [&](auto z, auto dp, auto full) {
+    hipLaunchKernelGGL((att_dkv_kernel<decltype(z), decltype(dp)::value, decltype(full)::value>),
+                       dim3((unsigned)(tiles * n_kv)), dim3(THREADS), 0, s, a);
+    hipLaunchKernelGGL((att_dq_kernel<decltype(z), decltype(dp)::value, decltype(full)::value>),
+                       dim3((unsigned)(tiles * n_head)), dim3(THREADS), 0, s, a);
+  });
+  return hip_status(hipGetLastError());
+}

@@ -19,6 +19,7 @@ enum : int {
   ERR_TASK_ID = 4,     // traj_task outside [0, n_task)
   ERR_GROUP_ID = 8,    // traj_group outside [0, n_group)
   ERR_MAX_ACT = 16,    // more action tokens than the workspace was laid out for
+  ERR_SEQ_START = 32,  // sequence offsets that decrease or leave [0, T]
 };
 
 __device__ __forceinline__ float bf16_bits_to_f32(uint16_t b) {

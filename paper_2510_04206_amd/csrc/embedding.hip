@@ -1,0 +1,407 @@
+// Embedding of a packed stream of token ids, and its gradient by sorted tokens (gfx950).
+//
+//   forward   y[n] = scale W[id[n]]
+//   backward  dW[v] (+)= scale * sum over tokens n with id[n] = v of dy[n], n ascending
+//
+// Forward: a wave copies up to 2048 elements of a row.  Memory bounds it.
+//
+// Backward, three launches, no floating-point atomics:
+//   sort  A workgroup owns `range` neighbouring ids and reads all T ids twice.  First it counts
+//         (its ids, a counter per id and wave, and how many ids lie below its own: so it knows
+//         where its tokens start without asking another workgroup), then it places its
+//         tokens in order.  A wave has a run of consecutive tokens and its own counters,
+//         so the order within an id is the tokens'.
+//   rows  The sorted tokens in chunks of 32, each row's run of tokens added up in registers.
+//         A run that lies within its chunk goes to dW, a piece of one that crosses into
+//         another chunk to a partial sum (a separator's run is thousands of tokens: it
+//         is added by as many workgroups).  The rows of ids that do not occur are cleared by
+//         further workgroups of the same launch.
+//   join  adds the pieces of each crossing run in order.
+#include <math.h>
+
+#include "rows.hpp"
+
+namespace agrl {
+namespace {
+
+constexpr int SEG = 64 * CH * 4;       // elements of a row that a wave takes at a time (forward)
+constexpr int64_t MAX_TOKENS = ((int64_t)1 << 31) - 1024;
+
+struct EmbedArgs {
+  int64_t T;
+  int32_t d, V, segs;
+  const void* w;
+  const int32_t* id;
+  const uint8_t* live;
+  float scale;
+  void* y;
+  int64_t ld_y;
+  int* err;
+};
+
+template <typename W, typename Y>
+__global__ void __launch_bounds__(256) embed_fwd_kernel(EmbedArgs a) {
+  const int lane = threadIdx.x & 63;
+  const int64_t first = (int64_t)blockIdx.x * 4 + __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6);
+  const int64_t items = a.T * a.segs;
+  for (int64_t it = first; it < items; it += (int64_t)gridDim.x * 4) {
+    const int64_t n = it / a.segs;
+    const int c0 = (int)(it - n * a.segs) * SEG + lane * CH;
+    const bool live = !a.live || a.live[n] != 0;
+    const int id = live ? a.id[n] : 0;
+    const bool bad = id < 0 || id >= a.V;
+    if (bad && c0 == 0) set_error(a.err, ERR_TOKEN_ID);
+    const W* row = (const W*)a.w + (int64_t)(bad ? 0 : id) * a.d;
+    Y* y = (Y*)a.y + n * a.ld_y;
+    Chunk<W> x[4];
+#pragma unroll
+    for (int k = 0; k < 4; ++k) {
+      const int c = c0 + k * 64 * CH;
+      if (!live || c >= a.d)
+        x[k].zero();
+      else if (c + CH <= a.d)
+        x[k].load(row + c);
+      else
+        x[k].load_some(row + c, a.d - c);
+    }
+#pragma unroll
+    for (int k = 0; k < 4; ++k) {
+      const int c = c0 + k * 64 * CH;
+      float f[CH];
+#pragma unroll
+      for (int e = 0; e < CH; ++e) f[e] = bad ? NAN : live ? x[k].get(e) * a.scale : 0.0f;
+      if (c + CH <= a.d)
+        Chunk<Y>::store(y + c, f);
+      else if (c < a.d)
+        Chunk<Y>::store_some(y + c, f, a.d - c);
+    }
+  }
+}
+
+// ------------------------------------------------------------------ backward
+constexpr int SORT_WAVES = 16;
+constexpr int MAX_RANGE = 512;         // ids per workgroup: 32 KiB of counters
+constexpr int CHUNK = 32;              // sorted tokens per chunk
+constexpr int SLAB = 1024;             // columns per workgroup, four a lane
+constexpr int ZROWS = 8;               // rows that a clearing workgroup looks at
+
+struct SortArgs {
+  int64_t T;
+  int32_t V, range;
+  const int32_t* id;
+  const uint8_t* live;
+  int2* sorted;          // [T] token, id
+  int32_t* row_start;    // [V + 1] first sorted token of each id
+  int* err;
+};
+
+__device__ __forceinline__ int wave_sum_int(int v) {
+#pragma unroll
+  for (int o = 32; o; o >>= 1) v += __shfl_xor(v, o);
+  return v;
+}
+
+__global__ void __launch_bounds__(64 * SORT_WAVES) embed_sort_kernel(SortArgs a) {
+  extern __shared__ int cnt[];                       // [SORT_WAVES][range]
+  __shared__ int below_of[SORT_WAVES], ids_of[SORT_WAVES];
+  const int lane = threadIdx.x & 63;
+  const int wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6);
+  const int lo = blockIdx.x * a.range, hi = min(lo + a.range, a.V);
+  for (int i = threadIdx.x; i < SORT_WAVES * a.range; i += 64 * SORT_WAVES) cnt[i] = 0;
+  __syncthreads();
+  int* own = cnt + wave * a.range;
+  const int64_t per = cdiv(cdiv(a.T, (int64_t)SORT_WAVES), (int64_t)64) * 64;
+  const int64_t t0 = wave * per, t1 = min(a.T, t0 + per);
+  constexpr int NONE = 0x7fffffff;
+  constexpr int AHEAD = 16;                          // loads in flight
+  // a token's id, or NONE for dead tokens and ids out of range
+  auto fetch = [&](int64_t t) {
+    if (t >= t1 || (a.live && a.live[t] == 0)) return NONE;
+    const int id = a.id[t];
+    if (id < 0 || id >= a.V) {
+      if (blockIdx.x == 0) set_error(a.err, ERR_TOKEN_ID);
+      return NONE;
+    }
+    return id;
+  };
+  int below = 0;
+  for (int64_t t = t0 + lane; t < t1 + lane; t += 64 * AHEAD) {
+    int id[AHEAD];
+#pragma unroll
+    for (int k = 0; k < AHEAD; ++k) id[k] = fetch(t + 64 * k);
+#pragma unroll
+    for (int k = 0; k < AHEAD; ++k) {
+      below += id[k] < lo;
+      if (id[k] >= lo && id[k] < hi) atomicAdd(&own[id[k] - lo], 1);
+    }
+  }
+  below = wave_sum_int(below);
+  if (lane == 0) below_of[wave] = below;
+  __syncthreads();
+  // where each id and wave starts: ids in order, within an id the waves in order
+  const int i = threadIdx.x;
+  int mine = 0, sum;
+  if (i < a.range)
+    for (int w = 0; w < SORT_WAVES; ++w) mine += cnt[w * a.range + i];
+  sum = mine;
+#pragma unroll
+  for (int o = 1; o < 64; o <<= 1) {
+    const int up = __shfl_up(sum, o);
+    if (lane >= o) sum += up;
+  }
+  if (lane == 63) ids_of[wave] = sum;
+  __syncthreads();
+  int start = sum - mine;
+  for (int w = 0; w < SORT_WAVES; ++w) start += below_of[w] + (w < wave ? ids_of[w] : 0);
+  if (i < a.range) {
+    if (lo + i <= a.V) a.row_start[lo + i] = start;
+    if (lo + i == a.V - 1) a.row_start[a.V] = start + mine;
+    for (int w = 0; w < SORT_WAVES; ++w) {
+      const int n = cnt[w * a.range + i];
+      cnt[w * a.range + i] = start;
+      start += n;
+    }
+  }
+  __syncthreads();
+  for (int64_t t = t0 + lane; t < t1 + lane; t += 64 * AHEAD) {
+    int id[AHEAD];
+#pragma unroll
+    for (int k = 0; k < AHEAD; ++k) id[k] = fetch(t + 64 * k);
+#pragma unroll
+    for (int k = 0; k < AHEAD; ++k) {
+      uint64_t todo = __ballot(id[k] >= lo && id[k] < hi);
+      while (todo) {
+        const int lead = __builtin_ctzll(todo);
+        const int v = __builtin_amdgcn_readlane(id[k], lead);
+        const uint64_t same = __ballot(id[k] == v);
+        const int at = own[v - lo];
+        if (id[k] == v)
+          a.sorted[at + __popcll(same & (((uint64_t)1 << lane) - 1))] = make_int2((int)(t + 64 * k), v);
+        if (lane == lead) own[v - lo] = at + __popcll(same);
+        __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");    // (the wave's LDS accesses are in order)
+        todo &= ~same;
+      }
+    }
+  }
+}
+
+typedef float f32x4_a4v __attribute__((aligned(4), ext_vector_type(4)));
+typedef uint32_t u32x2_a2v __attribute__((aligned(2), ext_vector_type(2)));
+
+// four elements of a row, those past its end 0
+__device__ __forceinline__ f32x4 load4(const float* p, int n) {
+  if (n >= 4) return *(const f32x4_a4v*)p;
+  f32x4 v = {0.0f, 0.0f, 0.0f, 0.0f};
+  for (int k = 0; k < 3; ++k)
+    if (k < n) v[k] = p[k];
+  return v;
+}
+__device__ __forceinline__ f32x4 load4(const uint16_t* p, int n) {
+  if (n >= 4) {
+    const u32x2_a2v v = *(const u32x2_a2v*)p;
+    return f32x4{__uint_as_float(v.x << 16), __uint_as_float(v.x & 0xffff0000u),
+                 __uint_as_float(v.y << 16), __uint_as_float(v.y & 0xffff0000u)};
+  }
+  f32x4 v = {0.0f, 0.0f, 0.0f, 0.0f};
+  for (int k = 0; k < 3; ++k)
+    if (k < n) v[k] = bf16_bits_to_f32(p[k]);
+  return v;
+}
+__device__ __forceinline__ void store4(float* p, f32x4 v, int n) {
+  if (n >= 4) {
+    *(f32x4_a4v*)p = v;
+  } else {
+    for (int k = 0; k < 3; ++k)
+      if (k < n) p[k] = v[k];
+  }
+}
+
+struct RowsArgs {
+  int32_t d, V, slabs, accumulate;
+  int64_t chunks;
+  const void* dy;
+  int64_t ld_dy;
+  float scale;
+  const int2* sorted;
+  const int32_t* row_start;
+  float* part;           // [chunks][2][d]: the piece that comes in, the piece that goes out
+  float* dw;
+};
+
+__device__ __forceinline__ void put_row(const RowsArgs& a, int v, int col, int n, f32x4 sum) {
+  float* p = a.dw + (int64_t)v * a.d + col;
+  sum *= a.scale;
+  if (a.accumulate) sum += load4(p, n);
+  store4(p, sum, n);
+}
+
+template <typename Y>
+__global__ void __launch_bounds__(256) embed_rows_kernel(RowsArgs a) {
+  const int64_t adding = a.chunks * a.slabs;
+  if (blockIdx.x >= adding) {
+    const int v0 = (int)(blockIdx.x - adding) * ZROWS;
+    for (int v = v0; v < min(v0 + ZROWS, a.V); ++v) {
+      if (a.row_start[v] != a.row_start[v + 1]) continue;
+      float* p = a.dw + (int64_t)v * a.d;
+      for (int c = threadIdx.x * 4; c < a.d; c += 1024) store4(p + c, f32x4{0, 0, 0, 0}, a.d - c);
+    }
+    return;
+  }
+  const int64_t c = blockIdx.x / a.slabs;
+  const int col = (int)(blockIdx.x - c * a.slabs) * SLAB + threadIdx.x * 4;
+  const int total = a.row_start[a.V];
+  const int64_t p0 = c * CHUNK;
+  if (p0 >= total) return;
+  const int n = (int)min((int64_t)CHUNK, total - p0);
+  __shared__ int tok[CHUNK], ids[CHUNK + 2];         // ids[k + 1]: of the chunk's token k
+  if (threadIdx.x < CHUNK + 2) {
+    const int64_t p = p0 + threadIdx.x - 1;
+    const int2 s = p >= 0 && p < total ? a.sorted[p] : make_int2(0, -1);
+    ids[threadIdx.x] = s.y;
+    if (threadIdx.x >= 1 && threadIdx.x <= CHUNK) tok[threadIdx.x - 1] = s.x;
+  }
+  __syncthreads();
+  const int left = a.d - col;
+  if (left <= 0) return;
+  f32x4 sum = {0.0f, 0.0f, 0.0f, 0.0f};
+  bool in = __builtin_amdgcn_readfirstlane(ids[0]) == __builtin_amdgcn_readfirstlane(ids[1]);
+  for (int k0 = 0; k0 < n; k0 += 8) {
+    f32x4 x[8];
+#pragma unroll
+    for (int k = 0; k < 8; ++k) {
+      const int64_t t = __builtin_amdgcn_readfirstlane(tok[min(k0 + k, n - 1)]);
+      x[k] = load4((const Y*)a.dy + t * a.ld_dy + col, left);
+    }
+#pragma unroll
+    for (int k = 0; k < 8; ++k) {
+      if (k0 + k >= n) break;
+      sum += x[k];
+      const int v = __builtin_amdgcn_readfirstlane(ids[k0 + k + 1]);
+      const bool same = v == __builtin_amdgcn_readfirstlane(ids[k0 + k + 2]);
+      if (same && k0 + k + 1 < n) continue;
+      if (!in && !same)
+        put_row(a, v, col, left, sum);
+      else
+        store4(a.part + (2 * c + (in ? 0 : 1)) * a.d + col, sum, left);
+      in = false;
+      sum = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
+    }
+  }
+}
+
+// A run that starts in chunk c and goes on: its pieces in order.
+__global__ void __launch_bounds__(256) embed_join_kernel(RowsArgs a) {
+  const int64_t c = blockIdx.x / a.slabs;
+  const int col = (int)(blockIdx.x - c * a.slabs) * SLAB + threadIdx.x * 4;
+  const int64_t p1 = (c + 1) * CHUNK;
+  if (p1 >= a.row_start[a.V]) return;
+  const int v = a.sorted[p1].y;
+  const int64_t first = a.row_start[v];
+  if (first >= p1 || first < c * CHUNK) return;      // no run goes on, or it came in from before
+  const int left = a.d - col;
+  if (left <= 0) return;
+  const int64_t last = ((int64_t)a.row_start[v + 1] - 1) / CHUNK;
+  f32x4 sum = load4(a.part + (2 * c + 1) * a.d + col, left);
+  const float* p = a.part + (2 * c + 2) * a.d + col;
+#pragma unroll 8
+  for (int64_t k = c + 1; k <= last; ++k, p += 2 * (int64_t)a.d) sum += load4(p, left);
+  put_row(a, v, col, left, sum);
+}
+
+struct Space {
+  size_t sorted, starts, part, total;
+};
+Space embed_space(int64_t T, int32_t d, int32_t V) {
+  auto up = [](size_t n) { return (n + 255) & ~(size_t)255; };
+  Space s;
+  s.sorted = 0;
+  s.starts = up((size_t)T * sizeof(int2));
+  s.part = s.starts + up(((size_t)V + 1) * 4);
+  s.total = s.part + (size_t)cdiv(T, (int64_t)CHUNK) * 2 * d * 4;
+  return s;
+}
+
+// every launch within the grid's 2^31 workgroups
+bool embed_sizes(int64_t T, int32_t d, int32_t V) {
+  return T >= 0 && T <= MAX_TOKENS && d > 0 && d <= (1 << 20) && V > 0 && V < 0x7fffffff &&
+         cdiv(T, (int64_t)CHUNK) * cdiv(d, SLAB) + cdiv(V, ZROWS) < 0x7fffffff;
+}
+
+}  // namespace
+}  // namespace agrl
+
+extern "C" int agrl_token_embed_fwd(int64_t T, int32_t d, int32_t V, int32_t w_dtype, int32_t dtype,
+                                    const void* weight, const int32_t* token_id,
+                                    const uint8_t* live_mask, float scale, void* y, int64_t ld_y,
+                                    void* stream) {
+  using namespace agrl;
+  const char* fn = "agrl_token_embed_fwd";
+  if ((dtype != AGRL_BF16 && dtype != AGRL_F32) || (w_dtype != AGRL_BF16 && w_dtype != AGRL_F32))
+    return fail(AGRL_E_DTYPE, fn, "dtype must be AGRL_BF16 or AGRL_F32");
+  if (!embed_sizes(T, d, V)) return fail(AGRL_E_SHAPE, fn, "bad T, d or V");
+  if (ld_y < d) return fail(AGRL_E_SHAPE, fn, "ld_y is smaller than d");
+  if (!isfinite(scale)) return fail(AGRL_E_FLAGS, fn, "scale must be finite");
+  if (T == 0) return AGRL_OK;
+  if (!weight || !token_id || !y) return fail(AGRL_E_NULL, fn, "weight, token_id or y is NULL");
+  const EmbedArgs a = {T, d, V, cdiv(d, SEG), weight, token_id, live_mask, scale, y, ld_y,
+                       device_error_ptr()};
+  const int64_t need = cdiv(T * a.segs, (int64_t)4), most = (int64_t)device_cu_count() * 8;
+  const dim3 grid((unsigned)(need < most ? need : most)), block(256);
+  hipStream_t s = (hipStream_t)stream;
+  if (w_dtype == AGRL_BF16 && dtype == AGRL_BF16)
+    hipLaunchKernelGGL((embed_fwd_kernel<uint16_t, uint16_t>), grid, block, 0, s, a);
+  else if (w_dtype == AGRL_BF16)
+    hipLaunchKernelGGL((embed_fwd_kernel<uint16_t, float>), grid, block, 0, s, a);
+  else if (dtype == AGRL_BF16)
+    hipLaunchKernelGGL((embed_fwd_kernel<float, uint16_t>), grid, block, 0, s, a);
+  else
+    hipLaunchKernelGGL((embed_fwd_kernel<float, float>), grid, block, 0, s, a);
+  return hip_status(hipGetLastError());
+}
+
+extern "C" size_t agrl_token_embed_bwd_workspace_size(int64_t T, int32_t d, int32_t V) {
+  return agrl::embed_sizes(T, d, V) ? agrl::embed_space(T, d, V).total : 0;
+}
+
+extern "C" int agrl_token_embed_bwd(int64_t T, int32_t d, int32_t V, int32_t dy_dtype,
+                                    const int32_t* token_id, const uint8_t* live_mask,
+                                    const void* dy, int64_t ld_dy, float scale, int32_t accumulate,
+                                    void* workspace, size_t ws_bytes, float* dweight, void* stream) {
+  using namespace agrl;
+  const char* fn = "agrl_token_embed_bwd";
+  if (dy_dtype != AGRL_BF16 && dy_dtype != AGRL_F32)
+    return fail(AGRL_E_DTYPE, fn, "dy_dtype must be AGRL_BF16 or AGRL_F32");
+  if (!embed_sizes(T, d, V)) return fail(AGRL_E_SHAPE, fn, "bad T, d or V");
+  if (ld_dy < d) return fail(AGRL_E_SHAPE, fn, "ld_dy is smaller than d");
+  if (!isfinite(scale)) return fail(AGRL_E_FLAGS, fn, "scale must be finite");
+  if (accumulate != 0 && accumulate != 1) return fail(AGRL_E_FLAGS, fn, "accumulate must be 0 or 1");
+  if (T == 0 && accumulate) return AGRL_OK;
+  if (!dweight || (T > 0 && (!token_id || !dy)))
+    return fail(AGRL_E_NULL, fn, "token_id, dy or dweight is NULL");
+  const Space sp = embed_space(T, d, V);
+  if (!workspace || ws_bytes < sp.total)
+    return fail(AGRL_E_WORKSPACE, fn, "workspace missing or too small");
+  if ((uintptr_t)workspace % 256 != 0)
+    return fail(AGRL_E_UNSUPPORTED, fn, "workspace must be 256-byte aligned");
+  uint8_t* ws = (uint8_t*)workspace;
+  int2* sorted = (int2*)(ws + sp.sorted);
+  int32_t* starts = (int32_t*)(ws + sp.starts);
+  hipStream_t s = (hipStream_t)stream;
+  // an id range a compute unit, as far as the counters fit: what a workgroup places one after
+  // another is then as little as can be
+  const int fair = cdiv(V, device_cu_count());
+  const SortArgs so = {T, V, fair < MAX_RANGE ? fair : MAX_RANGE, token_id, live_mask, sorted, starts,
+                       device_error_ptr()};
+  hipLaunchKernelGGL(embed_sort_kernel, dim3(cdiv(V, so.range)), dim3(64 * SORT_WAVES),
+                     SORT_WAVES * so.range * 4, s, so);
+  const RowsArgs r = {d, V, cdiv(d, SLAB), accumulate, cdiv(T, (int64_t)CHUNK), dy, ld_dy, scale,
+                      sorted, starts, (float*)(ws + sp.part), dweight};
+  const dim3 grid((unsigned)(r.chunks * r.slabs + (accumulate ? 0 : cdiv(V, ZROWS)))), block(256);
+  if (dy_dtype == AGRL_BF16)
+    hipLaunchKernelGGL(embed_rows_kernel<uint16_t>, grid, block, 0, s, r);
+  else
+    hipLaunchKernelGGL(embed_rows_kernel<float>, grid, block, 0, s, r);
+  if (r.chunks > 1)
+    hipLaunchKernelGGL(embed_join_kernel, dim3((unsigned)((r.chunks - 1) * r.slabs)), block, 0, s, r);
+  return hip_status(hipGetLastError());
+}
