@@ -22,6 +22,7 @@
 
 #include <type_traits>
 
+#include "gemm.hpp"
 #include "rows.hpp"
 
 namespace agrl {
@@ -239,9 +240,8 @@ __device__ __forceinline__ int offsets_upto(const int32_t* start, int n_seq, int
 struct Place {
   int begin, end;
   bool live;
-  // first, last: the wave's tokens' range (all lanes); n within it
-  __device__ __forceinline__ Place(const int32_t* start, int n_seq, int T, int first, int last, int n) {
-    int lo = offsets_upto(start, n_seq, first), hi = offsets_upto(start, n_seq, last);
+  // lo, hi: offsets up to the first and the last of the wave's tokens; n one of them
+  __device__ __forceinline__ Place(const int32_t* start, int n_seq, int T, int lo, int hi, int n) {
     while (lo < hi) {
       const int mid = (lo + hi) >> 1;
       if (start[mid] <= n)
@@ -446,7 +446,8 @@ __global__ void __launch_bounds__(THREADS, sizeof(T) == 2 ? 2 : 1) att_fwd_kerne
   const int kv = j % a.n_kv, head = kv * a.rep + j / a.n_kv;
   const int wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6), lane = threadIdx.x & 63;
   const int first = tile * BM + wave * 32, n = first + (lane & 31);
-  const Place at(a.start, a.n_seq, a.T, first, first + 31, n);
+  const Place at(a.start, a.n_seq, a.T, offsets_upto(a.start, a.n_seq, first),
+                 offsets_upto(a.start, a.n_seq, first + 31), n);
   const Span span = query_span(at, n);
   const uint32_t len = at.live ? n - at.begin + 1 : 0;
   int lo, hi;
@@ -540,6 +541,339 @@ __global__ void __launch_bounds__(THREADS, sizeof(T) == 2 ? 2 : 1) att_fwd_kerne
   put_row<T, DP, FULL>((T*)a.o.p + head * a.o.hs + (int64_t)n * a.o.ld, o, 1.0f / l, !at.live, n < a.T, a.d);
 }
 
+// ------------------------------------------------------------------ forward, pipelined
+// 64 queries a wave (two column blocks), one wave a SIMD: half the LDS reads per product, and registers for a
+// pipeline in which nothing waits.  Keys go by halves of 32: while the exponentials of one half run on the
+// vector ALU, the matrix cores form the next half's scores and the previous half's share of o.  A phase
+// has a slot per MFMA (32 cycles of the matrix core); each carries two of the half's 64 columns' values, and
+// every other one an LDS fragment read, three fragments ahead.  K and V go straight from global
+// memory into rings of three tiles of 64, K a tile ahead of V.
+//
+// The softmax's reference is the row's own score q k, which is one of those that count: the sum is at least 1, and
+// there is no running maximum to follow.  Weights may grow to 2^96 before that fails (scores 66 above the row's own);
+// then, or where a NaN or infinite element of V met a weight of 0, a result
+// is not finite, and the workgroup goes through its tile again step by step, with references that follow the maximum
+// and masked elements taken out.
+constexpr int PIPE_ROWS = 64 * WAVES;
+
+template <int N, class F>
+__device__ __forceinline__ void slots(F&& f) {
+  static_for<N>(f);
+}
+
+// Copies of 64-row tiles of a head into LDS, 1 KiB an instruction; rows past the end repeat the last one
+template <int DP>
+struct Copy {
+  using TL = Tile<uint16_t, DP>;
+  static constexpr int RPI = 1024 / TL::ROW, PER = 64 / RPI / WAVES, BYTES = 64 * TL::ROW;
+  const uint8_t* p;
+  int64_t ldb;
+  uint32_t r, c, off;        // lane's row and byte of the first copy, its offset
+  uint32_t lds;
+  int T;
+  __device__ __forceinline__ void init(const void* head, int64_t ld, uint32_t lds_base, int wave, int rows) {
+    const int lane = threadIdx.x & 63;
+    p = (const uint8_t*)head;
+    ldb = ld * 2;
+    T = rows;
+    r = wave * RPI + lane / TL::CPR;
+    c = ((lane & (TL::CPR - 1)) ^ TL::sw(r)) << 4;
+    off = r * (uint32_t)ldb + c;
+    lds = __builtin_amdgcn_readfirstlane(lds_base + wave * 1024);
+  }
+  __device__ __forceinline__ void tile(int row0, int slot) const {
+    const uint8_t* base = p + (int64_t)row0 * ldb;
+    const uint32_t to = lds + slot * BYTES;
+    if (row0 + 64 <= T) {
+      slots<PER>([&](auto i) {
+        bf16k::copy16<i.value * WAVES * 1024>(base + (int64_t)(i.value * WAVES * RPI) * ldb, off, to);
+      });
+    } else {
+      slots<PER>([&](auto i) {
+        const uint32_t row = min(r + i.value * WAVES * RPI, (uint32_t)(T - 1 - row0));
+        bf16k::copy16<i.value * WAVES * 1024>(base, row * (uint32_t)ldb + c, to);
+      });
+    }
+  }
+};
+
+__device__ __forceinline__ uint32_t lds_address(const void* p) {
+  return (uint32_t)(uintptr_t)(__attribute__((address_space(3))) const uint8_t*)p;
+}
+
+template <int DP>
+__global__ void __launch_bounds__(THREADS, 1) att_fwd_pipe_kernel(AttArgs a) {
+  using T = uint16_t;
+  using TL = Tile<T, DP>;
+  using M = Mma<T>;
+  constexpr int NS = TL::NS, ND = TL::ND, NP = TL::NP, ROW = TL::ROW, RING = 3 * Copy<DP>::BYTES;
+  __shared__ __align__(16) uint8_t lds_k[RING], lds_v[RING];
+  __shared__ int lds_span[2][WAVES];
+  if (a.err) check_offsets(a.start, a.n_seq, a.T, a.err);
+  const int tiles = (a.T + PIPE_ROWS - 1) / PIPE_ROWS;
+  const int tile = tiles - 1 - blockIdx.x / a.n_head, j = blockIdx.x % a.n_head;
+  const int kv = j % a.n_kv, head = kv * a.rep + j / a.n_kv;
+  const int wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6), lane = threadIdx.x & 63;
+  const int first = tile * PIPE_ROWS + wave * 64;
+  const int nA = first + (lane & 31), nB = nA + 32;
+  const int upto0 = offsets_upto(a.start, a.n_seq, first), upto1 = offsets_upto(a.start, a.n_seq, first + 63);
+  const Place at[2] = {Place(a.start, a.n_seq, a.T, upto0, upto1, nA),
+                       Place(a.start, a.n_seq, a.T, upto0, upto1, nB)};
+  const Span part[2] = {query_span(at[0], nA), query_span(at[1], nB)};
+  const Span span = {min(part[0].lo, part[1].lo), max(part[0].hi, part[1].hi),
+                     max(part[0].full_lo, part[1].full_lo), min(part[0].full_hi, part[1].full_hi)};
+  int lo, hi;
+  join(span, lds_span, lo, hi);
+
+  const typename TL::Lane L;
+  u32x4 q[2][NS];
+  const T* qp = (const T*)a.q.p + head * a.q.hs;
+  hold<T, DP, true>(q[0], qp + (int64_t)nA * a.q.ld, at[0].live, a.d);
+  hold<T, DP, true>(q[1], qp + (int64_t)nB * a.q.ld, at[1].live, a.d);
+  Copy<DP> ck, cv;
+  ck.init((const T*)a.k.p + kv * a.k.hs, a.k.ld, lds_address(lds_k), wave, a.T);
+  cv.init((const T*)a.v.p + kv * a.v.hs, a.v.ld, lds_address(lds_v), wave, a.T);
+  const float sl2 = a.scale * LOG2E;
+  f32x16 o[2][ND] = {};
+  float l[2] = {0.0f, 0.0f}, m[2];
+  const uint32_t len[2] = {at[0].live ? nA - at[0].begin + 1u : 0u, at[1].live ? nB - at[1].begin + 1u : 0u};
+  // the reference: the row's own score
+  float ref[2];
+#pragma unroll
+  for (int cb = 0; cb < 2; ++cb) {
+    u32x4 own[NS];
+    hold<T, DP, true>(own, (const T*)a.k.p + kv * a.k.hs + (int64_t)(cb ? nB : nA) * a.k.ld, at[cb].live, a.d);
+    float dot = 0.0f;
+#pragma unroll
+    for (int s = 0; s < NS; ++s)
+#pragma unroll
+      for (int e = 0; e < 4; ++e) {
+        const uint32_t x = q[cb][s][e], y = own[s][e];
+        dot = __builtin_amdgcn_fdot2_f32_bf16(__builtin_bit_cast(bf16x2, x), __builtin_bit_cast(bf16x2, y), dot, false);
+      }
+    ref[cb] = (dot + other_half(dot)) * sl2;
+  }
+  const int t0 = lo / 64, t1 = lo < hi ? (hi + 63) / 64 : t0;
+  // the wave's tiles, and those of them that all its columns count whole
+  const int w0 = span.lo < span.hi ? span.lo / 64 : t1, w1 = span.lo < span.hi ? (span.hi + 63) / 64 : t0;
+  const int f0 = (span.full_lo + 63) / 64, f1 = span.full_hi / 64;
+  // what passes from phase to phase
+  constexpr int AHEAD = 3, FR = AHEAD + 1;
+  f32x16 s0[2], s1[2];
+  u32x4 p0[2][NP], p1[2][NP], fr[FR];
+  int ko[NS], vo[ND][2];
+#pragma unroll
+  for (int s = 0; s < NS; ++s) ko[s] = 0;
+#pragma unroll
+  for (int c = 0; c < ND; ++c) vo[c][0] = vo[c][1] = 0;
+#pragma unroll
+  for (int b = 0; b < 2; ++b) {
+    s0[b] = s1[b] = f32x16{};
+#pragma unroll
+    for (int i = 0; i < NP; ++i) p0[b][i] = p1[b][i] = u32x4{0, 0, 0, 0};
+  }
+#pragma unroll
+  for (int i = 0; i < FR; ++i) fr[i] = u32x4{0, 0, 0, 0};
+
+  auto read_v = [&](int half, int s, int c) {
+    const uint8_t* x = lds_v + (half * 32 + s * 16) * ROW;
+    const u32x2 u = __builtin_bit_cast(u32x2, __builtin_amdgcn_ds_read_tr16_b64_v4bf16((lds_bf16x4*)(x + vo[c][0])));
+    const u32x2 w = __builtin_bit_cast(u32x2, __builtin_amdgcn_ds_read_tr16_b64_v4bf16((lds_bf16x4*)(x + vo[c][1] + 8 * ROW)));
+    return u32x4{u.x, u.y, w.x, w.y};
+  };
+  // The weights of `cur` into `pn`, the next half's scores (rows 32 KH of the tile that ko points at) into `nxt`, the
+  // previous half's weights `pp` times V (rows 32 VH of vo's tile).  `move`: what ko (behind its last read for this
+  // phase) or vo (before its first) advance by.
+  auto phase = [&](auto first_c, auto masked_c, f32x16 (&cur)[2], f32x16 (&nxt)[2], u32x4 (&pp)[2][NP], u32x4 (&pn)[2][NP],
+                   int move, int key0) {
+    constexpr bool FIRST = decltype(first_c)::value;      // of a tile
+    constexpr bool MASKED = decltype(masked_c)::value;
+    // keys counted from the lane's first row of the half to its columns' first key
+    const int from[2] = {key0 + 4 * (lane >> 5) - at[0].begin, key0 + 4 * (lane >> 5) - at[1].begin};
+    constexpr int KH = FIRST ? 1 : 0, VH = FIRST ? 1 : 0;
+    constexpr int NQ = 2 * NS, NM = NQ + 2 * NP * ND, NF = NM / 2;
+    slots<NM>([&](auto slot) {
+      constexpr int i = slot.value, fi = i / 2, b = i & 1;
+      if constexpr (b == 0) {
+        constexpr int n = fi + AHEAD;
+        if constexpr (n < NS)
+          fr[n % FR] = *(const u32x4*)(lds_k + KH * 32 * ROW + ko[n]);
+        else if constexpr (n < NF)
+          fr[n % FR] = read_v(VH, (n - NS) / ND, (n - NS) % ND);
+        else
+          fr[n % FR] = *(const u32x4*)(lds_k + (KH ^ 1) * 32 * ROW + ko[n - NF]);
+      }
+      if constexpr (i < NQ) {
+        nxt[b] = M::mma(fr[fi % FR], q[b][fi], fi == 0 ? f32x16{} : nxt[b]);
+      } else {
+        constexpr int s = (fi - NS) / ND, c = (fi - NS) % ND;
+        o[b][c] = M::mma(fr[fi % FR], pp[b][s], o[b][c]);
+      }
+      if constexpr (FIRST && i >= NQ && i < NQ + NS) ko[i - NQ] += move;
+      if constexpr (!FIRST && i < 2 * ND) vo[i >> 1][i & 1] += move;
+      constexpr int e0 = i * 16 / NM * 2, e1 = (i + 1) * 16 / NM * 2;      // values of the two columns
+#pragma unroll
+      for (int e = e0; e < e1; e += 2) {
+        const int cb = e >> 4, r = e & 15;
+#pragma unroll
+        for (int k = 0; k < 2; ++k) {
+          if constexpr (MASKED) {
+            const bool in = (uint32_t)(from[cb] + 8 * (r >> 2) + (r & 3) + k) < len[cb];
+            cur[cb][r + k] = in ? cur[cb][r + k] : -INFINITY;
+          }
+          cur[cb][r + k] = __builtin_amdgcn_exp2f(fmaf(cur[cb][r + k], sl2, -ref[cb]));
+          l[cb] += cur[cb][r + k];
+        }
+        uint32_t w = M::pack(cur[cb][r], cur[cb][r + 1]);
+        asm volatile("" : "+v"(w), "+v"(l[cb]));          // (here, not where it is used)
+        pn[cb][r >> 3][(r & 7) >> 1] = w;
+      }
+      __builtin_amdgcn_sched_barrier(0);
+    });
+  };
+
+  constexpr int TB = Copy<DP>::BYTES;
+  int slot = 0;        // of tile t in both rings
+  auto begin = [&]() {
+    slot = 0;
+    if (t0 >= t1) return;
+    ck.tile(t0 * 64, 0);
+    if (t0 + 1 < t1) ck.tile(t0 * 64 + 64, 1);
+    cv.tile(t0 * 64, 0);
+  };
+  // tile t has landed, the next ones are on their way
+  auto arrive = [&](int t) {
+    asm volatile("s_waitcnt vmcnt(0)\n\ts_barrier" ::: "memory");
+    const int next = slot == 2 ? 0 : slot + 1;
+    if (t + 2 < t1) ck.tile(t * 64 + 128, next == 2 ? 0 : next + 1);
+    if (t + 1 < t1) cv.tile(t * 64 + 64, next);
+  };
+  begin();
+  int t = t0;
+  for (; t < min(w0, t1); ++t) {
+    arrive(t);
+    slot = slot == 2 ? 0 : slot + 1;
+  }
+  if (t < w1) {
+    arrive(t);
+    // the first half's scores; no weights are pending yet (V's first half meets weights of 0)
+    const int at_k = slot * TB;
+#pragma unroll
+    for (int s = 0; s < NS; ++s) ko[s] = (L.row ^ (s << 5)) + at_k;
+#pragma unroll
+    for (int c = 0; c < ND; ++c) {
+      vo[c][0] = (L.tr ^ (c << 6)) + at_k;
+      vo[c][1] = (L.tr ^ (c << 6) ^ 32) + at_k;
+    }
+#pragma unroll
+    for (int b = 0; b < 2; ++b) {
+      s0[b] = mul_rows<T, DP>(lds_k + at_k, L, 0, q[b]);
+#pragma unroll
+      for (int i = 0; i < NP; ++i) p1[b][i] = u32x4{0, 0, 0, 0};
+    }
+#pragma unroll
+    for (int i = 0; i < AHEAD; ++i) fr[i] = *(const u32x4*)(lds_k + 32 * ROW + ko[i]);
+    static_assert((NS + NP * ND) % FR == 0, "a phase starts at the ring's first fragment");
+    int vmove = 0;
+    auto through = [&](auto masked_c, int until) {
+      while (t < until) {
+        const int kmove = slot == 2 ? -2 * TB : TB;
+        phase(std::true_type{}, masked_c, s0, s1, p1, p0, kmove, t * 64);
+        phase(std::false_type{}, masked_c, s1, s0, p0, p1, vmove, t * 64 + 32);
+        vmove = kmove;
+        slot = slot == 2 ? 0 : slot + 1;
+        if (++t < w1) arrive(t);
+      }
+    };
+    through(std::true_type{}, min(f0, w1));
+    through(std::false_type{}, min(f1, w1));
+    through(std::true_type{}, w1);
+#pragma unroll
+    for (int s = 0; s < NP; ++s)
+#pragma unroll
+      for (int c = 0; c < ND; ++c) {
+        const u32x4 v = read_v(1, s, c);
+        o[0][c] = M::mma(v, p1[0][s], o[0][c]);
+        o[1][c] = M::mma(v, p1[1][s], o[1][c]);
+      }
+  }
+  for (; t < t1; ++t) {
+    arrive(t);
+    slot = slot == 2 ? 0 : slot + 1;
+  }
+  bool lost = false;
+#pragma unroll
+  for (int cb = 0; cb < 2; ++cb) {
+    m[cb] = ref[cb];
+    l[cb] += other_half(l[cb]);
+    float z = l[cb] > 0.5f && l[cb] < 0x1p96f ? 0.0f : 1.0f;
+#pragma unroll
+    for (int c = 0; c < ND; ++c)
+#pragma unroll
+      for (int r = 0; r < 16; ++r) z = fmaf(o[cb][c][r], 0.0f, z);
+    lost = lost || (at[cb].live && z != 0.0f);       // (1 or NaN)
+  }
+  if (__syncthreads_or(lost)) {
+#pragma unroll
+    for (int cb = 0; cb < 2; ++cb) {
+      l[cb] = 0.0f;
+#pragma unroll
+      for (int c = 0; c < ND; ++c) o[cb][c] = f32x16{};
+    }
+    begin();
+    for (t = t0; t < t1; ++t) {
+      arrive(t);
+      const int at_k = slot * TB;
+#pragma unroll
+      for (int cb = 0; cb < 2; ++cb) {
+        if (t * 64 + 64 <= part[cb].lo || t * 64 >= part[cb].hi) continue;
+#pragma unroll
+        for (int b = 0; b < 2; ++b) {
+          f32x16 s = mul_rows<T, DP>(lds_k + at_k, L, b, q[cb]);
+          uint32_t ok = 0;
+          float top = -INFINITY;
+#pragma unroll
+          for (int r = 0; r < 16; ++r) {
+            const bool in = (uint32_t)(t * 64 + 32 * b + acc_row(r) - at[cb].begin) < len[cb];
+            ok |= in ? 1u << r : 0u;
+            s[r] = in ? s[r] : -INFINITY;
+            top = fmaxf(top, s[r]);
+          }
+          top = fmaxf(top, other_half(top)) * sl2;
+          // (rows that nothing was wrong with keep their reference, and so their bits)
+          const bool far = top > m[cb] + 64.0f;
+          const float to = far ? top : m[cb], f = far ? __builtin_amdgcn_exp2f(m[cb] - to) : 1.0f;
+          m[cb] = to;
+          l[cb] *= f;
+#pragma unroll
+          for (int c = 0; c < ND; ++c) o[cb][c] *= f;
+          const float from = to == -INFINITY ? 0.0f : to;
+          u32x4 p[NP];
+#pragma unroll
+          for (int r = 0; r < 16; ++r) {
+            s[r] = __builtin_amdgcn_exp2f(fmaf(s[r], sl2, -from));
+            l[cb] += s[r];
+          }
+#pragma unroll
+          for (int i = 0; i < NP; ++i) p[i] = M::frag(s, i);
+          add_cols<T, DP, true>(o[cb], lds_v + at_k, L, b, p, ok);
+        }
+      }
+      slot = slot == 2 ? 0 : slot + 1;
+    }
+#pragma unroll
+    for (int cb = 0; cb < 2; ++cb) l[cb] += other_half(l[cb]);
+  }
+#pragma unroll
+  for (int cb = 0; cb < 2; ++cb) {
+    const int n = cb ? nB : nA;
+    if (a.lse && n < a.T && lane < 32)
+      a.lse[(int64_t)head * a.T + n] = at[cb].live ? LN2 * (m[cb] + __builtin_amdgcn_logf(l[cb])) : 0.0f;
+    put_row<T, DP, true>((T*)a.o.p + head * a.o.hs + (int64_t)n * a.o.ld, o[cb], 1.0f / l[cb], !at[cb].live,
+                         n < a.T, a.d);
+  }
+}
+
 // ------------------------------------------------------------------ backward
 // lse in powers of 2 and D = sum do o, [n_head, T].  A wave takes a token's heads in turn, 16 lanes a head.
 struct DeltaArgs {
@@ -593,7 +927,8 @@ __global__ void __launch_bounds__(THREADS, sizeof(T) == 2 ? 2 : 1) att_dq_kernel
   const int kv = j % a.n_kv, head = kv * a.rep + j / a.n_kv;
   const int wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6), lane = threadIdx.x & 63;
   const int first = tile * BM + wave * 32, n = first + (lane & 31);
-  const Place at(a.start, a.n_seq, a.T, first, first + 31, n);
+  const Place at(a.start, a.n_seq, a.T, offsets_upto(a.start, a.n_seq, first),
+                 offsets_upto(a.start, a.n_seq, first + 31), n);
   const Span span = query_span(at, n);
   const uint32_t len = at.live ? n - at.begin + 1 : 0;
   int lo, hi;
@@ -674,7 +1009,8 @@ __global__ void __launch_bounds__(THREADS, 1) att_dkv_kernel(AttArgs a) {
   const int tile = blockIdx.x / a.n_kv, kv = blockIdx.x % a.n_kv;
   const int wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6), lane = threadIdx.x & 63;
   const int first = tile * BM + wave * 32, n = first + (lane & 31);
-  const Place at(a.start, a.n_seq, a.T, first, first + 31, n);
+  const Place at(a.start, a.n_seq, a.T, offsets_upto(a.start, a.n_seq, first),
+                 offsets_upto(a.start, a.n_seq, first + 31), n);
   // a key is counted by the rows from itself to its sequence's end
   const Span span = {wave_min(at.live ? n : 0x7fffffff), wave_max(at.live ? at.end : 0),
                      wave_max(n), __all(at.live) ? wave_min(at.end) : 0};
@@ -782,6 +1118,11 @@ int att_strides(const char* fn, int64_t ld, int64_t hs) {
   return ld < 0 || hs < 0 ? fail(AGRL_E_SHAPE, fn, "a stride is negative") : AGRL_OK;
 }
 
+// Whether 16-byte copies reach every row of a bf16 operand, 64 rows within 32-bit offsets
+bool copies(const Heads& h) {
+  return (uintptr_t)h.p % 16 == 0 && h.ld % 8 == 0 && h.hs % 8 == 0 && h.ld < (1 << 24);
+}
+
 // f(element type, padded head size, whether it is the head size)
 template <class F>
 void att_pick(int32_t dtype, int32_t d, F&& f) {
@@ -823,6 +1164,14 @@ extern "C" int agrl_attention_fwd(int64_t T, int32_t n_seq, int32_t n_head, int3
   a.T = (int32_t)T, a.n_seq = n_seq, a.n_head = n_head, a.n_kv = n_kv, a.rep = n_head / n_kv, a.d = d;
   a.q = {q, ld_q, head_q}, a.k = {k, ld_k, head_k}, a.v = {v, ld_v, head_v};
   a.start = seq_start, a.scale = scale, a.o = {o, ld_o, head_o}, a.lse = lse, a.err = device_error_ptr();
+  if (dtype == AGRL_BF16 && (d == 64 || d == 128) && copies(a.k) && copies(a.v)) {
+    const dim3 grid((unsigned)(cdiv(T, (int64_t)PIPE_ROWS) * n_head));
+    if (d == 128)
+      hipLaunchKernelGGL(att_fwd_pipe_kernel<128>, grid, dim3(THREADS), 0, (hipStream_t)stream, a);
+    else
+      hipLaunchKernelGGL(att_fwd_pipe_kernel<64>, grid, dim3(THREADS), 0, (hipStream_t)stream, a);
+    return hip_status(hipGetLastError());
+  }
   att_pick(dtype, d, [&](auto z, auto dp, auto full) {
     hipLaunchKernelGGL((att_fwd_kernel<decltype(z), decltype(dp)::value, decltype(full)::value>),
                        dim3((unsigned)(cdiv(T, (int64_t)BM) * n_head)), dim3(THREADS), 0, (hipStream_t)stream, a);
