@@ -658,7 +658,8 @@ __global__ void __launch_bounds__(THREADS, 1) att_fwd_pipe_kernel(AttArgs a) {
   const int w0 = span.lo < span.hi ? span.lo / 64 : t1, w1 = span.lo < span.hi ? (span.hi + 63) / 64 : t0;
   const int f0 = (span.full_lo + 63) / 64, f1 = span.full_hi / 64;
   // what passes from phase to phase
-  constexpr int AHEAD = 3, FR = AHEAD + 1;
+  constexpr int AHEAD = DP == 128 ? 7 : 3, FR = AHEAD + 1;
+  static_assert(AHEAD <= NS, "what is read ahead of a phase is K");
   f32x16 s0[2], s1[2];
   u32x4 p0[2][NP], p1[2][NP], fr[FR];
   int ko[NS], vo[ND][2];
@@ -711,23 +712,29 @@ __global__ void __launch_bounds__(THREADS, 1) att_fwd_pipe_kernel(AttArgs a) {
       }
       if constexpr (FIRST && i >= NQ && i < NQ + NS) ko[i - NQ] += move;
       if constexpr (!FIRST && i < 2 * ND) vo[i >> 1][i & 1] += move;
-      constexpr int e0 = i * 16 / NM * 2, e1 = (i + 1) * 16 / NM * 2;      // values of the two columns
-#pragma unroll
-      for (int e = e0; e < e1; e += 2) {
-        const int cb = e >> 4, r = e & 15;
-#pragma unroll
-        for (int k = 0; k < 2; ++k) {
+      // a value takes three slots: its exponent, the exponential, the sum and the conversion
+      constexpr int EPS = 32 / NM, last = i + 1 == NM ? 32 : 0;
+      slots<32>([&](auto e_c) {
+        constexpr int e = e_c.value, cb = e >> 4, r = e & 15;
+        float x = cur[cb][r];
+        if constexpr (e / EPS == i) {
           if constexpr (MASKED) {
-            const bool in = (uint32_t)(from[cb] + 8 * (r >> 2) + (r & 3) + k) < len[cb];
-            cur[cb][r + k] = in ? cur[cb][r + k] : -INFINITY;
+            const bool in = (uint32_t)(from[cb] + 8 * (r >> 2) + (r & 3)) < len[cb];
+            x = in ? x : -INFINITY;
           }
-          cur[cb][r + k] = __builtin_amdgcn_exp2f(fmaf(cur[cb][r + k], sl2, -ref[cb]));
-          l[cb] += cur[cb][r + k];
+          x = fmaf(x, sl2, -ref[cb]);
         }
-        uint32_t w = M::pack(cur[cb][r], cur[cb][r + 1]);
-        asm volatile("" : "+v"(w), "+v"(l[cb]));          // (here, not where it is used)
-        pn[cb][r >> 3][(r & 7) >> 1] = w;
-      }
+        if constexpr (e / EPS == i - 1 || (last && e / EPS == i)) x = __builtin_amdgcn_exp2f(x);
+        if constexpr (e / EPS == i - 2 || (last && e / EPS >= i - 1)) {
+          l[cb] += x;
+          if constexpr (r & 1) {
+            uint32_t w = M::pack(cur[cb][r - 1], x);
+            asm volatile("" : "+v"(w), "+v"(l[cb]));          // (here, not where it is used)
+            pn[cb][r >> 3][(r & 7) >> 1] = w;
+          }
+        }
+        cur[cb][r] = x;
+      });
       __builtin_amdgcn_sched_barrier(0);
     });
   };
