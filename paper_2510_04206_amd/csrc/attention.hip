@@ -581,9 +581,10 @@ struct Copy {
     off = r * (uint32_t)ldb + c;
     lds = __builtin_amdgcn_readfirstlane(lds_base + wave * 1024);
   }
-  __device__ __forceinline__ void tile(int row0, int slot) const {
-    const uint8_t* base = p + (int64_t)row0 * ldb;
-    const uint32_t to = lds + slot * BYTES;
+  // rows row0 .. row0 + 63 of the head `head` bytes on, to byte `at` of the ring
+  __device__ __forceinline__ void tile(int row0, int at, int64_t head = 0) const {
+    const uint8_t* base = p + head + (int64_t)row0 * ldb;
+    const uint32_t to = lds + at;
     if (row0 + 64 <= T) {
       slots<PER>([&](auto i) {
         bf16k::copy16<i.value * WAVES * 1024>(base + (int64_t)(i.value * WAVES * RPI) * ldb, off, to);
@@ -745,15 +746,15 @@ __global__ void __launch_bounds__(THREADS, 1) att_fwd_pipe_kernel(AttArgs a) {
     slot = 0;
     if (t0 >= t1) return;
     ck.tile(t0 * 64, 0);
-    if (t0 + 1 < t1) ck.tile(t0 * 64 + 64, 1);
+    if (t0 + 1 < t1) ck.tile(t0 * 64 + 64, TB);
     cv.tile(t0 * 64, 0);
   };
   // tile t has landed, the next ones are on their way
   auto arrive = [&](int t) {
     asm volatile("s_waitcnt vmcnt(0)\n\ts_barrier" ::: "memory");
     const int next = slot == 2 ? 0 : slot + 1;
-    if (t + 2 < t1) ck.tile(t * 64 + 128, next == 2 ? 0 : next + 1);
-    if (t + 1 < t1) cv.tile(t * 64 + 64, next);
+    if (t + 2 < t1) ck.tile(t * 64 + 128, (next == 2 ? 0 : next + 1) * TB);
+    if (t + 1 < t1) cv.tile(t * 64 + 64, next * TB);
   };
   begin();
   int t = t0;
@@ -1105,6 +1106,257 @@ __global__ void __launch_bounds__(THREADS, 1) att_dkv_kernel(AttArgs a) {
   put_row<T, DP, FULL>((T*)a.dv.p + kv * a.dv.hs + (int64_t)n * a.dv.ld, dv, 1.0f, !at.live, n < a.T, a.d);
 }
 
+// ------------------------------------------------------------------ backward, pipelined
+// As in the forward: a slot per MFMA, the vector ALU's share of a half of 32 rows spread over the slots of a phase,
+// fragments read AHEAD of their use, tiles of 64 rows copied into rings.  Weights are at most 1, so nothing needs
+// a reference; a result that is not finite sends the workgroup through its tile again, step by step
+// with masked elements taken out.
+
+// dk, dv: 32 keys a wave.  A phase forms the next half's S and dP, the previous half's shares of dv and dk, and on the
+// vector ALU this half's P and dS.  A ring of four tiles: Q's and do's rows are read a half ahead, their
+// columns a half behind.
+template <int DP>
+__global__ void __launch_bounds__(THREADS, 1) att_dkv_pipe_kernel(AttArgs a) {
+  using T = uint16_t;
+  using TL = Tile<T, DP>;
+  using M = Mma<T>;
+  constexpr int NS = TL::NS, ND = TL::ND, NP = TL::NP, ROW = TL::ROW, TB = Copy<DP>::BYTES;
+  constexpr int SLOT = 2 * TB, RING = 4 * SLOT, STAT = 2 * 64 * 4;
+  __shared__ __align__(16) uint8_t lds[RING];                 // [4][Q, do]
+  __shared__ __align__(16) uint8_t lds_s[4 * STAT];           // [4][lse, D][64]
+  __shared__ int lds_span[2][WAVES];
+  const int tile = blockIdx.x / a.n_kv, kv = blockIdx.x % a.n_kv;
+  const int wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6), lane = threadIdx.x & 63;
+  const int first = tile * BM + wave * 32, n = first + (lane & 31);
+  const Place at(a.start, a.n_seq, a.T, offsets_upto(a.start, a.n_seq, first),
+                 offsets_upto(a.start, a.n_seq, first + 31), n);
+  const Span span = {wave_min(at.live ? n : 0x7fffffff), wave_max(at.live ? at.end : 0),
+                     wave_max(n), __all(at.live) ? wave_min(at.end) : 0};
+  const uint32_t len = at.live ? at.end - n : 0;
+  const bool head_of = at.live && at.begin == n;
+  int lo, hi;
+  join(span, lds_span, lo, hi);
+  const int t0 = lo / 64, t1 = lo < hi ? (hi + 63) / 64 : t0, per = t1 - t0, steps = per * a.rep;
+  const int w0 = span.lo < span.hi ? span.lo / 64 : t1, w1 = span.lo < span.hi ? (span.hi + 63) / 64 : t0;
+  const int f0 = (span.full_lo + 63) / 64, f1 = span.full_hi / 64;
+
+  const typename TL::Lane L;
+  u32x4 k[NS], v[NS];
+  hold<T, DP, true>(k, (const T*)a.k.p + kv * a.k.hs + (int64_t)n * a.k.ld, at.live, a.d);
+  hold<T, DP, true>(v, (const T*)a.v.p + kv * a.v.hs + (int64_t)n * a.v.ld, at.live, a.d);
+  Copy<DP> cq, cg;
+  cq.init((const T*)a.q.p + (int64_t)kv * a.rep * a.q.hs, a.q.ld, lds_address(lds), wave, a.T);
+  cg.init((const T*)a.dout.p + (int64_t)kv * a.rep * a.dout.hs, a.dout.ld, lds_address(lds) + TB, wave, a.T);
+  const float* stats = (threadIdx.x < 64 ? a.lse2 : a.delta) + (int64_t)kv * a.rep * a.T;
+  const float sl2 = a.scale * LOG2E;
+  f32x16 dk[ND] = {}, dv[ND] = {};
+  constexpr int AHEAD = 7, FR = AHEAD + 1;
+  f32x16 s0 = {}, s1 = {}, d0 = {}, d1 = {};
+  u32x4 p0[NP], p1[NP], e0[NP], e1[NP], fr[FR];
+  f32x4 zt[2], dt[2];
+  int ko[NS], vo[ND][2], so = 0;
+#pragma unroll
+  for (int i = 0; i < NP; ++i) p0[i] = p1[i] = e0[i] = e1[i] = u32x4{0, 0, 0, 0};
+#pragma unroll
+  for (int i = 0; i < FR; ++i) fr[i] = u32x4{0, 0, 0, 0};
+
+  auto read_col = [&](int off, int s, int c) {
+    const uint8_t* x = lds + off + s * 16 * ROW;
+    const u32x2 u = __builtin_bit_cast(u32x2, __builtin_amdgcn_ds_read_tr16_b64_v4bf16((lds_bf16x4*)(x + vo[c][0])));
+    const u32x2 w = __builtin_bit_cast(u32x2, __builtin_amdgcn_ds_read_tr16_b64_v4bf16((lds_bf16x4*)(x + vo[c][1] + 8 * ROW)));
+    return u32x4{u.x, u.y, w.x, w.y};
+  };
+  auto read_stat = [&](int half, int g) {
+    zt[g & 1] = *(const f32x4*)(lds_s + so + half * 128 + g * 32);
+    dt[g & 1] = *(const f32x4*)(lds_s + so + half * 128 + g * 32 + 256);
+  };
+  // this half's P and dS from s, d into pn, en; the next half's scores and dP into sn, dn; the previous half's pp, ep
+  // into dv and dk.  move: as in the forward, so after its last read of the tile.
+  auto phase = [&](auto first_c, auto masked_c, f32x16& s, f32x16& d, f32x16& sn, f32x16& dn, u32x4 (&pp)[NP],
+                   u32x4 (&ep)[NP], u32x4 (&pn)[NP], u32x4 (&en)[NP], int move, int smove, int q0) {
+    constexpr bool FIRST = decltype(first_c)::value, MASKED = decltype(masked_c)::value;
+    constexpr int KH = FIRST ? 1 : 0, NC = NP * ND, NM = 2 * NS + 2 * NC;
+    const uint32_t from = q0 + 4 * (lane >> 5) - n;
+    slots<NM>([&](auto slot) {
+      constexpr int i = slot.value, rd = i + AHEAD;
+      if constexpr (rd < 2 * NS)
+        fr[rd % FR] = *(const u32x4*)(lds + KH * 32 * ROW + (rd < NS ? 0 : TB) + ko[rd % NS]);
+      else if constexpr (rd < NM) {
+        constexpr int c = (rd - 2 * NS) % NC;
+        fr[rd % FR] = read_col(KH * 32 * ROW + (rd < 2 * NS + NC ? TB : 0), c / ND, c % ND);
+      } else {
+        fr[rd % FR] = *(const u32x4*)(lds + (KH ^ 1) * 32 * ROW + (rd - NM < NS ? 0 : TB) + ko[(rd - NM) % NS]);
+      }
+      if constexpr (i < NS)
+        sn = M::mma(fr[i % FR], k[i], i == 0 ? f32x16{} : sn);
+      else if constexpr (i < 2 * NS)
+        dn = M::mma(fr[i % FR], v[i - NS], i == NS ? f32x16{} : dn);
+      else if constexpr (i < 2 * NS + NC)
+        dv[(i - 2 * NS) % ND] = M::mma(fr[i % FR], pp[(i - 2 * NS) / ND], dv[(i - 2 * NS) % ND]);
+      else
+        dk[(i - 2 * NS - NC) % ND] = M::mma(fr[i % FR], ep[(i - 2 * NS - NC) / ND], dk[(i - 2 * NS - NC) % ND]);
+      if constexpr (FIRST && i >= 2 * NS && i < 3 * NS) ko[i - 2 * NS] += move;
+      if constexpr (!FIRST && i == 0)
+#pragma unroll
+        for (int c = 0; c < ND; ++c) vo[c][0] += move, vo[c][1] += move;
+      // a value takes two slots: the exponent, then the exponential and the rest
+      slots<16>([&](auto e_c) {
+        constexpr int r = e_c.value, sl = r * NM / 16;
+        float x = s[r], y = d[r];
+        bool in = true;
+        if constexpr (MASKED) in = from + 8 * (r >> 2) + (r & 3) < len;
+        if constexpr (sl == i) {
+          if constexpr (MASKED) x = in ? x : -INFINITY;
+          x = fmaf(x, sl2, -zt[(r >> 2) & 1][r & 3]);
+        }
+        if constexpr (sl + 1 == i || (sl == i && i + 1 == NM)) {
+          x = __builtin_amdgcn_exp2f(x);
+          y = x * (y - dt[(r >> 2) & 1][r & 3]);
+          if constexpr (MASKED) y = in && !(head_of && from + 8 * (r >> 2) + (r & 3) == 0) ? y : 0.0f;
+          if constexpr (r & 1) {
+            uint32_t w = M::pack(s[r - 1], x), z = M::pack(d[r - 1], y);
+            asm volatile("" : "+v"(w), "+v"(z));              // (here, not where it is used)
+            pn[r >> 3][(r & 7) >> 1] = w;
+            en[r >> 3][(r & 7) >> 1] = z;
+          }
+        }
+        s[r] = x;
+        d[r] = y;
+      });
+      // the row statistics, four rows at a time (behind the last value that used the two places)
+      constexpr int G = NM / 4;
+      if constexpr (i % G == 0 && i / G < 3) read_stat(FIRST ? 0 : 1, i / G + 1);
+      if constexpr (i == 3 * G) {
+        if constexpr (!FIRST) so += smove;
+        read_stat(FIRST ? 1 : 0, 0);
+      }
+      __builtin_amdgcn_sched_barrier(0);
+    });
+  };
+
+  float stat = 0.0f;
+  auto load_stat = [&](int u) {
+    const int row = (t0 + u % per) * 64 + (threadIdx.x & 63);
+    if (threadIdx.x < 128 && u < steps && row < a.T) stat = stats[(int64_t)(u / per) * a.T + row];
+  };
+  auto put_stat = [&](int u) {
+    if (threadIdx.x < 128) *(float*)(lds_s + (u & 3) * STAT + threadIdx.x * 4) = stat;
+  };
+  auto copy = [&](int u) {
+    if (u >= steps) return;
+    const int h = u / per, row = (t0 + u - h * per) * 64;
+    cq.tile(row, (u & 3) * SLOT, (int64_t)h * a.q.hs * 2);
+    cg.tile(row, (u & 3) * SLOT, (int64_t)h * a.dout.hs * 2);
+  };
+  int u = 0;           // the tile in turn, over all heads
+  auto begin = [&]() {
+    u = 0;
+    if (steps == 0) return;
+    load_stat(0);
+    put_stat(0);
+    load_stat(1);
+    copy(0);
+    copy(1);
+  };
+  // tile u and the next one have landed, the one after is on its way
+  auto arrive = [&]() {
+    asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+    put_stat(u + 1);
+    asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory");
+    load_stat(u + 2);
+    copy(u + 2);
+  };
+  begin();
+  for (int h = 0; h < a.rep; ++h) {
+    int t = t0;
+    for (; t < min(w0, t1); ++t, ++u) arrive();
+    if (t < w1) {
+      arrive();
+      const int at_q = (u & 3) * SLOT;
+#pragma unroll
+      for (int s = 0; s < NS; ++s) ko[s] = (L.row ^ (s << 5)) + at_q;
+#pragma unroll
+      for (int c = 0; c < ND; ++c) {
+        vo[c][0] = (L.tr ^ (c << 6)) + at_q;
+        vo[c][1] = (L.tr ^ (c << 6) ^ 32) + at_q;
+      }
+      so = (u & 3) * STAT + 16 * (lane >> 5);
+      s0 = mul_rows<T, DP>(lds + at_q, L, 0, k);
+      d0 = mul_rows<T, DP>(lds + at_q + TB, L, 0, v);
+#pragma unroll
+      for (int i = 0; i < NP; ++i) p1[i] = e1[i] = u32x4{0, 0, 0, 0};
+      read_stat(0, 0);
+#pragma unroll
+      for (int i = 0; i < AHEAD; ++i)
+        fr[i] = *(const u32x4*)(lds + 32 * ROW + (i < NS ? 0 : TB) + ko[i % NS]);
+      static_assert((2 * NS + 2 * NP * ND) % FR == 0, "a phase starts at the ring's first fragment");
+      int vmove = 0;
+      auto through = [&](auto masked_c, int until) {
+        while (t < until) {
+          const int kmove = (u & 3) == 3 ? -3 * SLOT : SLOT, smove = (u & 3) == 3 ? -3 * STAT : STAT;
+          phase(std::true_type{}, masked_c, s0, d0, s1, d1, p1, e1, p0, e0, kmove, 0, t * 64);
+          phase(std::false_type{}, masked_c, s1, d1, s0, d0, p0, e0, p1, e1, vmove, smove, t * 64 + 32);
+          vmove = kmove;
+          ++u;
+          if (++t < w1) arrive();
+        }
+      };
+      through(std::true_type{}, min(f0, w1));
+      through(std::false_type{}, min(f1, w1));
+      through(std::true_type{}, w1);
+#pragma unroll
+      for (int s = 0; s < NP; ++s)
+#pragma unroll
+        for (int c = 0; c < ND; ++c) {
+          dv[c] = M::mma(read_col(32 * ROW + TB, s, c), p1[s], dv[c]);
+          dk[c] = M::mma(read_col(32 * ROW, s, c), e1[s], dk[c]);
+        }
+    }
+    for (; t < t1; ++t, ++u) arrive();
+  }
+  float bad = 0.0f;
+#pragma unroll
+  for (int c = 0; c < ND; ++c)
+#pragma unroll
+    for (int r = 0; r < 16; ++r) bad = fmaf(dk[c][r], 0.0f, fmaf(dv[c][r], 0.0f, bad));
+  if (__syncthreads_or(at.live && bad != 0.0f)) {
+#pragma unroll
+    for (int c = 0; c < ND; ++c) dk[c] = dv[c] = f32x16{};
+    begin();
+    for (int h = 0; h < a.rep; ++h)
+      for (int t = t0; t < t1; ++t, ++u) {
+        arrive();
+        if (t < w0 || t >= w1) continue;
+        const uint8_t* q = lds + (u & 3) * SLOT;
+#pragma unroll 1
+        for (int b = 0; b < 2; ++b) {
+          f32x16 s = mul_rows<T, DP>(q + b * 32 * ROW, L, 0, k), ds = mul_rows<T, DP>(q + b * 32 * ROW + TB, L, 0, v);
+          const float* st = (const float*)(lds_s + (u & 3) * STAT) + 32 * b;
+          uint32_t ok = 0;
+#pragma unroll
+          for (int r = 0; r < 16; ++r) {
+            const uint32_t after = t * 64 + 32 * b + acc_row(r) - n;
+            const bool in = after < len;
+            ok |= in ? 1u << r : 0u;
+            s[r] = __builtin_amdgcn_exp2f(fmaf(in ? s[r] : -INFINITY, sl2, -st[acc_row(r)]));
+            ds[r] = in && !(head_of && after == 0) ? s[r] * (ds[r] - st[64 + acc_row(r)]) : 0.0f;
+            s[r] = in ? s[r] : 0.0f;
+          }
+          u32x4 p[NP], e[NP];
+#pragma unroll
+          for (int i = 0; i < NP; ++i) {
+            p[i] = M::frag(s, i);
+            e[i] = M::frag(ds, i);
+          }
+          add_cols<T, DP, true>(dv, q + TB, L, b, p, ok);
+          add_cols<T, DP, true>(dk, q, L, b, e, ok);
+        }
+      }
+  }
+  put_row<T, DP, true>((T*)a.dk.p + kv * a.dk.hs + (int64_t)n * a.dk.ld, dk, a.scale, !at.live, n < a.T, a.d);
+  put_row<T, DP, true>((T*)a.dv.p + kv * a.dv.hs + (int64_t)n * a.dv.ld, dv, 1.0f, !at.live, n < a.T, a.d);
+}
+
 constexpr int32_t ATT_MAX_D = 128;
 constexpr int64_t ATT_MAX_T = ((int64_t)1 << 31) - 65536;
 
@@ -1241,9 +1493,17 @@ extern "C" int agrl_attention_bwd(int64_t T, int32_t n_seq, int32_t n_head, int3
   a.dout = {dout, ld_do, head_do}, a.lse2 = lse2, a.delta = delta;
   a.dq = {dq, ld_dq, head_dq}, a.dk = {dk, ld_dk, head_dk}, a.dv = {dv, ld_dv, head_dv};
   const int64_t tiles = cdiv(T, (int64_t)BM);
+  const bool pipe = dtype == AGRL_BF16 && (d == 64 || d == 128) && copies(a.q) && copies(a.k) && copies(a.v) &&
+                    copies(a.dout);
+  const dim3 kgrid((unsigned)(tiles * n_kv));
+  if (pipe && d == 128)
+    hipLaunchKernelGGL(att_dkv_pipe_kernel<128>, kgrid, dim3(THREADS), 0, s, a);
+  else if (pipe)
+    hipLaunchKernelGGL(att_dkv_pipe_kernel<64>, kgrid, dim3(THREADS), 0, s, a);
   att_pick(dtype, d, [&](auto z, auto dp, auto full) {
-    hipLaunchKernelGGL((att_dkv_kernel<decltype(z), decltype(dp)::value, decltype(full)::value>),
-                       dim3((unsigned)(tiles * n_kv)), dim3(THREADS), 0, s, a);
+    if (!pipe)
+      hipLaunchKernelGGL((att_dkv_kernel<decltype(z), decltype(dp)::value, decltype(full)::value>),
+                         kgrid, dim3(THREADS), 0, s, a);
     hipLaunchKernelGGL((att_dq_kernel<decltype(z), decltype(dp)::value, decltype(full)::value>),
                        dim3((unsigned)(tiles * n_head)), dim3(THREADS), 0, s, a);
   });
