@@ -1348,13 +1348,249 @@ __global__ void __launch_bounds__(THREADS, 1) att_dkv_pipe_kernel(AttArgs a) {
             p[i] = M::frag(s, i);
             e[i] = M::frag(ds, i);
           }
-          add_cols<T, DP, true>(dv, q + TB, L, b, p, ok);
-          add_cols<T, DP, true>(dk, q, L, b, e, ok);
+          add_cols<T, DP, true>(dv, q + b * 32 * ROW + TB, L, 0, p, ok);
+          add_cols<T, DP, true>(dk, q + b * 32 * ROW, L, 0, e, ok);
         }
       }
   }
   put_row<T, DP, true>((T*)a.dk.p + kv * a.dk.hs + (int64_t)n * a.dk.ld, dk, a.scale, !at.live, n < a.T, a.d);
   put_row<T, DP, true>((T*)a.dv.p + kv * a.dv.hs + (int64_t)n * a.dv.ld, dv, 1.0f, !at.live, n < a.T, a.d);
+}
+
+// dq: 64 queries a wave.  A phase forms the next half's S, this half's dP and the previous half's share of dq; on the
+// vector ALU this half's P, then, behind dP, dS.
+template <int DP>
+__global__ void __launch_bounds__(THREADS, 1) att_dq_pipe_kernel(AttArgs a) {
+  using T = uint16_t;
+  using TL = Tile<T, DP>;
+  using M = Mma<T>;
+  constexpr int NS = TL::NS, ND = TL::ND, NP = TL::NP, ROW = TL::ROW, TB = Copy<DP>::BYTES;
+  __shared__ __align__(16) uint8_t lds_k[4 * TB], lds_v[2 * TB];
+  __shared__ int lds_span[2][WAVES];
+  if (a.err) check_offsets(a.start, a.n_seq, a.T, a.err);
+  const int tiles = (a.T + PIPE_ROWS - 1) / PIPE_ROWS;
+  const int tile = tiles - 1 - blockIdx.x / a.n_head, j = blockIdx.x % a.n_head;
+  const int kv = j % a.n_kv, head = kv * a.rep + j / a.n_kv;
+  const int wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6), lane = threadIdx.x & 63;
+  const int first = tile * PIPE_ROWS + wave * 64;
+  const int nA = first + (lane & 31), nB = nA + 32;
+  const int upto0 = offsets_upto(a.start, a.n_seq, first), upto1 = offsets_upto(a.start, a.n_seq, first + 63);
+  const Place at[2] = {Place(a.start, a.n_seq, a.T, upto0, upto1, nA),
+                       Place(a.start, a.n_seq, a.T, upto0, upto1, nB)};
+  const Span part[2] = {query_span(at[0], nA), query_span(at[1], nB)};
+  const Span span = {min(part[0].lo, part[1].lo), max(part[0].hi, part[1].hi),
+                     max(part[0].full_lo, part[1].full_lo), min(part[0].full_hi, part[1].full_hi)};
+  int lo, hi;
+  join(span, lds_span, lo, hi);
+  const int t0 = lo / 64, t1 = lo < hi ? (hi + 63) / 64 : t0;
+  const int w0 = span.lo < span.hi ? span.lo / 64 : t1, w1 = span.lo < span.hi ? (span.hi + 63) / 64 : t0;
+  const int f0 = (span.full_lo + 63) / 64, f1 = span.full_hi / 64;
+
+  const typename TL::Lane L;
+  u32x4 q[2][NS], g[2][NS];
+  float lse2[2], delta[2];
+  uint32_t len[2];
+#pragma unroll
+  for (int cb = 0; cb < 2; ++cb) {
+    const int n = cb ? nB : nA;
+    hold<T, DP, true>(q[cb], (const T*)a.q.p + head * a.q.hs + (int64_t)n * a.q.ld, at[cb].live, a.d);
+    hold<T, DP, true>(g[cb], (const T*)a.dout.p + head * a.dout.hs + (int64_t)n * a.dout.ld, at[cb].live, a.d);
+    lse2[cb] = at[cb].live ? a.lse2[(int64_t)head * a.T + n] : 0.0f;
+    delta[cb] = at[cb].live ? a.delta[(int64_t)head * a.T + n] : 0.0f;
+    len[cb] = at[cb].live ? n - at[cb].begin + 1 : 0;
+  }
+  Copy<DP> ck, cv;
+  ck.init((const T*)a.k.p + kv * a.k.hs, a.k.ld, lds_address(lds_k), wave, a.T);
+  cv.init((const T*)a.v.p + kv * a.v.hs, a.v.ld, lds_address(lds_v), wave, a.T);
+  const float sl2 = a.scale * LOG2E;
+  f32x16 dq[2][ND] = {};
+  constexpr int AHEAD = DP == 128 ? 7 : 3, FR = AHEAD + 1;
+  static_assert(AHEAD <= NS, "what is read ahead of a phase is K");
+  f32x16 s0[2], s1[2], dp[2];
+  u32x4 e0[2][NP], e1[2][NP], fr[FR];
+  int ko[NS], go[NS], vo[ND][2];
+#pragma unroll
+  for (int b = 0; b < 2; ++b) {
+    s0[b] = s1[b] = dp[b] = f32x16{};
+#pragma unroll
+    for (int i = 0; i < NP; ++i) e0[b][i] = e1[b][i] = u32x4{0, 0, 0, 0};
+  }
+#pragma unroll
+  for (int i = 0; i < FR; ++i) fr[i] = u32x4{0, 0, 0, 0};
+  auto read_col = [&](int half, int s, int c) {
+    const uint8_t* x = lds_k + (half * 32 + s * 16) * ROW;
+    const u32x2 u = __builtin_bit_cast(u32x2, __builtin_amdgcn_ds_read_tr16_b64_v4bf16((lds_bf16x4*)(x + vo[c][0])));
+    const u32x2 w = __builtin_bit_cast(u32x2, __builtin_amdgcn_ds_read_tr16_b64_v4bf16((lds_bf16x4*)(x + vo[c][1] + 8 * ROW)));
+    return u32x4{u.x, u.y, w.x, w.y};
+  };
+  auto phase = [&](auto first_c, auto masked_c, f32x16 (&cur)[2], f32x16 (&nxt)[2], u32x4 (&ep)[2][NP],
+                   u32x4 (&en)[2][NP], int move, int gmove, int key0) {
+    constexpr bool FIRST = decltype(first_c)::value, MASKED = decltype(masked_c)::value;
+    // S reads half KH of ko's tile, dP half GH of go's, dq half KH of vo's
+    constexpr int KH = FIRST ? 1 : 0, GH = FIRST ? 0 : 1;
+    constexpr int NQ = 2 * NS, NC = 2 * NP * ND, NM = 2 * NQ + NC, NF = NM / 2, LATE = 2 * NQ + NM / 24;
+    const int from[2] = {key0 + 4 * (lane >> 5) - at[0].begin, key0 + 4 * (lane >> 5) - at[1].begin};
+    slots<NM>([&](auto slot) {
+      constexpr int i = slot.value, fi = i / 2, b = i & 1;
+      if constexpr (b == 0) {
+        constexpr int n = fi + AHEAD;
+        if constexpr (n < NS)
+          fr[n % FR] = *(const u32x4*)(lds_k + KH * 32 * ROW + ko[n]);
+        else if constexpr (n < 2 * NS)
+          fr[n % FR] = *(const u32x4*)(lds_v + GH * 32 * ROW + go[n - NS]);
+        else if constexpr (n < NF)
+          fr[n % FR] = read_col(KH, (n - 2 * NS) / ND, (n - 2 * NS) % ND);
+        else
+          fr[n % FR] = *(const u32x4*)(lds_k + (KH ^ 1) * 32 * ROW + ko[n - NF]);
+      }
+      if constexpr (fi < NS)
+        nxt[b] = M::mma(fr[fi % FR], q[b][fi], fi == 0 ? f32x16{} : nxt[b]);
+      else if constexpr (fi < 2 * NS)
+        dp[b] = M::mma(fr[fi % FR], g[b][fi - NS], fi == NS ? f32x16{} : dp[b]);
+      else
+        dq[b][(fi - 2 * NS) % ND] = M::mma(fr[fi % FR], ep[b][(fi - 2 * NS) / ND], dq[b][(fi - 2 * NS) % ND]);
+      if constexpr (FIRST && i >= NQ && i < NQ + NS) ko[i - NQ] += move;
+      if constexpr (!FIRST && i < 2 * ND) vo[i >> 1][i & 1] += move;
+      if constexpr (!FIRST && i >= 2 * NQ && i < 2 * NQ + NS) go[i - 2 * NQ] += gmove;
+      slots<32>([&](auto e_c) {
+        constexpr int e = e_c.value, cb = e >> 4, r = e & 15, EPS = 16 / NS;
+        constexpr int late = LATE + e * (NM - LATE) / 32;
+        if constexpr (e / EPS == i) {
+          float x = cur[cb][r];
+          if constexpr (MASKED) {
+            const bool in = (uint32_t)(from[cb] + 8 * (r >> 2) + (r & 3)) < len[cb];
+            x = in ? x : -INFINITY;
+          }
+          cur[cb][r] = fmaf(x, sl2, -lse2[cb]);
+        }
+        if constexpr (e / EPS + 1 == i) cur[cb][r] = __builtin_amdgcn_exp2f(cur[cb][r]);
+        if constexpr (late == i) {
+          float x = cur[cb][r] * (dp[cb][r] - delta[cb]);
+          if constexpr (MASKED) {
+            const bool in = (uint32_t)(from[cb] + 8 * (r >> 2) + (r & 3)) < len[cb] && len[cb] > 1;
+            x = in ? x : 0.0f;
+          }
+          cur[cb][r] = x;
+          if constexpr (r & 1) {
+            uint32_t w = M::pack(cur[cb][r - 1], x);
+            asm volatile("" : "+v"(w));                       // (here, not where it is used)
+            en[cb][r >> 3][(r & 7) >> 1] = w;
+          }
+        }
+      });
+      __builtin_amdgcn_sched_barrier(0);
+    });
+  };
+  int u = 0;           // tile t - t0
+  auto begin = [&]() {
+    u = 0;
+    if (t0 >= t1) return;
+    ck.tile(t0 * 64, 0);
+    if (t0 + 1 < t1) ck.tile(t0 * 64 + 64, TB);
+    cv.tile(t0 * 64, 0);
+  };
+  auto arrive = [&](int t) {
+    asm volatile("s_waitcnt vmcnt(0)\n\ts_barrier" ::: "memory");
+    if (t + 2 < t1) ck.tile(t * 64 + 128, (u + 2 & 3) * TB);
+    if (t + 1 < t1) cv.tile(t * 64 + 64, (u + 1 & 1) * TB);
+  };
+  begin();
+  int t = t0;
+  for (; t < min(w0, t1); ++t, ++u) arrive(t);
+  if (t < w1) {
+    arrive(t);
+    const int at_k = (u & 3) * TB;
+#pragma unroll
+    for (int s = 0; s < NS; ++s) {
+      ko[s] = (L.row ^ (s << 5)) + at_k;
+      go[s] = (L.row ^ (s << 5)) + (u & 1) * TB;
+    }
+#pragma unroll
+    for (int c = 0; c < ND; ++c) {
+      vo[c][0] = (L.tr ^ (c << 6)) + at_k;
+      vo[c][1] = (L.tr ^ (c << 6) ^ 32) + at_k;
+    }
+#pragma unroll
+    for (int b = 0; b < 2; ++b) {
+      s0[b] = mul_rows<T, DP>(lds_k + at_k, L, 0, q[b]);
+#pragma unroll
+      for (int i = 0; i < NP; ++i) e1[b][i] = u32x4{0, 0, 0, 0};
+    }
+#pragma unroll
+    for (int i = 0; i < AHEAD; ++i) fr[i] = *(const u32x4*)(lds_k + 32 * ROW + ko[i]);
+    static_assert((2 * NS + NP * ND) % FR == 0, "a phase starts at the ring's first fragment");
+    int vmove = 0;
+    auto through = [&](auto masked_c, int until) {
+      while (t < until) {
+        const int kmove = (u & 3) == 3 ? -3 * TB : TB, gmove = u & 1 ? -TB : TB;
+        phase(std::true_type{}, masked_c, s0, s1, e1, e0, kmove, 0, t * 64);
+        phase(std::false_type{}, masked_c, s1, s0, e0, e1, vmove, gmove, t * 64 + 32);
+        vmove = kmove;
+        ++u;
+        if (++t < w1) arrive(t);
+      }
+    };
+    through(std::true_type{}, min(f0, w1));
+    through(std::false_type{}, min(f1, w1));
+    through(std::true_type{}, w1);
+#pragma unroll
+    for (int s = 0; s < NP; ++s)
+#pragma unroll
+      for (int c = 0; c < ND; ++c) {
+        const u32x4 x = read_col(1, s, c);
+        dq[0][c] = M::mma(x, e1[0][s], dq[0][c]);
+        dq[1][c] = M::mma(x, e1[1][s], dq[1][c]);
+      }
+  }
+  for (; t < t1; ++t, ++u) arrive(t);
+  bool lost = false;
+#pragma unroll
+  for (int cb = 0; cb < 2; ++cb) {
+    float z = 0.0f;
+#pragma unroll
+    for (int c = 0; c < ND; ++c)
+#pragma unroll
+      for (int r = 0; r < 16; ++r) z = fmaf(dq[cb][c][r], 0.0f, z);
+    lost = lost || (at[cb].live && z != 0.0f);
+  }
+  if (__syncthreads_or(lost)) {
+#pragma unroll
+    for (int cb = 0; cb < 2; ++cb)
+#pragma unroll
+      for (int c = 0; c < ND; ++c) dq[cb][c] = f32x16{};
+    begin();
+    for (t = t0; t < t1; ++t, ++u) {
+      arrive(t);
+      const uint8_t *k = lds_k + (u & 3) * TB, *v = lds_v + (u & 1) * TB;
+#pragma unroll
+      for (int cb = 0; cb < 2; ++cb) {
+        if (t * 64 + 64 <= part[cb].lo || t * 64 >= part[cb].hi) continue;
+#pragma unroll 1
+        for (int b = 0; b < 2; ++b) {
+          f32x16 s = mul_rows<T, DP>(k + b * 32 * ROW, L, 0, q[cb]);
+          const f32x16 d = mul_rows<T, DP>(v + b * 32 * ROW, L, 0, g[cb]);
+          uint32_t ok = 0;
+#pragma unroll
+          for (int r = 0; r < 16; ++r) {
+            const bool in = (uint32_t)(t * 64 + 32 * b + acc_row(r) - at[cb].begin) < len[cb];
+            ok |= in ? 1u << r : 0u;
+            s[r] = __builtin_amdgcn_exp2f(fmaf(in ? s[r] : -INFINITY, sl2, -lse2[cb]));
+            s[r] = in && len[cb] > 1 ? s[r] * (d[r] - delta[cb]) : 0.0f;
+          }
+          u32x4 e[NP];
+#pragma unroll
+          for (int i = 0; i < NP; ++i) e[i] = M::frag(s, i);
+          add_cols<T, DP, true>(dq[cb], k + b * 32 * ROW, L, 0, e, ok);
+        }
+      }
+    }
+  }
+#pragma unroll
+  for (int cb = 0; cb < 2; ++cb) {
+    const int n = cb ? nB : nA;
+    put_row<T, DP, true>((T*)a.dq.p + head * a.dq.hs + (int64_t)n * a.dq.ld, dq[cb], a.scale, !at[cb].live, n < a.T,
+                         a.d);
+  }
 }
 
 constexpr int32_t ATT_MAX_D = 128;
@@ -1495,17 +1731,23 @@ extern "C" int agrl_attention_bwd(int64_t T, int32_t n_seq, int32_t n_head, int3
   const int64_t tiles = cdiv(T, (int64_t)BM);
   const bool pipe = dtype == AGRL_BF16 && (d == 64 || d == 128) && copies(a.q) && copies(a.k) && copies(a.v) &&
                     copies(a.dout);
-  const dim3 kgrid((unsigned)(tiles * n_kv));
-  if (pipe && d == 128)
-    hipLaunchKernelGGL(att_dkv_pipe_kernel<128>, kgrid, dim3(THREADS), 0, s, a);
-  else if (pipe)
-    hipLaunchKernelGGL(att_dkv_pipe_kernel<64>, kgrid, dim3(THREADS), 0, s, a);
+  const dim3 kgrid((unsigned)(tiles * n_kv)), block(THREADS);
+  if (pipe) {
+    const dim3 qgrid((unsigned)(cdiv(T, (int64_t)PIPE_ROWS) * n_head));
+    if (d == 128) {
+      hipLaunchKernelGGL(att_dkv_pipe_kernel<128>, kgrid, block, 0, s, a);
+      hipLaunchKernelGGL(att_dq_pipe_kernel<128>, qgrid, block, 0, s, a);
+    } else {
+      hipLaunchKernelGGL(att_dkv_pipe_kernel<64>, kgrid, block, 0, s, a);
+      hipLaunchKernelGGL(att_dq_pipe_kernel<64>, qgrid, block, 0, s, a);
+    }
+    return hip_status(hipGetLastError());
+  }
   att_pick(dtype, d, [&](auto z, auto dp, auto full) {
-    if (!pipe)
-      hipLaunchKernelGGL((att_dkv_kernel<decltype(z), decltype(dp)::value, decltype(full)::value>),
-                         kgrid, dim3(THREADS), 0, s, a);
+    hipLaunchKernelGGL((att_dkv_kernel<decltype(z), decltype(dp)::value, decltype(full)::value>), kgrid, block, 0, s,
+                       a);
     hipLaunchKernelGGL((att_dq_kernel<decltype(z), decltype(dp)::value, decltype(full)::value>),
-                       dim3((unsigned)(tiles * n_head)), dim3(THREADS), 0, s, a);
+                       dim3((unsigned)(tiles * n_head)), block, 0, s, a);
   });
   return hip_status(hipGetLastError());
 }
