@@ -397,6 +397,7 @@ struct AttArgs {
   // backward
   Heads dout;
   const float *lse2, *delta;     // [n_head, T]: lse in powers of 2, sum do o
+  const int32_t* order;          // key tiles in the order they are taken
   HeadsOut dq, dk, dv;
 };
 
@@ -571,13 +572,14 @@ struct Copy {
   uint32_t r, c, off;        // lane's row and byte of the first copy, its offset
   uint32_t lds;
   int T;
-  __device__ __forceinline__ void init(const void* head, int64_t ld, uint32_t lds_base, int wave, int rows) {
+  // (the places past a head of d elements get its last chunk again: they meet zeros, or are not stored)
+  __device__ __forceinline__ void init(const void* head, int64_t ld, uint32_t lds_base, int wave, int rows, int d) {
     const int lane = threadIdx.x & 63;
     p = (const uint8_t*)head;
     ldb = ld * 2;
     T = rows;
     r = wave * RPI + lane / TL::CPR;
-    c = ((lane & (TL::CPR - 1)) ^ TL::sw(r)) << 4;
+    c = min((lane & (TL::CPR - 1)) ^ TL::sw(r), d / 8 - 1) << 4;
     off = r * (uint32_t)ldb + c;
     lds = __builtin_amdgcn_readfirstlane(lds_base + wave * 1024);
   }
@@ -602,7 +604,7 @@ __device__ __forceinline__ uint32_t lds_address(const void* p) {
   return (uint32_t)(uintptr_t)(__attribute__((address_space(3))) const uint8_t*)p;
 }
 
-template <int DP>
+template <int DP, bool FULL>
 __global__ void __launch_bounds__(THREADS, 1) att_fwd_pipe_kernel(AttArgs a) {
   using T = uint16_t;
   using TL = Tile<T, DP>;
@@ -629,11 +631,11 @@ __global__ void __launch_bounds__(THREADS, 1) att_fwd_pipe_kernel(AttArgs a) {
   const typename TL::Lane L;
   u32x4 q[2][NS];
   const T* qp = (const T*)a.q.p + head * a.q.hs;
-  hold<T, DP, true>(q[0], qp + (int64_t)nA * a.q.ld, at[0].live, a.d);
-  hold<T, DP, true>(q[1], qp + (int64_t)nB * a.q.ld, at[1].live, a.d);
+  hold<T, DP, FULL>(q[0], qp + (int64_t)nA * a.q.ld, at[0].live, a.d);
+  hold<T, DP, FULL>(q[1], qp + (int64_t)nB * a.q.ld, at[1].live, a.d);
   Copy<DP> ck, cv;
-  ck.init((const T*)a.k.p + kv * a.k.hs, a.k.ld, lds_address(lds_k), wave, a.T);
-  cv.init((const T*)a.v.p + kv * a.v.hs, a.v.ld, lds_address(lds_v), wave, a.T);
+  ck.init((const T*)a.k.p + kv * a.k.hs, a.k.ld, lds_address(lds_k), wave, a.T, a.d);
+  cv.init((const T*)a.v.p + kv * a.v.hs, a.v.ld, lds_address(lds_v), wave, a.T, a.d);
   const float sl2 = a.scale * LOG2E;
   f32x16 o[2][ND] = {};
   float l[2] = {0.0f, 0.0f}, m[2];
@@ -643,7 +645,7 @@ __global__ void __launch_bounds__(THREADS, 1) att_fwd_pipe_kernel(AttArgs a) {
 #pragma unroll
   for (int cb = 0; cb < 2; ++cb) {
     u32x4 own[NS];
-    hold<T, DP, true>(own, (const T*)a.k.p + kv * a.k.hs + (int64_t)(cb ? nB : nA) * a.k.ld, at[cb].live, a.d);
+    hold<T, DP, FULL>(own, (const T*)a.k.p + kv * a.k.hs + (int64_t)(cb ? nB : nA) * a.k.ld, at[cb].live, a.d);
     float dot = 0.0f;
 #pragma unroll
     for (int s = 0; s < NS; ++s)
@@ -877,7 +879,7 @@ __global__ void __launch_bounds__(THREADS, 1) att_fwd_pipe_kernel(AttArgs a) {
     const int n = cb ? nB : nA;
     if (a.lse && n < a.T && lane < 32)
       a.lse[(int64_t)head * a.T + n] = at[cb].live ? LN2 * (m[cb] + __builtin_amdgcn_logf(l[cb])) : 0.0f;
-    put_row<T, DP, true>((T*)a.o.p + head * a.o.hs + (int64_t)n * a.o.ld, o[cb], 1.0f / l[cb], !at[cb].live,
+    put_row<T, DP, FULL>((T*)a.o.p + head * a.o.hs + (int64_t)n * a.o.ld, o[cb], 1.0f / l[cb], !at[cb].live,
                          n < a.T, a.d);
   }
 }
@@ -885,15 +887,54 @@ __global__ void __launch_bounds__(THREADS, 1) att_fwd_pipe_kernel(AttArgs a) {
 // ------------------------------------------------------------------ backward
 // lse in powers of 2 and D = sum do o, [n_head, T].  A wave takes a token's heads in turn, 16 lanes a head.
 struct DeltaArgs {
-  int32_t T, n_head, d;
+  int32_t T, n_head, d, n_seq;
   Heads o, dout;
   const float* lse;
   float *lse2, *delta;
+  const int32_t* start;
+  int32_t* order;       // [tiles of BM keys], those with the most rows first
 };
+
+// The key tiles by the rows that count them, in 256 classes (the order within one does not matter: each tile's
+// results are its own).  One workgroup.
+__device__ __forceinline__ void order_tiles(const DeltaArgs& a) {
+  constexpr int CLASSES = 256;
+  __shared__ int from[CLASSES], widest;
+  const int tiles = (a.T + BM - 1) / BM;
+  // rows from the tile's first key to the end of its last one's sequence
+  auto rows = [&](int t) {
+    const int last = min(t * BM + BM, a.T) - 1;
+    int lo = 0, hi = a.n_seq + 1;
+    while (lo < hi) {
+      const int mid = lo + ((hi - lo) >> 1);
+      if (a.start[mid] <= last)
+        lo = mid + 1;
+      else
+        hi = mid;
+    }
+    return min(max(lo <= a.n_seq ? a.start[lo] : 0, last), a.T) - t * BM;
+  };
+  from[threadIdx.x] = 0;
+  if (threadIdx.x == 0) widest = 1;
+  __syncthreads();
+  for (int t = threadIdx.x; t < tiles; t += CLASSES) atomicMax(&widest, rows(t));
+  __syncthreads();
+  auto of = [&](int t) { return CLASSES - 1 - (int)((int64_t)rows(t) * (CLASSES - 1) / widest); };
+  for (int t = threadIdx.x; t < tiles; t += CLASSES) atomicAdd(&from[of(t)], 1);
+  __syncthreads();
+  int before = 0;
+  for (int c = 0; c < (int)threadIdx.x; ++c) before += from[c];
+  __syncthreads();
+  from[threadIdx.x] = before;
+  __syncthreads();
+  for (int t = threadIdx.x; t < tiles; t += CLASSES) a.order[atomicAdd(&from[of(t)], 1)] = t;
+}
+
 template <typename T>
 __global__ void __launch_bounds__(256) att_delta_kernel(DeltaArgs a) {
+  if (blockIdx.x == gridDim.x - 1) return order_tiles(a);
   const int l = threadIdx.x & 15, team = threadIdx.x >> 4;
-  for (int64_t i = (int64_t)blockIdx.x * 16 + team; i < (int64_t)a.T * a.n_head; i += (int64_t)gridDim.x * 16) {
+  for (int64_t i = (int64_t)blockIdx.x * 16 + team; i < (int64_t)a.T * a.n_head; i += (int64_t)(gridDim.x - 1) * 16) {
     const int n = (int)(i / a.n_head), h = (int)(i - (int64_t)n * a.n_head);
     const T* o = (const T*)a.o.p + (int64_t)n * a.o.ld + h * a.o.hs;
     const T* g = (const T*)a.dout.p + (int64_t)n * a.dout.ld + h * a.dout.hs;
@@ -1014,7 +1055,7 @@ __global__ void __launch_bounds__(THREADS, 1) att_dkv_kernel(AttArgs a) {
   __shared__ __align__(16) uint8_t lds_q[2][R * TL::ROW], lds_g[2][R * TL::ROW];
   __shared__ __align__(16) float lds_s[2][2][R];     // lse and D of the tile's rows
   __shared__ int lds_span[2][WAVES];
-  const int tile = blockIdx.x / a.n_kv, kv = blockIdx.x % a.n_kv;
+  const int tile = a.order[blockIdx.x / a.n_kv], kv = blockIdx.x % a.n_kv;
   const int wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6), lane = threadIdx.x & 63;
   const int first = tile * BM + wave * 32, n = first + (lane & 31);
   const Place at(a.start, a.n_seq, a.T, offsets_upto(a.start, a.n_seq, first),
@@ -1115,7 +1156,7 @@ __global__ void __launch_bounds__(THREADS, 1) att_dkv_kernel(AttArgs a) {
 // dk, dv: 32 keys a wave.  A phase forms the next half's S and dP, the previous half's shares of dv and dk, and on the
 // vector ALU this half's P and dS.  A ring of four tiles: Q's and do's rows are read a half ahead, their
 // columns a half behind.
-template <int DP>
+template <int DP, bool FULL>
 __global__ void __launch_bounds__(THREADS, 1) att_dkv_pipe_kernel(AttArgs a) {
   using T = uint16_t;
   using TL = Tile<T, DP>;
@@ -1125,7 +1166,7 @@ __global__ void __launch_bounds__(THREADS, 1) att_dkv_pipe_kernel(AttArgs a) {
   __shared__ __align__(16) uint8_t lds[RING];                 // [4][Q, do]
   __shared__ __align__(16) uint8_t lds_s[4 * STAT];           // [4][lse, D][64]
   __shared__ int lds_span[2][WAVES];
-  const int tile = blockIdx.x / a.n_kv, kv = blockIdx.x % a.n_kv;
+  const int tile = a.order[blockIdx.x / a.n_kv], kv = blockIdx.x % a.n_kv;
   const int wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6), lane = threadIdx.x & 63;
   const int first = tile * BM + wave * 32, n = first + (lane & 31);
   const Place at(a.start, a.n_seq, a.T, offsets_upto(a.start, a.n_seq, first),
@@ -1142,11 +1183,11 @@ __global__ void __launch_bounds__(THREADS, 1) att_dkv_pipe_kernel(AttArgs a) {
 
   const typename TL::Lane L;
   u32x4 k[NS], v[NS];
-  hold<T, DP, true>(k, (const T*)a.k.p + kv * a.k.hs + (int64_t)n * a.k.ld, at.live, a.d);
-  hold<T, DP, true>(v, (const T*)a.v.p + kv * a.v.hs + (int64_t)n * a.v.ld, at.live, a.d);
+  hold<T, DP, FULL>(k, (const T*)a.k.p + kv * a.k.hs + (int64_t)n * a.k.ld, at.live, a.d);
+  hold<T, DP, FULL>(v, (const T*)a.v.p + kv * a.v.hs + (int64_t)n * a.v.ld, at.live, a.d);
   Copy<DP> cq, cg;
-  cq.init((const T*)a.q.p + (int64_t)kv * a.rep * a.q.hs, a.q.ld, lds_address(lds), wave, a.T);
-  cg.init((const T*)a.dout.p + (int64_t)kv * a.rep * a.dout.hs, a.dout.ld, lds_address(lds) + TB, wave, a.T);
+  cq.init((const T*)a.q.p + (int64_t)kv * a.rep * a.q.hs, a.q.ld, lds_address(lds), wave, a.T, a.d);
+  cg.init((const T*)a.dout.p + (int64_t)kv * a.rep * a.dout.hs, a.dout.ld, lds_address(lds) + TB, wave, a.T, a.d);
   const float* stats = (threadIdx.x < 64 ? a.lse2 : a.delta) + (int64_t)kv * a.rep * a.T;
   const float sl2 = a.scale * LOG2E;
   f32x16 dk[ND] = {}, dv[ND] = {};
@@ -1353,13 +1394,13 @@ __global__ void __launch_bounds__(THREADS, 1) att_dkv_pipe_kernel(AttArgs a) {
         }
       }
   }
-  put_row<T, DP, true>((T*)a.dk.p + kv * a.dk.hs + (int64_t)n * a.dk.ld, dk, a.scale, !at.live, n < a.T, a.d);
-  put_row<T, DP, true>((T*)a.dv.p + kv * a.dv.hs + (int64_t)n * a.dv.ld, dv, 1.0f, !at.live, n < a.T, a.d);
+  put_row<T, DP, FULL>((T*)a.dk.p + kv * a.dk.hs + (int64_t)n * a.dk.ld, dk, a.scale, !at.live, n < a.T, a.d);
+  put_row<T, DP, FULL>((T*)a.dv.p + kv * a.dv.hs + (int64_t)n * a.dv.ld, dv, 1.0f, !at.live, n < a.T, a.d);
 }
 
 // dq: 64 queries a wave.  A phase forms the next half's S, this half's dP and the previous half's share of dq; on the
 // vector ALU this half's P, then, behind dP, dS.
-template <int DP>
+template <int DP, bool FULL>
 __global__ void __launch_bounds__(THREADS, 1) att_dq_pipe_kernel(AttArgs a) {
   using T = uint16_t;
   using TL = Tile<T, DP>;
@@ -1393,15 +1434,15 @@ __global__ void __launch_bounds__(THREADS, 1) att_dq_pipe_kernel(AttArgs a) {
 #pragma unroll
   for (int cb = 0; cb < 2; ++cb) {
     const int n = cb ? nB : nA;
-    hold<T, DP, true>(q[cb], (const T*)a.q.p + head * a.q.hs + (int64_t)n * a.q.ld, at[cb].live, a.d);
-    hold<T, DP, true>(g[cb], (const T*)a.dout.p + head * a.dout.hs + (int64_t)n * a.dout.ld, at[cb].live, a.d);
+    hold<T, DP, FULL>(q[cb], (const T*)a.q.p + head * a.q.hs + (int64_t)n * a.q.ld, at[cb].live, a.d);
+    hold<T, DP, FULL>(g[cb], (const T*)a.dout.p + head * a.dout.hs + (int64_t)n * a.dout.ld, at[cb].live, a.d);
     lse2[cb] = at[cb].live ? a.lse2[(int64_t)head * a.T + n] : 0.0f;
     delta[cb] = at[cb].live ? a.delta[(int64_t)head * a.T + n] : 0.0f;
     len[cb] = at[cb].live ? n - at[cb].begin + 1 : 0;
   }
   Copy<DP> ck, cv;
-  ck.init((const T*)a.k.p + kv * a.k.hs, a.k.ld, lds_address(lds_k), wave, a.T);
-  cv.init((const T*)a.v.p + kv * a.v.hs, a.v.ld, lds_address(lds_v), wave, a.T);
+  ck.init((const T*)a.k.p + kv * a.k.hs, a.k.ld, lds_address(lds_k), wave, a.T, a.d);
+  cv.init((const T*)a.v.p + kv * a.v.hs, a.v.ld, lds_address(lds_v), wave, a.T, a.d);
   const float sl2 = a.scale * LOG2E;
   f32x16 dq[2][ND] = {};
   constexpr int AHEAD = DP == 128 ? 7 : 3, FR = AHEAD + 1;
@@ -1588,7 +1629,7 @@ __global__ void __launch_bounds__(THREADS, 1) att_dq_pipe_kernel(AttArgs a) {
 #pragma unroll
   for (int cb = 0; cb < 2; ++cb) {
     const int n = cb ? nB : nA;
-    put_row<T, DP, true>((T*)a.dq.p + head * a.dq.hs + (int64_t)n * a.dq.ld, dq[cb], a.scale, !at[cb].live, n < a.T,
+    put_row<T, DP, FULL>((T*)a.dq.p + head * a.dq.hs + (int64_t)n * a.dq.ld, dq[cb], a.scale, !at[cb].live, n < a.T,
                          a.d);
   }
 }
@@ -1618,23 +1659,27 @@ bool copies(const Heads& h) {
   return (uintptr_t)h.p % 16 == 0 && h.ld % 8 == 0 && h.hs % 8 == 0 && h.ld < (1 << 24);
 }
 
+// f(padded head size, whether it is the head size)
+template <class F>
+void att_size(int32_t d, F&& f) {
+  if (d == 128)
+    f(std::integral_constant<int, 128>{}, std::true_type{});
+  else if (d == 64)
+    f(std::integral_constant<int, 64>{}, std::true_type{});
+  else if (d > 64)
+    f(std::integral_constant<int, 128>{}, std::false_type{});
+  else
+    f(std::integral_constant<int, 64>{}, std::false_type{});
+}
 // f(element type, padded head size, whether it is the head size)
 template <class F>
 void att_pick(int32_t dtype, int32_t d, F&& f) {
-  auto with = [&](auto z) {
-    if (d == 128)
-      f(z, std::integral_constant<int, 128>{}, std::true_type{});
-    else if (d == 64)
-      f(z, std::integral_constant<int, 64>{}, std::true_type{});
-    else if (d > 64)
-      f(z, std::integral_constant<int, 128>{}, std::false_type{});
+  att_size(d, [&](auto dp, auto full) {
+    if (dtype == AGRL_BF16)
+      f(uint16_t{}, dp, full);
     else
-      f(z, std::integral_constant<int, 64>{}, std::false_type{});
-  };
-  if (dtype == AGRL_BF16)
-    with(uint16_t{});
-  else
-    with(float{});
+      f(float{}, dp, full);
+  });
 }
 
 }  // namespace
@@ -1659,12 +1704,12 @@ extern "C" int agrl_attention_fwd(int64_t T, int32_t n_seq, int32_t n_head, int3
   a.T = (int32_t)T, a.n_seq = n_seq, a.n_head = n_head, a.n_kv = n_kv, a.rep = n_head / n_kv, a.d = d;
   a.q = {q, ld_q, head_q}, a.k = {k, ld_k, head_k}, a.v = {v, ld_v, head_v};
   a.start = seq_start, a.scale = scale, a.o = {o, ld_o, head_o}, a.lse = lse, a.err = device_error_ptr();
-  if (dtype == AGRL_BF16 && (d == 64 || d == 128) && copies(a.k) && copies(a.v)) {
+  if (dtype == AGRL_BF16 && d % 8 == 0 && copies(a.k) && copies(a.v)) {
     const dim3 grid((unsigned)(cdiv(T, (int64_t)PIPE_ROWS) * n_head));
-    if (d == 128)
-      hipLaunchKernelGGL(att_fwd_pipe_kernel<128>, grid, dim3(THREADS), 0, (hipStream_t)stream, a);
-    else
-      hipLaunchKernelGGL(att_fwd_pipe_kernel<64>, grid, dim3(THREADS), 0, (hipStream_t)stream, a);
+    att_size(d, [&](auto dp, auto full) {
+      hipLaunchKernelGGL((att_fwd_pipe_kernel<decltype(dp)::value, decltype(full)::value>), grid, dim3(THREADS), 0,
+                         (hipStream_t)stream, a);
+    });
     return hip_status(hipGetLastError());
   }
   att_pick(dtype, d, [&](auto z, auto dp, auto full) {
@@ -1680,7 +1725,7 @@ extern "C" size_t agrl_attention_bwd_workspace_size(int64_t T, int32_t n_head, i
   if ((dtype != AGRL_BF16 && dtype != AGRL_F32) || T <= 0 || T > ATT_MAX_T || n_head <= 0 || n_kv <= 0 ||
       n_head % n_kv || d <= 0 || d > ATT_MAX_D || cdiv(T, (int64_t)BM) * n_head >= 0x7fffffff)
     return 0;
-  return (size_t)T * n_head * 2 * sizeof(float);
+  return ((size_t)T * n_head * 2 + (size_t)agrl::cdiv(T, (int64_t)agrl::BM)) * 4;
 }
 
 extern "C" int agrl_attention_bwd(int64_t T, int32_t n_seq, int32_t n_head, int32_t n_kv, int32_t d,
@@ -1715,9 +1760,11 @@ extern "C" int agrl_attention_bwd(int64_t T, int32_t n_seq, int32_t n_head, int3
   hipStream_t s = (hipStream_t)stream;
   float* lse2 = (float*)workspace;
   float* delta = lse2 + T * n_head;
-  const DeltaArgs de = {(int32_t)T, n_head, d, {o, ld_o, head_o}, {dout, ld_do, head_do}, lse, lse2, delta};
+  int32_t* order = (int32_t*)(delta + T * n_head);
+  const DeltaArgs de = {(int32_t)T, n_head, d, n_seq, {o, ld_o, head_o}, {dout, ld_do, head_do}, lse, lse2, delta,
+                        seq_start, order};
   const int64_t need = cdiv(T * n_head, (int64_t)16), most = (int64_t)device_cu_count() * 16;
-  const dim3 dgrid((unsigned)(need < most ? need : most));
+  const dim3 dgrid((unsigned)(need < most ? need : most) + 1);
   if (dtype == AGRL_BF16)
     hipLaunchKernelGGL(att_delta_kernel<uint16_t>, dgrid, dim3(256), 0, s, de);
   else
@@ -1726,21 +1773,19 @@ extern "C" int agrl_attention_bwd(int64_t T, int32_t n_seq, int32_t n_head, int3
   a.T = (int32_t)T, a.n_seq = n_seq, a.n_head = n_head, a.n_kv = n_kv, a.rep = n_head / n_kv, a.d = d;
   a.q = {q, ld_q, head_q}, a.k = {k, ld_k, head_k}, a.v = {v, ld_v, head_v};
   a.start = seq_start, a.scale = scale, a.err = device_error_ptr();
-  a.dout = {dout, ld_do, head_do}, a.lse2 = lse2, a.delta = delta;
+  a.dout = {dout, ld_do, head_do}, a.lse2 = lse2, a.delta = delta, a.order = order;
   a.dq = {dq, ld_dq, head_dq}, a.dk = {dk, ld_dk, head_dk}, a.dv = {dv, ld_dv, head_dv};
   const int64_t tiles = cdiv(T, (int64_t)BM);
-  const bool pipe = dtype == AGRL_BF16 && (d == 64 || d == 128) && copies(a.q) && copies(a.k) && copies(a.v) &&
-                    copies(a.dout);
+  const bool pipe = dtype == AGRL_BF16 && d % 8 == 0 && copies(a.q) && copies(a.k) && copies(a.v) && copies(a.dout);
   const dim3 kgrid((unsigned)(tiles * n_kv)), block(THREADS);
   if (pipe) {
     const dim3 qgrid((unsigned)(cdiv(T, (int64_t)PIPE_ROWS) * n_head));
-    if (d == 128) {
-      hipLaunchKernelGGL(att_dkv_pipe_kernel<128>, kgrid, block, 0, s, a);
-      hipLaunchKernelGGL(att_dq_pipe_kernel<128>, qgrid, block, 0, s, a);
-    } else {
-      hipLaunchKernelGGL(att_dkv_pipe_kernel<64>, kgrid, block, 0, s, a);
-      hipLaunchKernelGGL(att_dq_pipe_kernel<64>, qgrid, block, 0, s, a);
-    }
+    att_size(d, [&](auto dp, auto full) {
+      constexpr int DP = decltype(dp)::value;
+      constexpr bool FULL = decltype(full)::value;
+      hipLaunchKernelGGL((att_dkv_pipe_kernel<DP, FULL>), kgrid, block, 0, s, a);
+      hipLaunchKernelGGL((att_dq_pipe_kernel<DP, FULL>), qgrid, block, 0, s, a);
+    });
     return hip_status(hipGetLastError());
   }
   att_pick(dtype, d, [&](auto z, auto dp, auto full) {

@@ -11,7 +11,7 @@
 //         where its tokens start without asking another workgroup), then it places its
 //         tokens in order.  A wave has a run of consecutive tokens and its own counters,
 //         so the order within an id is the tokens'.
-//   rows  The sorted tokens in chunks of 32, each row's run of tokens added up in registers.
+//   rows  The sorted tokens in chunks of 32 (few: of 8), each row's run of tokens added up in registers.
 //         A run that lies within its chunk goes to dW, a piece of one that crosses into
 //         another chunk to a partial sum (a separator's run is thousands of tokens: it
 //         is added by as many workgroups).  The rows of ids that do not occur are cleared by
@@ -81,7 +81,8 @@ __global__ void __launch_bounds__(256) embed_fwd_kernel(EmbedArgs a) {
 // ------------------------------------------------------------------ backward
 constexpr int SORT_WAVES = 16;
 constexpr int MAX_RANGE = 512;         // ids per workgroup: 32 KiB of counters
-constexpr int CHUNK = 32;              // sorted tokens per chunk
+constexpr int MAX_CHUNK = 32;          // sorted tokens per chunk, and of a small call
+constexpr int MIN_CHUNK = 8;
 constexpr int SLAB = 1024;             // columns per workgroup, four a lane
 constexpr int ZROWS = 8;               // rows that a clearing workgroup looks at
 
@@ -92,6 +93,7 @@ struct SortArgs {
   const uint8_t* live;
   int2* sorted;          // [T] token, id
   int32_t* row_start;    // [V + 1] first sorted token of each id
+  int32_t* crossing;     // number of runs that cross into another chunk: cleared here
   int* err;
 };
 
@@ -108,27 +110,36 @@ __global__ void __launch_bounds__(64 * SORT_WAVES) embed_sort_kernel(SortArgs a)
   const int wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6);
   const int lo = blockIdx.x * a.range, hi = min(lo + a.range, a.V);
   for (int i = threadIdx.x; i < SORT_WAVES * a.range; i += 64 * SORT_WAVES) cnt[i] = 0;
+  if (blockIdx.x == 0 && threadIdx.x == 0) *a.crossing = 0;
   __syncthreads();
   int* own = cnt + wave * a.range;
   const int64_t per = cdiv(cdiv(a.T, (int64_t)SORT_WAVES), (int64_t)64) * 64;
   const int64_t t0 = wave * per, t1 = min(a.T, t0 + per);
   constexpr int NONE = 0x7fffffff;
   constexpr int AHEAD = 16;                          // loads in flight
-  // a token's id, or NONE for dead tokens and ids out of range
-  auto fetch = [&](int64_t t) {
-    if (t >= t1 || (a.live && a.live[t] == 0)) return NONE;
-    const int id = a.id[t];
-    if (id < 0 || id >= a.V) {
-      if (blockIdx.x == 0) set_error(a.err, ERR_TOKEN_ID);
-      return NONE;
+  // the ids of tokens t, t + 64, ..: NONE for dead tokens and ids out of range.  (All loads first, from
+  // clamped places: behind a branch each would wait for the one before)
+  auto fetch = [&](int64_t t, int (&id)[AHEAD]) {
+    uint8_t live[AHEAD];
+#pragma unroll
+    for (int k = 0; k < AHEAD; ++k) {
+      const int64_t at = min(t + 64 * k, a.T - 1);
+      id[k] = a.id[at];
+      live[k] = a.live ? a.live[at] : 1;
     }
-    return id;
+    bool bad = false;
+#pragma unroll
+    for (int k = 0; k < AHEAD; ++k) {
+      const bool in = t + 64 * k < t1 && live[k] != 0, ok = id[k] >= 0 && id[k] < a.V;
+      bad = bad || (in && !ok);
+      id[k] = in && ok ? id[k] : NONE;
+    }
+    if (bad && blockIdx.x == 0) set_error(a.err, ERR_TOKEN_ID);
   };
   int below = 0;
   for (int64_t t = t0 + lane; t < t1 + lane; t += 64 * AHEAD) {
     int id[AHEAD];
-#pragma unroll
-    for (int k = 0; k < AHEAD; ++k) id[k] = fetch(t + 64 * k);
+    fetch(t, id);
 #pragma unroll
     for (int k = 0; k < AHEAD; ++k) {
       below += id[k] < lo;
@@ -165,22 +176,24 @@ __global__ void __launch_bounds__(64 * SORT_WAVES) embed_sort_kernel(SortArgs a)
   __syncthreads();
   for (int64_t t = t0 + lane; t < t1 + lane; t += 64 * AHEAD) {
     int id[AHEAD];
-#pragma unroll
-    for (int k = 0; k < AHEAD; ++k) id[k] = fetch(t + 64 * k);
+    fetch(t, id);
 #pragma unroll
     for (int k = 0; k < AHEAD; ++k) {
-      uint64_t todo = __ballot(id[k] >= lo && id[k] < hi);
-      while (todo) {
-        const int lead = __builtin_ctzll(todo);
-        const int v = __builtin_amdgcn_readlane(id[k], lead);
-        const uint64_t same = __ballot(id[k] == v);
-        const int at = own[v - lo];
-        if (id[k] == v)
-          a.sorted[at + __popcll(same & (((uint64_t)1 << lane) - 1))] = make_int2((int)(t + 64 * k), v);
-        if (lane == lead) own[v - lo] = at + __popcll(same);
-        __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");    // (the wave's LDS accesses are in order)
-        todo &= ~same;
+      const int v = id[k] - lo;
+      const bool in = id[k] >= lo && id[k] < hi;
+      uint64_t same = __ballot(in);
+      if (!same) continue;
+      // the wave's tokens with the lane's id: those that agree in each of its bits
+      for (int b = 0; 1 << b < a.range; ++b) {
+        const uint64_t set = __ballot(v >> b & 1);
+        same &= v >> b & 1 ? set : ~set;
       }
+      if (in) {
+        const int at = own[v], rank = __popcll(same & (((uint64_t)1 << lane) - 1));
+        a.sorted[at + rank] = make_int2((int)(t + 64 * k), id[k]);
+        if (rank == 0) own[v] = at + __popcll(same);
+      }
+      __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");    // (the wave's LDS accesses are in order)
     }
   }
 }
@@ -217,7 +230,7 @@ __device__ __forceinline__ void store4(float* p, f32x4 v, int n) {
 }
 
 struct RowsArgs {
-  int32_t d, V, slabs, accumulate;
+  int32_t d, V, slabs, accumulate, chunk;
   int64_t chunks;
   const void* dy;
   int64_t ld_dy;
@@ -225,17 +238,11 @@ struct RowsArgs {
   const int2* sorted;
   const int32_t* row_start;
   float* part;           // [chunks][2][d]: the piece that comes in, the piece that goes out
+  int32_t* crossing;     // number of runs that go on in another chunk, and each's first chunk (in any order)
   float* dw;
 };
 
-__device__ __forceinline__ void put_row(const RowsArgs& a, int v, int col, int n, f32x4 sum) {
-  float* p = a.dw + (int64_t)v * a.d + col;
-  sum *= a.scale;
-  if (a.accumulate) sum += load4(p, n);
-  store4(p, sum, n);
-}
-
-template <typename Y>
+template <typename Y, bool ADD>
 __global__ void __launch_bounds__(256) embed_rows_kernel(RowsArgs a) {
   const int64_t adding = a.chunks * a.slabs;
   if (blockIdx.x >= adding) {
@@ -250,37 +257,44 @@ __global__ void __launch_bounds__(256) embed_rows_kernel(RowsArgs a) {
   const int64_t c = blockIdx.x / a.slabs;
   const int col = (int)(blockIdx.x - c * a.slabs) * SLAB + threadIdx.x * 4;
   const int total = a.row_start[a.V];
-  const int64_t p0 = c * CHUNK;
+  const int64_t p0 = c * a.chunk;
   if (p0 >= total) return;
-  const int n = (int)min((int64_t)CHUNK, total - p0);
-  __shared__ int tok[CHUNK], ids[CHUNK + 2];         // ids[k + 1]: of the chunk's token k
-  if (threadIdx.x < CHUNK + 2) {
+  const int n = (int)min((int64_t)a.chunk, total - p0);
+  __shared__ int tok[MAX_CHUNK], ids[MAX_CHUNK + 2];         // ids[k + 1]: of the chunk's token k
+  if (threadIdx.x < a.chunk + 2) {
     const int64_t p = p0 + threadIdx.x - 1;
     const int2 s = p >= 0 && p < total ? a.sorted[p] : make_int2(0, -1);
     ids[threadIdx.x] = s.y;
-    if (threadIdx.x >= 1 && threadIdx.x <= CHUNK) tok[threadIdx.x - 1] = s.x;
+    if (threadIdx.x >= 1 && threadIdx.x <= a.chunk) tok[threadIdx.x - 1] = s.x;
   }
   __syncthreads();
+  auto id = [&](int k) { return __builtin_amdgcn_readfirstlane(ids[k + 1]); };
+  if (col == 0 && id(n - 1) == id(n) && a.row_start[id(n)] >= p0)
+    a.crossing[1 + atomicAdd(a.crossing, 1)] = (int)c;
   const int left = a.d - col;
   if (left <= 0) return;
   f32x4 sum = {0.0f, 0.0f, 0.0f, 0.0f};
-  bool in = __builtin_amdgcn_readfirstlane(ids[0]) == __builtin_amdgcn_readfirstlane(ids[1]);
+  bool in = id(-1) == id(0);                         // the run came in from the chunk before
   for (int k0 = 0; k0 < n; k0 += 8) {
-    f32x4 x[8];
+    f32x4 x[8], old[8];
+    // (the rows that the sums are added to come with them, not one after another when a run ends)
 #pragma unroll
     for (int k = 0; k < 8; ++k) {
       const int64_t t = __builtin_amdgcn_readfirstlane(tok[min(k0 + k, n - 1)]);
       x[k] = load4((const Y*)a.dy + t * a.ld_dy + col, left);
+      old[k] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
+      if constexpr (ADD)
+        if (k0 + k < n && id(k0 + k) != id(k0 + k + 1))
+          old[k] = load4(a.dw + (int64_t)id(k0 + k) * a.d + col, left);
     }
 #pragma unroll
     for (int k = 0; k < 8; ++k) {
       if (k0 + k >= n) break;
       sum += x[k];
-      const int v = __builtin_amdgcn_readfirstlane(ids[k0 + k + 1]);
-      const bool same = v == __builtin_amdgcn_readfirstlane(ids[k0 + k + 2]);
+      const bool same = id(k0 + k) == id(k0 + k + 1);
       if (same && k0 + k + 1 < n) continue;
       if (!in && !same)
-        put_row(a, v, col, left, sum);
+        store4(a.dw + (int64_t)id(k0 + k) * a.d + col, old[k] + sum * a.scale, left);
       else
         store4(a.part + (2 * c + (in ? 0 : 1)) * a.d + col, sum, left);
       in = false;
@@ -289,42 +303,57 @@ __global__ void __launch_bounds__(256) embed_rows_kernel(RowsArgs a) {
   }
 }
 
-// A run that starts in chunk c and goes on: its pieces in order.
+// The runs that cross: their pieces in order, 256 columns a workgroup, its four waves every fourth piece.
 __global__ void __launch_bounds__(256) embed_join_kernel(RowsArgs a) {
-  const int64_t c = blockIdx.x / a.slabs;
-  const int col = (int)(blockIdx.x - c * a.slabs) * SLAB + threadIdx.x * 4;
-  const int64_t p1 = (c + 1) * CHUNK;
-  if (p1 >= a.row_start[a.V]) return;
-  const int v = a.sorted[p1].y;
-  const int64_t first = a.row_start[v];
-  if (first >= p1 || first < c * CHUNK) return;      // no run goes on, or it came in from before
-  const int left = a.d - col;
-  if (left <= 0) return;
-  const int64_t last = ((int64_t)a.row_start[v + 1] - 1) / CHUNK;
-  f32x4 sum = load4(a.part + (2 * c + 1) * a.d + col, left);
-  const float* p = a.part + (2 * c + 2) * a.d + col;
-#pragma unroll 8
-  for (int64_t k = c + 1; k <= last; ++k, p += 2 * (int64_t)a.d) sum += load4(p, left);
-  put_row(a, v, col, left, sum);
+  constexpr int COLS = 256;
+  __shared__ f32x4 sums[3][64];
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, cols = (a.d + COLS - 1) / COLS;
+  const int64_t items = (int64_t)*a.crossing * cols;
+  for (int64_t i = blockIdx.x; i < items; i += gridDim.x) {
+    const int64_t c = a.crossing[1 + i / cols];
+    const int col = (int)(i % cols) * COLS + lane * 4, left = a.d - col;
+    const int v = a.sorted[(c + 1) * a.chunk].y;
+    const int64_t last = ((int64_t)a.row_start[v + 1] - 1) / a.chunk;
+    f32x4 sum = {0.0f, 0.0f, 0.0f, 0.0f}, old = sum;
+    if (left > 0) {
+      if (wave == 0 && a.accumulate) old = load4(a.dw + (int64_t)v * a.d + col, left);
+#pragma unroll 4
+      for (int64_t k = c + wave; k <= last; k += 4)
+        sum += load4(a.part + (2 * k + (k == c ? 1 : 0)) * a.d + col, left);
+    }
+    if (wave) sums[wave - 1][lane] = sum;
+    __syncthreads();
+    if (wave == 0 && left > 0) {
+      sum = (sum + sums[0][lane]) + (sums[1][lane] + sums[2][lane]);
+      store4(a.dw + (int64_t)v * a.d + col, old + sum * a.scale, left);
+    }
+    __syncthreads();
+  }
+}
+
+// Tokens per chunk: few tokens in chunks of 8, so that they fill the chip
+int chunk_of(int64_t T, int32_t d) {
+  return cdiv(T, (int64_t)MAX_CHUNK) * cdiv(d, SLAB) < 1024 ? MIN_CHUNK : MAX_CHUNK;
 }
 
 struct Space {
-  size_t sorted, starts, part, total;
+  size_t sorted, starts, crossing, part, total;
 };
 Space embed_space(int64_t T, int32_t d, int32_t V) {
   auto up = [](size_t n) { return (n + 255) & ~(size_t)255; };
   Space s;
   s.sorted = 0;
   s.starts = up((size_t)T * sizeof(int2));
-  s.part = s.starts + up(((size_t)V + 1) * 4);
-  s.total = s.part + (size_t)cdiv(T, (int64_t)CHUNK) * 2 * d * 4;
+  s.crossing = s.starts + up(((size_t)V + 1) * 4);
+  s.part = s.crossing + up(((size_t)cdiv(T, (int64_t)chunk_of(T, d)) + 1) * 4);
+  s.total = s.part + (size_t)cdiv(T, (int64_t)chunk_of(T, d)) * 2 * d * 4;
   return s;
 }
 
 // every launch within the grid's 2^31 workgroups
 bool embed_sizes(int64_t T, int32_t d, int32_t V) {
   return T >= 0 && T <= MAX_TOKENS && d > 0 && d <= (1 << 20) && V > 0 && V < 0x7fffffff &&
-         cdiv(T, (int64_t)CHUNK) * cdiv(d, SLAB) + cdiv(V, ZROWS) < 0x7fffffff;
+         cdiv(T, (int64_t)MIN_CHUNK) * cdiv(d, SLAB) + cdiv(V, ZROWS) < 0x7fffffff;
 }
 
 }  // namespace
@@ -391,17 +420,24 @@ extern "C" int agrl_token_embed_bwd(int64_t T, int32_t d, int32_t V, int32_t dy_
   // another is then as little as can be
   const int fair = cdiv(V, device_cu_count());
   const SortArgs so = {T, V, fair < MAX_RANGE ? fair : MAX_RANGE, token_id, live_mask, sorted, starts,
-                       device_error_ptr()};
+                       (int32_t*)(ws + sp.crossing), device_error_ptr()};
   hipLaunchKernelGGL(embed_sort_kernel, dim3(cdiv(V, so.range)), dim3(64 * SORT_WAVES),
                      SORT_WAVES * so.range * 4, s, so);
-  const RowsArgs r = {d, V, cdiv(d, SLAB), accumulate, cdiv(T, (int64_t)CHUNK), dy, ld_dy, scale,
-                      sorted, starts, (float*)(ws + sp.part), dweight};
+  const int chunk = chunk_of(T, d);
+  const RowsArgs r = {d, V, cdiv(d, SLAB), accumulate, chunk, cdiv(T, (int64_t)chunk), dy, ld_dy, scale,
+                      sorted, starts, (float*)(ws + sp.part), so.crossing, dweight};
   const dim3 grid((unsigned)(r.chunks * r.slabs + (accumulate ? 0 : cdiv(V, ZROWS)))), block(256);
-  if (dy_dtype == AGRL_BF16)
-    hipLaunchKernelGGL(embed_rows_kernel<uint16_t>, grid, block, 0, s, r);
+  if (dy_dtype == AGRL_BF16 && accumulate)
+    hipLaunchKernelGGL((embed_rows_kernel<uint16_t, true>), grid, block, 0, s, r);
+  else if (dy_dtype == AGRL_BF16)
+    hipLaunchKernelGGL((embed_rows_kernel<uint16_t, false>), grid, block, 0, s, r);
+  else if (accumulate)
+    hipLaunchKernelGGL((embed_rows_kernel<float, true>), grid, block, 0, s, r);
   else
-    hipLaunchKernelGGL(embed_rows_kernel<float>, grid, block, 0, s, r);
-  if (r.chunks > 1)
-    hipLaunchKernelGGL(embed_join_kernel, dim3((unsigned)((r.chunks - 1) * r.slabs)), block, 0, s, r);
+    hipLaunchKernelGGL((embed_rows_kernel<float, false>), grid, block, 0, s, r);
+  if (r.chunks > 1) {
+    const int64_t most = (int64_t)device_cu_count() * 4, need = (r.chunks - 1) * cdiv(d, 256);
+    hipLaunchKernelGGL(embed_join_kernel, dim3((unsigned)(need < most ? need : most)), block, 0, s, r);
+  }
   return hip_status(hipGetLastError());
 }
