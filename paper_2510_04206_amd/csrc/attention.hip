@@ -1153,6 +1153,12 @@ __global__ void __launch_bounds__(THREADS, 1) att_dkv_kernel(AttArgs a) {
 // a reference; a result that is not finite sends the workgroup through its tile again, step by step
 // with masked elements taken out.
 
+// lane R of the lane's group of 16, as an operand
+template <int R>
+__device__ __forceinline__ float row_lane(float v) {
+  return __int_as_float(__builtin_amdgcn_update_dpp(0, __float_as_int(v), 0x150 + R, 0xf, 0xf, false));
+}
+
 // dk, dv: 32 keys a wave.  A phase forms the next half's S and dP, the previous half's shares of dv and dk, and on the
 // vector ALU this half's P and dS.  A ring of four tiles: Q's and do's rows are read a half ahead, their
 // columns a half behind.
@@ -1194,7 +1200,7 @@ __global__ void __launch_bounds__(THREADS, 1) att_dkv_pipe_kernel(AttArgs a) {
   constexpr int AHEAD = 7, FR = AHEAD + 1;
   f32x16 s0 = {}, s1 = {}, d0 = {}, d1 = {};
   u32x4 p0[NP], p1[NP], e0[NP], e1[NP], fr[FR];
-  f32x4 zt[2], dt[2];
+  float zc = 0.0f, gc = 0.0f, zn, gn;      // lse / scale and D of this half and the next one
   int ko[NS], vo[ND][2], so = 0;
 #pragma unroll
   for (int i = 0; i < NP; ++i) p0[i] = p1[i] = e0[i] = e1[i] = u32x4{0, 0, 0, 0};
@@ -1207,9 +1213,11 @@ __global__ void __launch_bounds__(THREADS, 1) att_dkv_pipe_kernel(AttArgs a) {
     const u32x2 w = __builtin_bit_cast(u32x2, __builtin_amdgcn_ds_read_tr16_b64_v4bf16((lds_bf16x4*)(x + vo[c][1] + 8 * ROW)));
     return u32x4{u.x, u.y, w.x, w.y};
   };
-  auto read_stat = [&](int half, int g) {
-    zt[g & 1] = *(const f32x4*)(lds_s + so + half * 128 + g * 32);
-    dt[g & 1] = *(const f32x4*)(lds_s + so + half * 128 + g * 32 + 256);
+  // Row statistics of a half: lane r of a group of 16 reads those of accumulator row r, and the VALU's own broadcast
+  // within 16 lanes hands them out (16-byte reads by every lane were a fifth of the LDS's time)
+  auto read_stat = [&](int half) {
+    zn = *(const float*)(lds_s + so + half * 128);
+    gn = *(const float*)(lds_s + so + half * 128 + 256);
   };
   // this half's P and dS from s, d into pn, en; the next half's scores and dP into sn, dn; the previous half's pp, ep
   // into dv and dk.  move: as in the forward, so after its last read of the tile.
@@ -1247,12 +1255,12 @@ __global__ void __launch_bounds__(THREADS, 1) att_dkv_pipe_kernel(AttArgs a) {
         bool in = true;
         if constexpr (MASKED) in = from + 8 * (r >> 2) + (r & 3) < len;
         if constexpr (sl == i) {
+          x = (x - row_lane<r>(zc)) * sl2;
           if constexpr (MASKED) x = in ? x : -INFINITY;
-          x = fmaf(x, sl2, -zt[(r >> 2) & 1][r & 3]);
         }
         if constexpr (sl + 1 == i || (sl == i && i + 1 == NM)) {
           x = __builtin_amdgcn_exp2f(x);
-          y = x * (y - dt[(r >> 2) & 1][r & 3]);
+          y = x * (y - row_lane<r>(gc));
           if constexpr (MASKED) y = in && !(head_of && from + 8 * (r >> 2) + (r & 3) == 0) ? y : 0.0f;
           if constexpr (r & 1) {
             uint32_t w = M::pack(s[r - 1], x), z = M::pack(d[r - 1], y);
@@ -1264,97 +1272,103 @@ __global__ void __launch_bounds__(THREADS, 1) att_dkv_pipe_kernel(AttArgs a) {
         s[r] = x;
         d[r] = y;
       });
-      // the row statistics, four rows at a time (behind the last value that used the two places)
-      constexpr int G = NM / 4;
-      if constexpr (i % G == 0 && i / G < 3) read_stat(FIRST ? 0 : 1, i / G + 1);
-      if constexpr (i == 3 * G) {
+      if constexpr (i == NM / 2) {
         if constexpr (!FIRST) so += smove;
-        read_stat(FIRST ? 1 : 0, 0);
+        read_stat(FIRST ? 1 : 0);
       }
       __builtin_amdgcn_sched_barrier(0);
     });
+    zc = zn;
+    gc = gn;
   };
 
+  // Step u of the walk: all heads of the group at one tile, from the last tile to the first.  Key tiles of one sequence
+  // then start on the same rows and stay with each other, sharing them through the XCD's L2.
   float stat = 0.0f;
+  const float to_stat = threadIdx.x < 64 ? 1.0f / sl2 : 1.0f;
   auto load_stat = [&](int u) {
-    const int row = (t0 + u % per) * 64 + (threadIdx.x & 63);
-    if (threadIdx.x < 128 && u < steps && row < a.T) stat = stats[(int64_t)(u / per) * a.T + row];
+    const int row = (t1 - 1 - u / a.rep) * 64 + (threadIdx.x & 63);
+    if (threadIdx.x < 128 && u < steps && row < a.T) stat = stats[(int64_t)(u % a.rep) * a.T + row];
   };
   auto put_stat = [&](int u) {
-    if (threadIdx.x < 128) *(float*)(lds_s + (u & 3) * STAT + threadIdx.x * 4) = stat;
+    if (threadIdx.x < 128) *(float*)(lds_s + (u & 3) * STAT + threadIdx.x * 4) = stat * to_stat;
   };
   auto copy = [&](int u) {
     if (u >= steps) return;
-    const int h = u / per, row = (t0 + u - h * per) * 64;
+    const int up = u / a.rep, h = u - up * a.rep, row = (t1 - 1 - up) * 64;
     cq.tile(row, (u & 3) * SLOT, (int64_t)h * a.q.hs * 2);
     cg.tile(row, (u & 3) * SLOT, (int64_t)h * a.dout.hs * 2);
   };
-  int u = 0;           // the tile in turn, over all heads
   auto begin = [&]() {
-    u = 0;
     if (steps == 0) return;
     load_stat(0);
     put_stat(0);
     load_stat(1);
+    put_stat(1);
+    load_stat(2);
     copy(0);
     copy(1);
+    asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
   };
-  // tile u and the next one have landed, the one after is on its way
-  auto arrive = [&]() {
-    asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
-    put_stat(u + 1);
-    asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory");
-    load_stat(u + 2);
+  // Step u's rows and the next one's have landed, those of the one after are on their way.  Statistics are written two
+  // steps ahead: a wave that reads fragments in between has seen its write done before the next barrier,
+  // and needs no wait that would drain them; one that does not (idle) waits.
+  auto arrive = [&](int u, bool idle) {
+    if (idle) asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+    asm volatile("s_waitcnt vmcnt(0)\n\ts_barrier" ::: "memory");
+    put_stat(u + 2);
+    load_stat(u + 3);
     copy(u + 2);
   };
   begin();
-  for (int h = 0; h < a.rep; ++h) {
-    int t = t0;
-    for (; t < min(w0, t1); ++t, ++u) arrive();
-    if (t < w1) {
-      arrive();
-      const int at_q = (u & 3) * SLOT;
+  const int ua = w0 < w1 ? (t1 - w1) * a.rep : steps, ub = w0 < w1 ? (t1 - w0) * a.rep : steps;
+  int u = 0;
+  for (; u < ua; ++u) arrive(u, true);
+  if (u < ub) {
+    arrive(u, true);
+    const int at_q = (u & 3) * SLOT;
 #pragma unroll
-      for (int s = 0; s < NS; ++s) ko[s] = (L.row ^ (s << 5)) + at_q;
+    for (int s = 0; s < NS; ++s) ko[s] = (L.row ^ (s << 5)) + at_q;
+#pragma unroll
+    for (int c = 0; c < ND; ++c) {
+      vo[c][0] = (L.tr ^ (c << 6)) + at_q;
+      vo[c][1] = (L.tr ^ (c << 6) ^ 32) + at_q;
+    }
+    so = (u & 3) * STAT + (8 * ((lane & 15) >> 2) + (lane & 3) + 4 * (lane >> 5)) * 4;
+    s0 = mul_rows<T, DP>(lds + at_q, L, 0, k);
+    d0 = mul_rows<T, DP>(lds + at_q + TB, L, 0, v);
+#pragma unroll
+    for (int i = 0; i < NP; ++i) p1[i] = e1[i] = u32x4{0, 0, 0, 0};
+    read_stat(0);
+    zc = zn;
+    gc = gn;
+#pragma unroll
+    for (int i = 0; i < AHEAD; ++i)
+      fr[i] = *(const u32x4*)(lds + 32 * ROW + (i < NS ? 0 : TB) + ko[i % NS]);
+    static_assert((2 * NS + 2 * NP * ND) % FR == 0, "a phase starts at the ring's first fragment");
+    int vmove = 0;
+    auto through = [&](auto masked_c, int until) {
+      while (u < until) {
+        const int kmove = (u & 3) == 3 ? -3 * SLOT : SLOT, smove = (u & 3) == 3 ? -3 * STAT : STAT;
+        const int q0 = decltype(masked_c)::value ? (t1 - 1 - u / a.rep) * 64 : 0;
+        phase(std::true_type{}, masked_c, s0, d0, s1, d1, p1, e1, p0, e0, kmove, 0, q0);
+        phase(std::false_type{}, masked_c, s1, d1, s0, d0, p0, e0, p1, e1, vmove, smove, q0 + 32);
+        vmove = kmove;
+        if (++u < ub) arrive(u, false);
+      }
+    };
+    through(std::true_type{}, min((t1 - min(f1, t1)) * a.rep, ub));
+    through(std::false_type{}, min((t1 - min(f0, t1)) * a.rep, ub));
+    through(std::true_type{}, ub);
+#pragma unroll
+    for (int s = 0; s < NP; ++s)
 #pragma unroll
       for (int c = 0; c < ND; ++c) {
-        vo[c][0] = (L.tr ^ (c << 6)) + at_q;
-        vo[c][1] = (L.tr ^ (c << 6) ^ 32) + at_q;
+        dv[c] = M::mma(read_col(32 * ROW + TB, s, c), p1[s], dv[c]);
+        dk[c] = M::mma(read_col(32 * ROW, s, c), e1[s], dk[c]);
       }
-      so = (u & 3) * STAT + 16 * (lane >> 5);
-      s0 = mul_rows<T, DP>(lds + at_q, L, 0, k);
-      d0 = mul_rows<T, DP>(lds + at_q + TB, L, 0, v);
-#pragma unroll
-      for (int i = 0; i < NP; ++i) p1[i] = e1[i] = u32x4{0, 0, 0, 0};
-      read_stat(0, 0);
-#pragma unroll
-      for (int i = 0; i < AHEAD; ++i)
-        fr[i] = *(const u32x4*)(lds + 32 * ROW + (i < NS ? 0 : TB) + ko[i % NS]);
-      static_assert((2 * NS + 2 * NP * ND) % FR == 0, "a phase starts at the ring's first fragment");
-      int vmove = 0;
-      auto through = [&](auto masked_c, int until) {
-        while (t < until) {
-          const int kmove = (u & 3) == 3 ? -3 * SLOT : SLOT, smove = (u & 3) == 3 ? -3 * STAT : STAT;
-          phase(std::true_type{}, masked_c, s0, d0, s1, d1, p1, e1, p0, e0, kmove, 0, t * 64);
-          phase(std::false_type{}, masked_c, s1, d1, s0, d0, p0, e0, p1, e1, vmove, smove, t * 64 + 32);
-          vmove = kmove;
-          ++u;
-          if (++t < w1) arrive();
-        }
-      };
-      through(std::true_type{}, min(f0, w1));
-      through(std::false_type{}, min(f1, w1));
-      through(std::true_type{}, w1);
-#pragma unroll
-      for (int s = 0; s < NP; ++s)
-#pragma unroll
-        for (int c = 0; c < ND; ++c) {
-          dv[c] = M::mma(read_col(32 * ROW + TB, s, c), p1[s], dv[c]);
-          dk[c] = M::mma(read_col(32 * ROW, s, c), e1[s], dk[c]);
-        }
-    }
-    for (; t < t1; ++t, ++u) arrive();
   }
+  for (; u < steps; ++u) arrive(u, true);
   float bad = 0.0f;
 #pragma unroll
   for (int c = 0; c < ND; ++c)
@@ -1364,9 +1378,9 @@ __global__ void __launch_bounds__(THREADS, 1) att_dkv_pipe_kernel(AttArgs a) {
 #pragma unroll
     for (int c = 0; c < ND; ++c) dk[c] = dv[c] = f32x16{};
     begin();
-    for (int h = 0; h < a.rep; ++h)
-      for (int t = t0; t < t1; ++t, ++u) {
-        arrive();
+    for (u = 0; u < steps; ++u) {
+        arrive(u, true);
+        const int t = t1 - 1 - u / a.rep;
         if (t < w0 || t >= w1) continue;
         const uint8_t* q = lds + (u & 3) * SLOT;
 #pragma unroll 1
@@ -1379,7 +1393,7 @@ __global__ void __launch_bounds__(THREADS, 1) att_dkv_pipe_kernel(AttArgs a) {
             const uint32_t after = t * 64 + 32 * b + acc_row(r) - n;
             const bool in = after < len;
             ok |= in ? 1u << r : 0u;
-            s[r] = __builtin_amdgcn_exp2f(fmaf(in ? s[r] : -INFINITY, sl2, -st[acc_row(r)]));
+            s[r] = __builtin_amdgcn_exp2f(in ? (s[r] - st[acc_row(r)]) * sl2 : -INFINITY);
             ds[r] = in && !(head_of && after == 0) ? s[r] * (ds[r] - st[64 + acc_row(r)]) : 0.0f;
             s[r] = in ? s[r] : 0.0f;
           }
