@@ -399,6 +399,8 @@ struct AttArgs {
   const float *lse2, *delta;     // [n_head, T]: lse in powers of 2, sum do o
   const int32_t* order;          // key tiles in the order they are taken
   HeadsOut dq, dk, dv;
+  int32_t splits;                // parts that a group's heads are dealt to, each a workgroup's
+  float* part;                   // more than one: [splits][2][T, n_kv, d] sums of dk and dv
 };
 
 // What a wave's 32 columns need: its range of the other side
@@ -1046,6 +1048,66 @@ __global__ void __launch_bounds__(THREADS, sizeof(T) == 2 ? 2 : 1) att_dq_kernel
   put_row<T, DP, FULL>((T*)a.dq.p + head * a.dq.hs + (int64_t)n * a.dq.ld, dq, a.scale, !at.live, n < a.T, a.d);
 }
 
+// The key tile, key head and query heads of a workgroup; the first ranks' first
+struct KeyTile {
+  int rank, kv, split, head, heads;
+  __device__ __forceinline__ KeyTile(const AttArgs& a, int b) {
+    const int each = a.n_kv * a.splits, j = b % each;
+    rank = b / each;
+    kv = j % a.n_kv;
+    split = j / a.n_kv;
+    const int h0 = split * a.rep / a.splits;
+    head = kv * a.rep + h0;
+    heads = (split + 1) * a.rep / a.splits - h0;
+  }
+};
+
+// dk and dv of the lane's key, or its part of them
+template <typename T, int DP, bool FULL, int ND>
+__device__ __forceinline__ void put_keys(const AttArgs& a, const KeyTile& w, int n, const f32x16 (&dk)[ND],
+                                         const f32x16 (&dv)[ND], bool live) {
+  if (a.splits > 1) {
+    const int64_t all = (int64_t)a.T * a.n_kv * a.d;
+    float* p = a.part + 2 * w.split * all + ((int64_t)n * a.n_kv + w.kv) * a.d;
+    put_row<float, DP, FULL>(p, dk, a.scale, !live, n < a.T, a.d);
+    put_row<float, DP, FULL>(p + all, dv, 1.0f, !live, n < a.T, a.d);
+  } else {
+    put_row<T, DP, FULL>((T*)a.dk.p + w.kv * a.dk.hs + (int64_t)n * a.dk.ld, dk, a.scale, !live, n < a.T, a.d);
+    put_row<T, DP, FULL>((T*)a.dv.p + w.kv * a.dv.hs + (int64_t)n * a.dv.ld, dv, 1.0f, !live, n < a.T, a.d);
+  }
+}
+
+// The parts of dk and dv in order, 8 elements a lane
+template <typename T>
+__global__ void __launch_bounds__(256) att_join_kernel(AttArgs a) {
+  const int per = (a.d + CH - 1) / CH;
+  const int64_t rows = (int64_t)a.T * a.n_kv, all = rows * a.d;
+  for (int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x; i < rows * per; i += (int64_t)gridDim.x * 256) {
+    const int64_t row = i / per, n = row / a.n_kv;
+    const int c = (int)(i - row * per) * CH, kv = (int)(row - n * a.n_kv), some = a.d - c;
+#pragma unroll
+    for (int which = 0; which < 2; ++which) {
+      const float* p = a.part + which * all + row * a.d + c;
+      float f[CH] = {};
+      for (int s = 0; s < a.splits; ++s, p += 2 * all) {
+        Chunk<float> x;
+        if (some >= CH)
+          x.load(p);
+        else
+          x.load_some(p, some);
+#pragma unroll
+        for (int k = 0; k < CH; ++k) f[k] += x.get(k);
+      }
+      const HeadsOut& o = which ? a.dv : a.dk;
+      T* to = (T*)o.p + n * o.ld + kv * o.hs + c;
+      if (some >= CH)
+        Chunk<T>::store(to, f);
+      else
+        Chunk<T>::store_some(to, f, some);
+    }
+  }
+}
+
 // dk and dv: keys in the columns, the rows of Q and do go through LDS, head after head of the group.
 template <typename T, int DP, bool FULL>
 __global__ void __launch_bounds__(THREADS, 1) att_dkv_kernel(AttArgs a) {
@@ -1055,7 +1117,8 @@ __global__ void __launch_bounds__(THREADS, 1) att_dkv_kernel(AttArgs a) {
   __shared__ __align__(16) uint8_t lds_q[2][R * TL::ROW], lds_g[2][R * TL::ROW];
   __shared__ __align__(16) float lds_s[2][2][R];     // lse and D of the tile's rows
   __shared__ int lds_span[2][WAVES];
-  const int tile = a.order[blockIdx.x / a.n_kv], kv = blockIdx.x % a.n_kv;
+  const KeyTile w(a, blockIdx.x);
+  const int tile = a.order[w.rank], kv = w.kv, reps = w.heads;
   const int wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6), lane = threadIdx.x & 63;
   const int first = tile * BM + wave * 32, n = first + (lane & 31);
   const Place at(a.start, a.n_seq, a.T, offsets_upto(a.start, a.n_seq, first),
@@ -1076,9 +1139,9 @@ __global__ void __launch_bounds__(THREADS, 1) att_dkv_kernel(AttArgs a) {
   f32x16 dk[TL::ND] = {}, dv[TL::ND] = {};
   Stage<T, DP, R, THREADS, FULL> sq, sg;
   float stat = 0.0f;
-  const int t0 = lo / R * R, per = lo < hi ? (hi - t0 + R - 1) / R : 0, steps = per * a.rep;
+  const int t0 = lo / R * R, per = lo < hi ? (hi - t0 + R - 1) / R : 0, steps = per * w.heads;
   auto load = [&](int i) {
-    const int head = kv * a.rep + i / per, q0 = t0 + (i - i / per * per) * R;
+    const int head = w.head + i / per, q0 = t0 + (i - i / per * per) * R;
     sq.load((const T*)a.q.p + head * a.q.hs, a.q.ld, q0, a.T, a.d);
     sg.load((const T*)a.dout.p + head * a.dout.hs, a.dout.ld, q0, a.T, a.d);
     const int r = q0 + (threadIdx.x & (R - 1));
@@ -1143,8 +1206,7 @@ __global__ void __launch_bounds__(THREADS, 1) att_dkv_kernel(AttArgs a) {
     if (i + 1 < steps) store(buf ^ 1);
     __syncthreads();
   }
-  put_row<T, DP, FULL>((T*)a.dk.p + kv * a.dk.hs + (int64_t)n * a.dk.ld, dk, a.scale, !at.live, n < a.T, a.d);
-  put_row<T, DP, FULL>((T*)a.dv.p + kv * a.dv.hs + (int64_t)n * a.dv.ld, dv, 1.0f, !at.live, n < a.T, a.d);
+  put_keys<T, DP, FULL>(a, w, n, dk, dv, at.live);
 }
 
 // ------------------------------------------------------------------ backward, pipelined
@@ -1172,7 +1234,8 @@ __global__ void __launch_bounds__(THREADS, 1) att_dkv_pipe_kernel(AttArgs a) {
   __shared__ __align__(16) uint8_t lds[RING];                 // [4][Q, do]
   __shared__ __align__(16) uint8_t lds_s[4 * STAT];           // [4][lse, D][64]
   __shared__ int lds_span[2][WAVES];
-  const int tile = a.order[blockIdx.x / a.n_kv], kv = blockIdx.x % a.n_kv;
+  const KeyTile w(a, blockIdx.x);
+  const int tile = a.order[w.rank], kv = w.kv, reps = w.heads;
   const int wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6), lane = threadIdx.x & 63;
   const int first = tile * BM + wave * 32, n = first + (lane & 31);
   const Place at(a.start, a.n_seq, a.T, offsets_upto(a.start, a.n_seq, first),
@@ -1183,7 +1246,7 @@ __global__ void __launch_bounds__(THREADS, 1) att_dkv_pipe_kernel(AttArgs a) {
   const bool head_of = at.live && at.begin == n;
   int lo, hi;
   join(span, lds_span, lo, hi);
-  const int t0 = lo / 64, t1 = lo < hi ? (hi + 63) / 64 : t0, per = t1 - t0, steps = per * a.rep;
+  const int t0 = lo / 64, t1 = lo < hi ? (hi + 63) / 64 : t0, per = t1 - t0, steps = per * reps;
   const int w0 = span.lo < span.hi ? span.lo / 64 : t1, w1 = span.lo < span.hi ? (span.hi + 63) / 64 : t0;
   const int f0 = (span.full_lo + 63) / 64, f1 = span.full_hi / 64;
 
@@ -1192,9 +1255,9 @@ __global__ void __launch_bounds__(THREADS, 1) att_dkv_pipe_kernel(AttArgs a) {
   hold<T, DP, FULL>(k, (const T*)a.k.p + kv * a.k.hs + (int64_t)n * a.k.ld, at.live, a.d);
   hold<T, DP, FULL>(v, (const T*)a.v.p + kv * a.v.hs + (int64_t)n * a.v.ld, at.live, a.d);
   Copy<DP> cq, cg;
-  cq.init((const T*)a.q.p + (int64_t)kv * a.rep * a.q.hs, a.q.ld, lds_address(lds), wave, a.T, a.d);
-  cg.init((const T*)a.dout.p + (int64_t)kv * a.rep * a.dout.hs, a.dout.ld, lds_address(lds) + TB, wave, a.T, a.d);
-  const float* stats = (threadIdx.x < 64 ? a.lse2 : a.delta) + (int64_t)kv * a.rep * a.T;
+  cq.init((const T*)a.q.p + (int64_t)w.head * a.q.hs, a.q.ld, lds_address(lds), wave, a.T, a.d);
+  cg.init((const T*)a.dout.p + (int64_t)w.head * a.dout.hs, a.dout.ld, lds_address(lds) + TB, wave, a.T, a.d);
+  const float* stats = (threadIdx.x < 64 ? a.lse2 : a.delta) + (int64_t)w.head * a.T;
   const float sl2 = a.scale * LOG2E;
   f32x16 dk[ND] = {}, dv[ND] = {};
   constexpr int AHEAD = 7, FR = AHEAD + 1;
@@ -1287,15 +1350,15 @@ __global__ void __launch_bounds__(THREADS, 1) att_dkv_pipe_kernel(AttArgs a) {
   float stat = 0.0f;
   const float to_stat = threadIdx.x < 64 ? 1.0f / sl2 : 1.0f;
   auto load_stat = [&](int u) {
-    const int row = (t1 - 1 - u / a.rep) * 64 + (threadIdx.x & 63);
-    if (threadIdx.x < 128 && u < steps && row < a.T) stat = stats[(int64_t)(u % a.rep) * a.T + row];
+    const int row = (t1 - 1 - u / reps) * 64 + (threadIdx.x & 63);
+    if (threadIdx.x < 128 && u < steps && row < a.T) stat = stats[(int64_t)(u % reps) * a.T + row];
   };
   auto put_stat = [&](int u) {
     if (threadIdx.x < 128) *(float*)(lds_s + (u & 3) * STAT + threadIdx.x * 4) = stat * to_stat;
   };
   auto copy = [&](int u) {
     if (u >= steps) return;
-    const int up = u / a.rep, h = u - up * a.rep, row = (t1 - 1 - up) * 64;
+    const int up = u / reps, h = u - up * reps, row = (t1 - 1 - up) * 64;
     cq.tile(row, (u & 3) * SLOT, (int64_t)h * a.q.hs * 2);
     cg.tile(row, (u & 3) * SLOT, (int64_t)h * a.dout.hs * 2);
   };
@@ -1321,7 +1384,7 @@ __global__ void __launch_bounds__(THREADS, 1) att_dkv_pipe_kernel(AttArgs a) {
     copy(u + 2);
   };
   begin();
-  const int ua = w0 < w1 ? (t1 - w1) * a.rep : steps, ub = w0 < w1 ? (t1 - w0) * a.rep : steps;
+  const int ua = w0 < w1 ? (t1 - w1) * reps : steps, ub = w0 < w1 ? (t1 - w0) * reps : steps;
   int u = 0;
   for (; u < ua; ++u) arrive(u, true);
   if (u < ub) {
@@ -1350,15 +1413,15 @@ __global__ void __launch_bounds__(THREADS, 1) att_dkv_pipe_kernel(AttArgs a) {
     auto through = [&](auto masked_c, int until) {
       while (u < until) {
         const int kmove = (u & 3) == 3 ? -3 * SLOT : SLOT, smove = (u & 3) == 3 ? -3 * STAT : STAT;
-        const int q0 = decltype(masked_c)::value ? (t1 - 1 - u / a.rep) * 64 : 0;
+        const int q0 = decltype(masked_c)::value ? (t1 - 1 - u / reps) * 64 : 0;
         phase(std::true_type{}, masked_c, s0, d0, s1, d1, p1, e1, p0, e0, kmove, 0, q0);
         phase(std::false_type{}, masked_c, s1, d1, s0, d0, p0, e0, p1, e1, vmove, smove, q0 + 32);
         vmove = kmove;
         if (++u < ub) arrive(u, false);
       }
     };
-    through(std::true_type{}, min((t1 - min(f1, t1)) * a.rep, ub));
-    through(std::false_type{}, min((t1 - min(f0, t1)) * a.rep, ub));
+    through(std::true_type{}, min((t1 - min(f1, t1)) * reps, ub));
+    through(std::false_type{}, min((t1 - min(f0, t1)) * reps, ub));
     through(std::true_type{}, ub);
 #pragma unroll
     for (int s = 0; s < NP; ++s)
@@ -1380,7 +1443,7 @@ __global__ void __launch_bounds__(THREADS, 1) att_dkv_pipe_kernel(AttArgs a) {
     begin();
     for (u = 0; u < steps; ++u) {
         arrive(u, true);
-        const int t = t1 - 1 - u / a.rep;
+        const int t = t1 - 1 - u / reps;
         if (t < w0 || t >= w1) continue;
         const uint8_t* q = lds + (u & 3) * SLOT;
 #pragma unroll 1
@@ -1408,8 +1471,7 @@ __global__ void __launch_bounds__(THREADS, 1) att_dkv_pipe_kernel(AttArgs a) {
         }
       }
   }
-  put_row<T, DP, FULL>((T*)a.dk.p + kv * a.dk.hs + (int64_t)n * a.dk.ld, dk, a.scale, !at.live, n < a.T, a.d);
-  put_row<T, DP, FULL>((T*)a.dv.p + kv * a.dv.hs + (int64_t)n * a.dv.ld, dv, 1.0f, !at.live, n < a.T, a.d);
+  put_keys<T, DP, FULL>(a, w, n, dk, dv, at.live);
 }
 
 // dq: 64 queries a wave.  A phase forms the next half's S, this half's dP and the previous half's share of dq; on the
@@ -1668,6 +1730,27 @@ int att_strides(const char* fn, int64_t ld, int64_t hs) {
   return ld < 0 || hs < 0 ? fail(AGRL_E_SHAPE, fn, "a stride is negative") : AGRL_OK;
 }
 
+// Parts that the heads of a group are dealt to: the walks of key tiles differ in length, so a chip of 256 units wants
+// several each.  128 tiles of 4 key heads with 7 query heads each: MEASURED_SPLITS
+int att_splits(int64_t T, int32_t n_head, int32_t n_kv) {
+  const int64_t items = cdiv(T, (int64_t)BM) * n_kv, want = cdiv((int64_t)256, items), rep = n_head / n_kv;
+  return (int)(want < rep ? want : rep);
+}
+
+struct AttSpace {
+  size_t delta, order, part, total;
+};
+AttSpace att_space(int64_t T, int32_t n_head, int32_t n_kv, int32_t d) {
+  auto up = [](size_t n) { return (n + 255) & ~(size_t)255; };
+  const int splits = att_splits(T, n_head, n_kv);
+  AttSpace s;
+  s.delta = up((size_t)T * n_head * 4);
+  s.order = 2 * s.delta;
+  s.part = s.order + up((size_t)cdiv(T, (int64_t)BM) * 4);
+  s.total = s.part + (splits > 1 ? (size_t)splits * 2 * T * n_kv * d * 4 : 0);
+  return s;
+}
+
 // Whether 16-byte copies reach every row of a bf16 operand, 64 rows within 32-bit offsets
 bool copies(const Heads& h) {
   return (uintptr_t)h.p % 16 == 0 && h.ld % 8 == 0 && h.hs % 8 == 0 && h.ld < (1 << 24);
@@ -1739,7 +1822,7 @@ extern "C" size_t agrl_attention_bwd_workspace_size(int64_t T, int32_t n_head, i
   if ((dtype != AGRL_BF16 && dtype != AGRL_F32) || T <= 0 || T > ATT_MAX_T || n_head <= 0 || n_kv <= 0 ||
       n_head % n_kv || d <= 0 || d > ATT_MAX_D || cdiv(T, (int64_t)BM) * n_head >= 0x7fffffff)
     return 0;
-  return ((size_t)T * n_head * 2 + (size_t)agrl::cdiv(T, (int64_t)agrl::BM)) * 4;
+  return att_space(T, n_head, n_kv, d).total;
 }
 
 extern "C" int agrl_attention_bwd(int64_t T, int32_t n_seq, int32_t n_head, int32_t n_kv, int32_t d,
@@ -1772,9 +1855,11 @@ extern "C" int agrl_attention_bwd(int64_t T, int32_t n_seq, int32_t n_head, int3
   if ((uintptr_t)workspace % 256 != 0)
     return fail(AGRL_E_UNSUPPORTED, fn, "workspace must be 256-byte aligned");
   hipStream_t s = (hipStream_t)stream;
-  float* lse2 = (float*)workspace;
-  float* delta = lse2 + T * n_head;
-  int32_t* order = (int32_t*)(delta + T * n_head);
+  const AttSpace sp = att_space(T, n_head, n_kv, d);
+  uint8_t* ws = (uint8_t*)workspace;
+  float* lse2 = (float*)ws;
+  float* delta = (float*)(ws + sp.delta);
+  int32_t* order = (int32_t*)(ws + sp.order);
   const DeltaArgs de = {(int32_t)T, n_head, d, n_seq, {o, ld_o, head_o}, {dout, ld_do, head_do}, lse, lse2, delta,
                         seq_start, order};
   const int64_t need = cdiv(T * n_head, (int64_t)16), most = (int64_t)device_cu_count() * 16;
@@ -1788,10 +1873,11 @@ extern "C" int agrl_attention_bwd(int64_t T, int32_t n_seq, int32_t n_head, int3
   a.q = {q, ld_q, head_q}, a.k = {k, ld_k, head_k}, a.v = {v, ld_v, head_v};
   a.start = seq_start, a.scale = scale, a.err = device_error_ptr();
   a.dout = {dout, ld_do, head_do}, a.lse2 = lse2, a.delta = delta, a.order = order;
+  a.splits = att_splits(T, n_head, n_kv), a.part = (float*)(ws + sp.part);
   a.dq = {dq, ld_dq, head_dq}, a.dk = {dk, ld_dk, head_dk}, a.dv = {dv, ld_dv, head_dv};
   const int64_t tiles = cdiv(T, (int64_t)BM);
   const bool pipe = dtype == AGRL_BF16 && d % 8 == 0 && copies(a.q) && copies(a.k) && copies(a.v) && copies(a.dout);
-  const dim3 kgrid((unsigned)(tiles * n_kv)), block(THREADS);
+  const dim3 kgrid((unsigned)(tiles * n_kv * a.splits)), block(THREADS);
   if (pipe) {
     const dim3 qgrid((unsigned)(cdiv(T, (int64_t)PIPE_ROWS) * n_head));
     att_size(d, [&](auto dp, auto full) {
@@ -1800,13 +1886,22 @@ extern "C" int agrl_attention_bwd(int64_t T, int32_t n_seq, int32_t n_head, int3
       hipLaunchKernelGGL((att_dkv_pipe_kernel<DP, FULL>), kgrid, block, 0, s, a);
       hipLaunchKernelGGL((att_dq_pipe_kernel<DP, FULL>), qgrid, block, 0, s, a);
     });
-    return hip_status(hipGetLastError());
+  } else {
+    att_pick(dtype, d, [&](auto z, auto dp, auto full) {
+      using E = decltype(z);
+      constexpr int DP = decltype(dp)::value;
+      constexpr bool FULL = decltype(full)::value;
+      hipLaunchKernelGGL((att_dkv_kernel<E, DP, FULL>), kgrid, block, 0, s, a);
+      hipLaunchKernelGGL((att_dq_kernel<E, DP, FULL>), dim3((unsigned)(tiles * n_head)), block, 0, s, a);
+    });
   }
-  att_pick(dtype, d, [&](auto z, auto dp, auto full) {
-    hipLaunchKernelGGL((att_dkv_kernel<decltype(z), decltype(dp)::value, decltype(full)::value>), kgrid, block, 0, s,
-                       a);
-    hipLaunchKernelGGL((att_dq_kernel<decltype(z), decltype(dp)::value, decltype(full)::value>),
-                       dim3((unsigned)(tiles * n_head)), block, 0, s, a);
-  });
+  if (a.splits > 1) {
+    const int64_t want = cdiv(T * n_kv * cdiv(d, CH), (int64_t)256), top = (int64_t)device_cu_count() * 8;
+    const dim3 jgrid((unsigned)(want < top ? want : top));
+    if (dtype == AGRL_BF16)
+      hipLaunchKernelGGL(att_join_kernel<uint16_t>, jgrid, dim3(256), 0, s, a);
+    else
+      hipLaunchKernelGGL(att_join_kernel<float>, jgrid, dim3(256), 0, s, a);
+  }
   return hip_status(hipGetLastError());
 }
