@@ -1292,21 +1292,23 @@ __global__ void __launch_bounds__(THREADS, 1) att_dkv_pipe_kernel(AttArgs a) {
     slots<NM>([&](auto slot) {
       constexpr int i = slot.value, rd = i + AHEAD;
       if constexpr (rd < 2 * NS)
-        fr[rd % FR] = *(const u32x4*)(lds + KH * 32 * ROW + (rd < NS ? 0 : TB) + ko[rd % NS]);
+        fr[rd % FR] = *(const u32x4*)(lds + KH * 32 * ROW + (rd & 1) * TB + ko[rd / 2]);
       else if constexpr (rd < NM) {
-        constexpr int c = (rd - 2 * NS) % NC;
-        fr[rd % FR] = read_col(KH * 32 * ROW + (rd < 2 * NS + NC ? TB : 0), c / ND, c % ND);
+        constexpr int c = (rd - 2 * NS) / 2;
+        fr[rd % FR] = read_col(KH * 32 * ROW + (rd & 1 ? 0 : TB), c / ND, c % ND);
       } else {
-        fr[rd % FR] = *(const u32x4*)(lds + (KH ^ 1) * 32 * ROW + (rd - NM < NS ? 0 : TB) + ko[(rd - NM) % NS]);
+        fr[rd % FR] = *(const u32x4*)(lds + (KH ^ 1) * 32 * ROW + (rd & 1) * TB + ko[(rd - NM) / 2]);
       }
-      if constexpr (i < NS)
-        sn = M::mma(fr[i % FR], k[i], i == 0 ? f32x16{} : sn);
+      // (two sums in turn: one behind the other the matrix core waits for each product's result)
+      constexpr int c = (i - 2 * NS) / 2;
+      if constexpr (i < 2 * NS && i % 2 == 0)
+        sn = M::mma(fr[i % FR], k[i / 2], i == 0 ? f32x16{} : sn);
       else if constexpr (i < 2 * NS)
-        dn = M::mma(fr[i % FR], v[i - NS], i == NS ? f32x16{} : dn);
-      else if constexpr (i < 2 * NS + NC)
-        dv[(i - 2 * NS) % ND] = M::mma(fr[i % FR], pp[(i - 2 * NS) / ND], dv[(i - 2 * NS) % ND]);
+        dn = M::mma(fr[i % FR], v[i / 2], i == 1 ? f32x16{} : dn);
+      else if constexpr (i % 2 == 0)
+        dv[c % ND] = M::mma(fr[i % FR], pp[c / ND], dv[c % ND]);
       else
-        dk[(i - 2 * NS - NC) % ND] = M::mma(fr[i % FR], ep[(i - 2 * NS - NC) / ND], dk[(i - 2 * NS - NC) % ND]);
+        dk[c % ND] = M::mma(fr[i % FR], ep[c / ND], dk[c % ND]);
       if constexpr (FIRST && i >= 2 * NS && i < 3 * NS) ko[i - 2 * NS] += move;
       if constexpr (!FIRST && i == 0)
 #pragma unroll
@@ -1407,7 +1409,7 @@ __global__ void __launch_bounds__(THREADS, 1) att_dkv_pipe_kernel(AttArgs a) {
     gc = gn;
 #pragma unroll
     for (int i = 0; i < AHEAD; ++i)
-      fr[i] = *(const u32x4*)(lds + 32 * ROW + (i < NS ? 0 : TB) + ko[i % NS]);
+      fr[i] = *(const u32x4*)(lds + 32 * ROW + (i & 1) * TB + ko[i / 2]);
     static_assert((2 * NS + 2 * NP * ND) % FR == 0, "a phase starts at the ring's first fragment");
     int vmove = 0;
     auto through = [&](auto masked_c, int until) {
