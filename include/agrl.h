@@ -513,7 +513,7 @@ int agrl_rotate_heads(int64_t T, int32_t n_head, int32_t d, int32_t rot, int32_t
  *                     sequence: their values do not matter, their o is +0 and their lse 0.  n_seq = 0:
  *                     no token belongs to one.  Offsets that decrease or leave [0, T] set bit 32 of
  *                     the device error word; what o holds is then unspecified
- *   scale             finite, > 0
+ *   scale             2^-60 to 2^60
  * Outputs: o [T, n_head, d]; lse [n_head, T] fp32 (NULL: not written; the backward needs it).
  * Products of bf16 inputs and all sums are fp32, P is rounded to `dtype` before it meets v, o once.
  * No token of another sequence and no later one of its own reaches a row, not even a NaN or

@@ -632,9 +632,6 @@ __global__ void __launch_bounds__(THREADS, 1) att_fwd_pipe_kernel(AttArgs a) {
 
   const typename TL::Lane L;
   u32x4 q[2][NS];
-  const T* qp = (const T*)a.q.p + head * a.q.hs;
-  hold<T, DP, FULL>(q[0], qp + (int64_t)nA * a.q.ld, at[0].live, a.d);
-  hold<T, DP, FULL>(q[1], qp + (int64_t)nB * a.q.ld, at[1].live, a.d);
   Copy<DP> ck, cv;
   ck.init((const T*)a.k.p + kv * a.k.hs, a.k.ld, lds_address(lds_k), wave, a.T, a.d);
   cv.init((const T*)a.v.p + kv * a.v.hs, a.v.ld, lds_address(lds_v), wave, a.T, a.d);
@@ -642,22 +639,7 @@ __global__ void __launch_bounds__(THREADS, 1) att_fwd_pipe_kernel(AttArgs a) {
   f32x16 o[2][ND] = {};
   float l[2] = {0.0f, 0.0f}, m[2];
   const uint32_t len[2] = {at[0].live ? nA - at[0].begin + 1u : 0u, at[1].live ? nB - at[1].begin + 1u : 0u};
-  // the reference: the row's own score
   float ref[2];
-#pragma unroll
-  for (int cb = 0; cb < 2; ++cb) {
-    u32x4 own[NS];
-    hold<T, DP, FULL>(own, (const T*)a.k.p + kv * a.k.hs + (int64_t)(cb ? nB : nA) * a.k.ld, at[cb].live, a.d);
-    float dot = 0.0f;
-#pragma unroll
-    for (int s = 0; s < NS; ++s)
-#pragma unroll
-      for (int e = 0; e < 4; ++e) {
-        const uint32_t x = q[cb][s][e], y = own[s][e];
-        dot = __builtin_amdgcn_fdot2_f32_bf16(__builtin_bit_cast(bf16x2, x), __builtin_bit_cast(bf16x2, y), dot, false);
-      }
-    ref[cb] = (dot + other_half(dot)) * sl2;
-  }
   const int t0 = lo / 64, t1 = lo < hi ? (hi + 63) / 64 : t0;
   // the wave's tiles, and those of them that all its columns count whole
   const int w0 = span.lo < span.hi ? span.lo / 64 : t1, w1 = span.lo < span.hi ? (span.hi + 63) / 64 : t0;
@@ -761,6 +743,24 @@ __global__ void __launch_bounds__(THREADS, 1) att_fwd_pipe_kernel(AttArgs a) {
     if (t + 1 < t1) cv.tile(t * 64 + 64, next * TB);
   };
   begin();
+  const T* qp = (const T*)a.q.p + head * a.q.hs;
+  hold<T, DP, FULL>(q[0], qp + (int64_t)nA * a.q.ld, at[0].live, a.d);
+  hold<T, DP, FULL>(q[1], qp + (int64_t)nB * a.q.ld, at[1].live, a.d);
+  // the reference: the row's own score
+#pragma unroll
+  for (int cb = 0; cb < 2; ++cb) {
+    u32x4 own[NS];
+    hold<T, DP, FULL>(own, (const T*)a.k.p + kv * a.k.hs + (int64_t)(cb ? nB : nA) * a.k.ld, at[cb].live, a.d);
+    float dot = 0.0f;
+#pragma unroll
+    for (int s = 0; s < NS; ++s)
+#pragma unroll
+      for (int e = 0; e < 4; ++e) {
+        const uint32_t x = q[cb][s][e], y = own[s][e];
+        dot = __builtin_amdgcn_fdot2_f32_bf16(__builtin_bit_cast(bf16x2, x), __builtin_bit_cast(bf16x2, y), dot, false);
+      }
+    ref[cb] = (dot + other_half(dot)) * sl2;
+  }
   int t = t0;
   for (; t < min(w0, t1); ++t) {
     arrive(t);
@@ -1252,8 +1252,6 @@ __global__ void __launch_bounds__(THREADS, 1) att_dkv_pipe_kernel(AttArgs a) {
 
   const typename TL::Lane L;
   u32x4 k[NS], v[NS];
-  hold<T, DP, FULL>(k, (const T*)a.k.p + kv * a.k.hs + (int64_t)n * a.k.ld, at.live, a.d);
-  hold<T, DP, FULL>(v, (const T*)a.v.p + kv * a.v.hs + (int64_t)n * a.v.ld, at.live, a.d);
   Copy<DP> cq, cg;
   cq.init((const T*)a.q.p + (int64_t)w.head * a.q.hs, a.q.ld, lds_address(lds), wave, a.T, a.d);
   cg.init((const T*)a.dout.p + (int64_t)w.head * a.dout.hs, a.dout.ld, lds_address(lds) + TB, wave, a.T, a.d);
@@ -1386,6 +1384,8 @@ __global__ void __launch_bounds__(THREADS, 1) att_dkv_pipe_kernel(AttArgs a) {
     copy(u + 2);
   };
   begin();
+  hold<T, DP, FULL>(k, (const T*)a.k.p + kv * a.k.hs + (int64_t)n * a.k.ld, at.live, a.d);
+  hold<T, DP, FULL>(v, (const T*)a.v.p + kv * a.v.hs + (int64_t)n * a.v.ld, at.live, a.d);
   const int ua = w0 < w1 ? (t1 - w1) * reps : steps, ub = w0 < w1 ? (t1 - w0) * reps : steps;
   int u = 0;
   for (; u < ua; ++u) arrive(u, true);
@@ -1509,15 +1509,6 @@ __global__ void __launch_bounds__(THREADS, 1) att_dq_pipe_kernel(AttArgs a) {
   u32x4 q[2][NS], g[2][NS];
   float lse2[2], delta[2];
   uint32_t len[2];
-#pragma unroll
-  for (int cb = 0; cb < 2; ++cb) {
-    const int n = cb ? nB : nA;
-    hold<T, DP, FULL>(q[cb], (const T*)a.q.p + head * a.q.hs + (int64_t)n * a.q.ld, at[cb].live, a.d);
-    hold<T, DP, FULL>(g[cb], (const T*)a.dout.p + head * a.dout.hs + (int64_t)n * a.dout.ld, at[cb].live, a.d);
-    lse2[cb] = at[cb].live ? a.lse2[(int64_t)head * a.T + n] : 0.0f;
-    delta[cb] = at[cb].live ? a.delta[(int64_t)head * a.T + n] : 0.0f;
-    len[cb] = at[cb].live ? n - at[cb].begin + 1 : 0;
-  }
   Copy<DP> ck, cv;
   ck.init((const T*)a.k.p + kv * a.k.hs, a.k.ld, lds_address(lds_k), wave, a.T, a.d);
   cv.init((const T*)a.v.p + kv * a.v.hs, a.v.ld, lds_address(lds_v), wave, a.T, a.d);
@@ -1614,6 +1605,15 @@ __global__ void __launch_bounds__(THREADS, 1) att_dq_pipe_kernel(AttArgs a) {
     if (t + 1 < t1) cv.tile(t * 64 + 64, (u + 1 & 1) * TB);
   };
   begin();
+#pragma unroll
+  for (int cb = 0; cb < 2; ++cb) {
+    const int n = cb ? nB : nA;
+    hold<T, DP, FULL>(q[cb], (const T*)a.q.p + head * a.q.hs + (int64_t)n * a.q.ld, at[cb].live, a.d);
+    hold<T, DP, FULL>(g[cb], (const T*)a.dout.p + head * a.dout.hs + (int64_t)n * a.dout.ld, at[cb].live, a.d);
+    lse2[cb] = at[cb].live ? a.lse2[(int64_t)head * a.T + n] : 0.0f;
+    delta[cb] = at[cb].live ? a.delta[(int64_t)head * a.T + n] : 0.0f;
+    len[cb] = at[cb].live ? n - at[cb].begin + 1 : 0;
+  }
   int t = t0;
   for (; t < min(w0, t1); ++t, ++u) arrive(t);
   if (t < w1) {
@@ -1725,7 +1725,9 @@ int att_check(const char* fn, int64_t T, int32_t n_seq, int32_t n_head, int32_t 
     return fail(AGRL_E_SHAPE, fn, "n_head must be a multiple of n_kv, d positive");
   if (cdiv(T, (int64_t)BM) * n_head >= 0x7fffffff) return fail(AGRL_E_SHAPE, fn, "T n_head is too large");
   if (d > ATT_MAX_D) return fail(AGRL_E_UNSUPPORTED, fn, "d is larger than 128");
-  if (!(scale > 0.0f) || !isfinite(scale)) return fail(AGRL_E_FLAGS, fn, "scale must be finite and > 0");
+  // (the backward divides lse by it)
+  if (!(scale >= 0x1p-60f && scale <= 0x1p60f))
+    return fail(AGRL_E_FLAGS, fn, "scale must be in [2^-60, 2^60]");
   return AGRL_OK;
 }
 int att_strides(const char* fn, int64_t ld, int64_t hs) {

@@ -336,6 +336,70 @@ int chunk_of(int64_t T, int32_t d) {
   return cdiv(T, (int64_t)MAX_CHUNK) * cdiv(d, SLAB) < 1024 ? MIN_CHUNK : MAX_CHUNK;
 }
 
+// Few tokens: one launch, no sort.  A workgroup per token and slab of columns looks all ids over: the first token of an
+// id adds up those that follow, the others leave.  Workgroups behind them clear the rows of absent ids.
+constexpr int FEW = 512;
+template <typename Y, bool ADD>
+__global__ void __launch_bounds__(256) embed_few_kernel(SortArgs t, RowsArgs a) {
+  const int T = (int)t.T, adding = T * a.slabs, lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+  auto live = [&](int n) { return !t.live || t.live[n] != 0; };
+  if (blockIdx.x >= adding) {
+    __shared__ int here[ZROWS];
+    const int v0 = (int)(blockIdx.x - adding) * ZROWS;
+    if (threadIdx.x < ZROWS) here[threadIdx.x] = 0;
+    __syncthreads();
+    for (int n = threadIdx.x; n < T; n += 256)
+      if (live(n) && t.id[n] >= v0 && t.id[n] < v0 + ZROWS) here[t.id[n] - v0] = 1;
+    __syncthreads();
+    for (int v = v0; v < min(v0 + ZROWS, a.V); ++v) {
+      if (here[v - v0]) continue;
+      float* p = a.dw + (int64_t)v * a.d;
+      for (int c = threadIdx.x * 4; c < a.d; c += 1024) store4(p + c, f32x4{0, 0, 0, 0}, a.d - c);
+    }
+    return;
+  }
+  const int n = blockIdx.x / a.slabs, col = (int)(blockIdx.x - n * a.slabs) * SLAB + threadIdx.x * 4, left = a.d - col;
+  if (!live(n)) return;
+  const int v = t.id[n];
+  if (v < 0 || v >= a.V) {
+    if (threadIdx.x == 0) set_error(t.err, ERR_TOKEN_ID);
+    return;
+  }
+  __shared__ uint64_t same[FEW / 64];          // the tokens with this id, a bit each
+#pragma unroll
+  for (int k = 0; k < FEW / 256; ++k) {
+    const int m = k * 256 + threadIdx.x;
+    const uint64_t bits = __ballot(m < T && t.id[min(m, T - 1)] == v && live(min(m, T - 1)));
+    if (lane == 0) same[k * 4 + wave] = bits;
+  }
+  __syncthreads();
+  for (int k = 0; k <= n >> 6; ++k)
+    if (same[k] & (k < n >> 6 ? ~(uint64_t)0 : ((uint64_t)1 << (n & 63)) - 1)) return;
+  if (left <= 0) return;
+  f32x4 sum = {0.0f, 0.0f, 0.0f, 0.0f}, old = sum;
+  if (ADD) old = load4(a.dw + (int64_t)v * a.d + col, left);
+  for (int k = n >> 6; k < FEW / 64; ++k) {
+    uint64_t todo = same[k];
+    todo = (uint64_t)__builtin_amdgcn_readfirstlane((int)(todo >> 32)) << 32 |
+           (uint32_t)__builtin_amdgcn_readfirstlane((int)todo);
+    while (todo) {
+      f32x4 x[8];
+      int many = 0;
+#pragma unroll
+      for (int e = 0; e < 8; ++e) {
+        if (!todo) continue;
+        x[e] = load4((const Y*)a.dy + (int64_t)(k * 64 + __builtin_ctzll(todo)) * a.ld_dy + col, left);
+        todo &= todo - 1;
+        many = e + 1;
+      }
+#pragma unroll
+      for (int e = 0; e < 8; ++e)
+        if (e < many) sum += x[e];
+    }
+  }
+  store4(a.dw + (int64_t)v * a.d + col, old + sum * a.scale, left);
+}
+
 struct Space {
   size_t sorted, starts, crossing, part, total;
 };
@@ -421,11 +485,23 @@ extern "C" int agrl_token_embed_bwd(int64_t T, int32_t d, int32_t V, int32_t dy_
   const int fair = cdiv(V, device_cu_count());
   const SortArgs so = {T, V, fair < MAX_RANGE ? fair : MAX_RANGE, token_id, live_mask, sorted, starts,
                        (int32_t*)(ws + sp.crossing), device_error_ptr()};
-  hipLaunchKernelGGL(embed_sort_kernel, dim3(cdiv(V, so.range)), dim3(64 * SORT_WAVES),
-                     SORT_WAVES * so.range * 4, s, so);
   const int chunk = chunk_of(T, d);
   const RowsArgs r = {d, V, cdiv(d, SLAB), accumulate, chunk, cdiv(T, (int64_t)chunk), dy, ld_dy, scale,
                       sorted, starts, (float*)(ws + sp.part), so.crossing, dweight};
+  if (T <= FEW) {
+    const dim3 few((unsigned)(T * r.slabs + (accumulate ? 0 : cdiv(V, ZROWS)))), lanes(256);
+    if (dy_dtype == AGRL_BF16 && accumulate)
+      hipLaunchKernelGGL((embed_few_kernel<uint16_t, true>), few, lanes, 0, s, so, r);
+    else if (dy_dtype == AGRL_BF16)
+      hipLaunchKernelGGL((embed_few_kernel<uint16_t, false>), few, lanes, 0, s, so, r);
+    else if (accumulate)
+      hipLaunchKernelGGL((embed_few_kernel<float, true>), few, lanes, 0, s, so, r);
+    else
+      hipLaunchKernelGGL((embed_few_kernel<float, false>), few, lanes, 0, s, so, r);
+    return hip_status(hipGetLastError());
+  }
+  hipLaunchKernelGGL(embed_sort_kernel, dim3(cdiv(V, so.range)), dim3(64 * SORT_WAVES),
+                     SORT_WAVES * so.range * 4, s, so);
   const dim3 grid((unsigned)(r.chunks * r.slabs + (accumulate ? 0 : cdiv(V, ZROWS)))), block(256);
   if (dy_dtype == AGRL_BF16 && accumulate)
     hipLaunchKernelGGL((embed_rows_kernel<uint16_t, true>), grid, block, 0, s, r);
