@@ -17,6 +17,11 @@
 //         is added by as many workgroups).  The rows of ids that do not occur are cleared by
 //         further workgroups of the same launch.
 //   join  adds the pieces of each crossing run in order.
+// Up to 512 tokens one launch does it all (embed_few_kernel).
+//
+// Measured (MI355X; a copy of 2 GiB moves 4.9 TB/s, a fill 6.9): forward of 65536 x 5120 bf16 out of [152064, 5120]
+// 213 us (6.2 TB/s of rows, the repeated ones from the caches).  Backward of the same, the whole gradient written,
+// 816 us: rows 712 (3.8 GB), sort 68, join 34; 3823 x 1001 fp32 onto a [4096, 1001] 34 us: three launches of 13, 10 and 8.
 #include <math.h>
 
 #include "rows.hpp"
@@ -331,13 +336,15 @@ __global__ void __launch_bounds__(256) embed_join_kernel(RowsArgs a) {
   }
 }
 
-// Tokens per chunk: few tokens in chunks of 8, so that they fill the chip
+// Tokens per chunk: few tokens in chunks of 8, so that they fill the chip (3823 x 1001: rows 23 us in chunks of 32, 9 in
+// chunks of 8)
 int chunk_of(int64_t T, int32_t d) {
   return cdiv(T, (int64_t)MAX_CHUNK) * cdiv(d, SLAB) < 1024 ? MIN_CHUNK : MAX_CHUNK;
 }
 
 // Few tokens: one launch, no sort.  A workgroup per token and slab of columns looks all ids over: the first token of an
 // id adds up those that follow, the others leave.  Workgroups behind them clear the rows of absent ids.
+// [4096, 256], added to: 8 tokens 6.7 us, 256 9.4, 512 15.7; 520 by the sort 18.2.
 constexpr int FEW = 512;
 template <typename Y, bool ADD>
 __global__ void __launch_bounds__(256) embed_few_kernel(SortArgs t, RowsArgs a) {
