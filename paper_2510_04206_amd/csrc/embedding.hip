@@ -102,12 +102,6 @@ struct SortArgs {
   int* err;
 };
 
-__device__ __forceinline__ int wave_sum_int(int v) {
-#pragma unroll
-  for (int o = 32; o; o >>= 1) v += __shfl_xor(v, o);
-  return v;
-}
-
 __global__ void __launch_bounds__(64 * SORT_WAVES) embed_sort_kernel(SortArgs a) {
   extern __shared__ int cnt[];                       // [SORT_WAVES][range]
   __shared__ int below_of[SORT_WAVES], ids_of[SORT_WAVES];
@@ -125,6 +119,16 @@ __global__ void __launch_bounds__(64 * SORT_WAVES) embed_sort_kernel(SortArgs a)
   // the ids of tokens t, t + 64, ..: NONE for dead tokens and ids out of range.  (All loads first, from
   // clamped places: behind a branch each would wait for the one before)
   auto fetch = [&](int64_t t, int (&id)[AHEAD]) {
+    // whole batches without a mask, the usual ones: nothing but the loads and a look at the largest (the vector ALU
+    // is what bounds this kernel: every workgroup sees every id)
+    if (!a.live && t - lane + 64 * AHEAD <= t1) {
+      uint32_t most = 0;
+#pragma unroll
+      for (int k = 0; k < AHEAD; ++k) id[k] = (a.id + t)[64 * k];
+#pragma unroll
+      for (int k = 0; k < AHEAD; ++k) most = max(most, (uint32_t)id[k]);
+      if (!__any(most >= (uint32_t)a.V)) return;
+    }
     uint8_t live[AHEAD];
 #pragma unroll
     for (int k = 0; k < AHEAD; ++k) {
@@ -141,24 +145,26 @@ __global__ void __launch_bounds__(64 * SORT_WAVES) embed_sort_kernel(SortArgs a)
     }
     if (bad && blockIdx.x == 0) set_error(a.err, ERR_TOKEN_ID);
   };
-  int below = 0;
+  int below = 0, id[AHEAD];                          // (few tokens stay in registers for the second pass)
   for (int64_t t = t0 + lane; t < t1 + lane; t += 64 * AHEAD) {
-    int id[AHEAD];
     fetch(t, id);
 #pragma unroll
     for (int k = 0; k < AHEAD; ++k) {
-      below += id[k] < lo;
-      if (id[k] >= lo && id[k] < hi) atomicAdd(&own[id[k] - lo], 1);
+      below += __popcll(__ballot(id[k] < lo));
+      const uint32_t v = id[k] - lo;
+      if (v < (uint32_t)(hi - lo)) atomicAdd(&own[v], 1);
     }
   }
-  below = wave_sum_int(below);
   if (lane == 0) below_of[wave] = below;
   __syncthreads();
   // where each id and wave starts: ids in order, within an id the waves in order
   const int i = threadIdx.x;
   int mine = 0, sum;
-  if (i < a.range)
-    for (int w = 0; w < SORT_WAVES; ++w) mine += cnt[w * a.range + i];
+  int each[SORT_WAVES];                              // the id's tokens in each wave's run
+#pragma unroll
+  for (int w = 0; w < SORT_WAVES; ++w) each[w] = i < a.range ? cnt[w * a.range + i] : 0;
+#pragma unroll
+  for (int w = 0; w < SORT_WAVES; ++w) mine += each[w];
   sum = mine;
 #pragma unroll
   for (int o = 1; o < 64; o <<= 1) {
@@ -168,24 +174,24 @@ __global__ void __launch_bounds__(64 * SORT_WAVES) embed_sort_kernel(SortArgs a)
   if (lane == 63) ids_of[wave] = sum;
   __syncthreads();
   int start = sum - mine;
+#pragma unroll
   for (int w = 0; w < SORT_WAVES; ++w) start += below_of[w] + (w < wave ? ids_of[w] : 0);
   if (i < a.range) {
     if (lo + i <= a.V) a.row_start[lo + i] = start;
     if (lo + i == a.V - 1) a.row_start[a.V] = start + mine;
+#pragma unroll
     for (int w = 0; w < SORT_WAVES; ++w) {
-      const int n = cnt[w * a.range + i];
       cnt[w * a.range + i] = start;
-      start += n;
+      start += each[w];
     }
   }
   __syncthreads();
   for (int64_t t = t0 + lane; t < t1 + lane; t += 64 * AHEAD) {
-    int id[AHEAD];
-    fetch(t, id);
+    if (per > 64 * AHEAD) fetch(t, id);
 #pragma unroll
     for (int k = 0; k < AHEAD; ++k) {
       const int v = id[k] - lo;
-      const bool in = id[k] >= lo && id[k] < hi;
+      const bool in = (uint32_t)v < (uint32_t)(hi - lo);
       uint64_t same = __ballot(in);
       if (!same) continue;
       // the wave's tokens with the lane's id: those that agree in each of its bits
