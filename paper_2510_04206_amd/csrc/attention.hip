@@ -252,7 +252,7 @@ struct Place {
   // lo, hi: offsets up to the first and the last of the wave's tokens; n one of them
   __device__ __forceinline__ Place(const int32_t* start, int n_seq, int T, int lo, int hi, int n) {
     while (lo < hi) {
-      const int mid = (lo + hi) >> 1;
+      const int mid = lo + ((hi - lo) >> 1);
       if (start[mid] <= n)
         lo = mid + 1;
       else
@@ -558,8 +558,8 @@ __global__ void __launch_bounds__(THREADS, sizeof(T) == 2 ? 2 : 1) att_fwd_kerne
 // pipeline in which nothing waits.  Keys go by halves of 32: while the exponentials of one half run on the
 // vector ALU, the matrix cores form the next half's scores and the previous half's share of o.  A phase
 // has a slot per MFMA (32 cycles of the matrix core); each carries two of the half's 64 columns' values, and
-// every other one an LDS fragment read, three fragments ahead.  K and V go straight from global
-// memory into rings of three tiles of 64, K a tile ahead of V.
+// every other one an LDS fragment read, seven fragments ahead (three with heads of 64).  K and V go
+// straight from global memory into rings of three tiles of 64, K a tile ahead of V.
 //
 // The softmax's reference is the row's own score q k, which is one of those that count: the sum is at least 1, and
 // there is no running maximum to follow.  Weights may grow to 2^96 before that fails (scores 66 above the row's own);
@@ -1728,7 +1728,7 @@ int att_check(const char* fn, int64_t T, int32_t n_seq, int32_t n_head, int32_t 
               float scale) {
   if (dtype != AGRL_BF16 && dtype != AGRL_F32)
     return fail(AGRL_E_DTYPE, fn, "dtype must be AGRL_BF16 or AGRL_F32");
-  if (T < 0 || T > ATT_MAX_T || n_seq < 0 || n_seq == 0x7fffffff)
+  if (T < 0 || T > ATT_MAX_T || n_seq < 0 || n_seq > (1 << 30))
     return fail(AGRL_E_SHAPE, fn, "bad T or n_seq");
   if (n_head <= 0 || n_kv <= 0 || n_head % n_kv || d <= 0)
     return fail(AGRL_E_SHAPE, fn, "n_head must be a multiple of n_kv, d positive");
