@@ -22,8 +22,8 @@
 // Kernels: att_fwd, att_dq and att_dkv serve every case with one simple loop; the pipelined ones further down serve bf16
 // with heads of whole 16-byte chunks, wherever those can be copied 16 bytes at a time.
 //
-// Measured (MI355X, bf16; a large library product reaches 1.47 PFLOP/s): forward of 32768 tokens, 40 heads over 8
-// of 128, in sequences of 26524 and 6244, 6.4 ms, 1.18 PFLOP/s, matrix cores busy 0.59 at 1.81 GHz (the power
+// Measured (MI355X, bf16; a large library product reaches 1.6 PFLOP/s): forward of 32768 tokens, 40 heads over 8
+// of 128, in sequences of 26524 and 6244, 6.4 to 6.7 ms, 1.14 to 1.19 PFLOP/s, matrix cores busy 0.59 at 1.81 GHz (the power
 // limit); of 28 heads over 4, in ten sequences around 3400, 1.0 ms, 0.9 PFLOP/s.  Backward of 16384 tokens of the
 // latter in five, 2.0 ms: dk and dv 1.24, dq 0.74 (0.58 PFLOP/s counting five products; seven are formed).  The
 // simple loops took 17.9, 2.15 and 10.4 ms: their registers spill, and every fragment read is waited for.

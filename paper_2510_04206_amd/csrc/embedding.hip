@@ -21,7 +21,7 @@
 //
 // Measured (MI355X; a copy of 2 GiB moves 4.9 TB/s, a fill 6.9): forward of 65536 x 5120 bf16 out of [152064, 5120]
 // 213 us (6.2 TB/s of rows, the repeated ones from the caches).  Backward of the same, the whole gradient written,
-// 816 us: rows 712 (3.8 GB), sort 68, join 34; 3823 x 1001 fp32 onto a [4096, 1001] 34 us: three launches of 13, 10 and 8.
+// 806 us: rows 712 (3.8 GB), sort 54, join 36; 3823 x 1001 fp32 onto a [4096, 1001] 31 us: three launches of 11, 10 and 9.
 #include <math.h>
 
 #include "rows.hpp"
