@@ -563,9 +563,10 @@ __global__ void __launch_bounds__(THREADS, sizeof(T) == 2 ? 2 : 1) att_fwd_kerne
 //
 // The softmax's reference is the row's own score q k, which is one of those that count: the sum is at least 1, and
 // there is no running maximum to follow.  Weights may grow to 2^96 before that fails (scores 66 above the row's own);
-// then, or where a NaN or infinite element of V met a weight of 0, a result
-// is not finite, and the workgroup goes through its tile again step by step, with references that follow the maximum
-// and masked elements taken out.
+// then, or where a result is not finite (a NaN or infinite element of V met a weight of 0, or a weight times a large one
+// left the range), the workgroup goes through its tile again step by step, masked elements taken out.  There a row whose
+// sum had left its range follows its maximum.  Any other keeps its reference: its results have the bits of the first pass, and
+// where they were not finite its weights are taken down by the power of 2 of its sum, which changes no mantissa.
 constexpr int PIPE_ROWS = 64 * WAVES;
 
 template <int N, class F>
@@ -822,17 +823,21 @@ __global__ void __launch_bounds__(THREADS, 1) att_fwd_pipe_kernel(AttArgs a) {
     arrive(t);
     slot = slot == 2 ? 0 : slot + 1;
   }
-  bool lost = false;
+  bool lost = false, follow[2];
+  float up[2] = {1.0f, 1.0f};            // what the weights of the second pass are smaller by
 #pragma unroll
   for (int cb = 0; cb < 2; ++cb) {
-    m[cb] = ref[cb];
     l[cb] += other_half(l[cb]);
-    float z = l[cb] > 0.5f && l[cb] < 0x1p96f ? 0.0f : 1.0f;
+    follow[cb] = !(l[cb] > 0.5f && l[cb] < 0x1p96f);
+    m[cb] = follow[cb] ? -INFINITY : ref[cb];
+    float z = 0.0f;
 #pragma unroll
     for (int c = 0; c < ND; ++c)
 #pragma unroll
       for (int r = 0; r < 16; ++r) z = fmaf(o[cb][c][r], 0.0f, z);
-    lost = lost || (at[cb].live && z != 0.0f);       // (1 or NaN)
+    z += other_half(z);                  // 0 or NaN
+    lost = lost || (at[cb].live && (follow[cb] || z != 0.0f));
+    if (!follow[cb] && z != 0.0f && l[cb] > 1.0f) up[cb] = __uint_as_float(__float_as_uint(l[cb]) & 0x7f800000u);
   }
   if (__syncthreads_or(lost)) {
 #pragma unroll
@@ -861,9 +866,9 @@ __global__ void __launch_bounds__(THREADS, 1) att_fwd_pipe_kernel(AttArgs a) {
             top = fmaxf(top, s[r]);
           }
           top = fmaxf(top, other_half(top)) * sl2;
-          // (rows that nothing was wrong with keep their reference, and so their bits)
-          const bool far = top > m[cb] + 64.0f;
+          const bool far = follow[cb] && top > m[cb];
           const float to = far ? top : m[cb], f = far ? __builtin_amdgcn_exp2f(m[cb] - to) : 1.0f;
+          const float down = __uint_as_float(0x7f000000u - __float_as_uint(up[cb]));        // 1 / up
           m[cb] = to;
           l[cb] *= f;
 #pragma unroll
@@ -872,7 +877,7 @@ __global__ void __launch_bounds__(THREADS, 1) att_fwd_pipe_kernel(AttArgs a) {
           u32x4 p[NP];
 #pragma unroll
           for (int r = 0; r < 16; ++r) {
-            s[r] = __builtin_amdgcn_exp2f(fmaf(s[r], sl2, -from));
+            s[r] = __builtin_amdgcn_exp2f(fmaf(s[r], sl2, -from)) * down;
             l[cb] += s[r];
           }
 #pragma unroll
@@ -889,7 +894,7 @@ __global__ void __launch_bounds__(THREADS, 1) att_fwd_pipe_kernel(AttArgs a) {
   for (int cb = 0; cb < 2; ++cb) {
     const int n = cb ? nB : nA;
     if (a.lse && n < a.T && lane < 32)
-      a.lse[(int64_t)head * a.T + n] = at[cb].live ? LN2 * (m[cb] + __builtin_amdgcn_logf(l[cb])) : 0.0f;
+      a.lse[(int64_t)head * a.T + n] = at[cb].live ? LN2 * (m[cb] + __builtin_amdgcn_logf(l[cb] * up[cb])) : 0.0f;
     put_row<T, DP, FULL>((T*)a.o.p + head * a.o.hs + (int64_t)n * a.o.ld, o[cb], 1.0f / l[cb], !at[cb].live,
                          n < a.T, a.d);
   }
