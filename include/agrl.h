@@ -516,6 +516,9 @@ int agrl_rotate_heads(int64_t T, int32_t n_head, int32_t d, int32_t rot, int32_t
  *   scale             2^-60 to 2^60
  * Outputs: o [T, n_head, d]; lse [n_head, T] fp32 (NULL: not written; the backward needs it).
  * Products of bf16 inputs and all sums are fp32, P is rounded to `dtype` before it meets v, o once.
+ * Scores may have any size that fp32 holds: the largest weight of a row is 1, the others are as exact as fp32 holds the
+ * differences of scores.  Sums of weights times v are fp32, weights up to 2^8 before the row is divided: the keys of a row
+ * times 2^8 |v| should stay within its range.
  * No token of another sequence and no later one of its own reaches a row, not even a NaN or
  * infinite one; an element of v that is not finite makes what counts it NaN or infinite.
  */
@@ -533,7 +536,8 @@ size_t agrl_attention_bwd_workspace_size(int64_t T, int32_t n_head, int32_t n_kv
  * Gradients of agrl_attention_fwd.  With P = exp(S - lse), D = sum over d of dout o and
  * dS = P (dout v^T - D):  dv = P^T dout, dq = scale dS k, dk = scale dS^T q; dk and dv are the sums over
  * the query heads that share a key head (in a fixed order).
- *   o, lse            as the forward left them; dout [T, n_head, d] in `dtype`
+ *   o, lse            as the forward left them (P is as exact as fp32 holds S and lse, so a lse formed in another way makes it
+ *                     off by exp of its difference); dout [T, n_head, d] in `dtype`
  *   workspace         256-byte aligned, agrl_attention_bwd_workspace_size bytes
  * Outputs in `dtype`: dq [T, n_head, d], dk and dv [T, n_kv, d] (+0 on tokens of no sequence); they may be
  * parts of one array [T, n_head + 2 n_kv, d].  P and dS are rounded to `dtype` before they

@@ -43,6 +43,21 @@ typedef uint16_t u16x2 __attribute__((ext_vector_type(2)));
 
 constexpr float LOG2E = 1.44269504088896341f, LN2 = 0.693147180559945309f;
 
+// Scores past some 2^24 are many units apart in fp32, and an exponent formed from two roundings of one score is off by as
+// much.  Such rows therefore subtract before they scale in the forward (the largest weight is exactly 1), their lse is scale m
+// + ln l, rounded once, and the backward takes S with the same rounding: where one key is all of a row,
+// S is the lse and the weight 1.  (No weight is above 1: both roundings are of growing functions.)  Up to FAR powers of 2
+// one fused operation does: it is off by 3 FAR 2^-24 = 2^-10.4 of a weight at most, less than a bf16 weight's rounding.
+constexpr float FAR = 4096.0f;
+__device__ __forceinline__ float row_lse(float m, float scale, float l) {
+  return fmaf(m, scale, LN2 * __builtin_amdgcn_logf(l));
+}
+__device__ __forceinline__ float weight_log2(float s, float scale, float lse) {
+#pragma clang fp contract(off)
+  const float S = s * scale;
+  return (S - lse) * LOG2E;
+}
+
 // [T, n_head, d]: rows `ld`, heads `hs` elements apart
 struct Heads {
   const void* p;
@@ -405,8 +420,9 @@ struct AttArgs {
   int* err;
   // backward
   Heads dout;
-  const float *lse2, *delta;     // [n_head, T]: lse in powers of 2, sum do o
+  const float *lse_in, *lse2, *delta;      // [n_head, T]: the forward's lse, in powers of 2, sum do o
   const int32_t* order;          // key tiles in the order they are taken
+  const uint8_t* far;            // [FLAGS] whether some row's lse is past FAR: not 0 anywhere
   HeadsOut dq, dk, dv;
   int32_t splits;                // parts that a group's heads are dealt to, each a workgroup's
   float* part;                   // more than one: [splits][2][T, n_kv, d] sums of dk and dv
@@ -509,13 +525,13 @@ __global__ void __launch_bounds__(THREADS, sizeof(T) == 2 ? 2 : 1) att_fwd_kerne
 #pragma unroll
         for (int r = 0; r < 16; ++r) top = fmaxf(top, s[b][r]);
       }
-      top = fmaxf(top, other_half(top)) * sl2;
+      top = fmaxf(top, other_half(top));
       // a column's reference moves only when the maximum has left it 2^8 behind: any reference gives the same
       // quotient (and a column's own, so no other row's values change its roundings)
-      const bool far = top > m + 8.0f;
+      const bool far = (top - m) * sl2 > 8.0f;
       if (__any(far)) {
         const float to = far ? top : m;
-        const float f = far ? __builtin_amdgcn_exp2f(m - to) : 1.0f;
+        const float f = far ? __builtin_amdgcn_exp2f((m - to) * sl2) : 1.0f;
         l *= f;
 #pragma unroll
         for (int c = 0; c < TL::ND; ++c) o[c] *= f;
@@ -527,7 +543,7 @@ __global__ void __launch_bounds__(THREADS, sizeof(T) == 2 ? 2 : 1) att_fwd_kerne
         u32x4 p[TL::NP];
 #pragma unroll
         for (int r = 0; r < 16; ++r) {
-          s[b][r] = __builtin_amdgcn_exp2f(fmaf(s[b][r], sl2, -ref));
+          s[b][r] = __builtin_amdgcn_exp2f((s[b][r] - ref) * sl2);
           l += s[b][r];
         }
 #pragma unroll
@@ -549,7 +565,7 @@ __global__ void __launch_bounds__(THREADS, sizeof(T) == 2 ? 2 : 1) att_fwd_kerne
   }
   l += other_half(l);
   if (a.lse && n < a.T && lane < 32)
-    a.lse[(int64_t)head * a.T + n] = at.live ? LN2 * (m + __builtin_amdgcn_logf(l)) : 0.0f;
+    a.lse[(int64_t)head * a.T + n] = at.live ? row_lse(m, a.scale, l) : 0.0f;
   put_row<T, DP, FULL>((T*)a.o.p + head * a.o.hs + (int64_t)n * a.o.ld, o, 1.0f / l, !at.live, n < a.T, a.d);
 }
 
@@ -565,7 +581,7 @@ __global__ void __launch_bounds__(THREADS, sizeof(T) == 2 ? 2 : 1) att_fwd_kerne
 // there is no running maximum to follow.  Weights may grow to 2^96 before that fails (scores 66 above the row's own);
 // then, or where a result is not finite (a NaN or infinite element of V met a weight of 0, or a weight times a large one
 // left the range), the workgroup goes through its tile again step by step, masked elements taken out.  There a row whose
-// sum had left its range follows its maximum.  Any other keeps its reference: its results have the bits of the first pass, and
+// sum had left its range, or whose own score is past FAR, follows its maximum.  Any other keeps its reference: its results have the bits of the first pass, and
 // where they were not finite its weights are taken down by the power of 2 of its sum, which changes no mantissa.
 constexpr int PIPE_ROWS = 64 * WAVES;
 
@@ -828,7 +844,7 @@ __global__ void __launch_bounds__(THREADS, 1) att_fwd_pipe_kernel(AttArgs a) {
 #pragma unroll
   for (int cb = 0; cb < 2; ++cb) {
     l[cb] += other_half(l[cb]);
-    follow[cb] = !(l[cb] > 0.5f && l[cb] < 0x1p96f);
+    follow[cb] = !(l[cb] > 0.5f && l[cb] < 0x1p96f && fabsf(ref[cb]) <= FAR);
     m[cb] = follow[cb] ? -INFINITY : ref[cb];
     float z = 0.0f;
 #pragma unroll
@@ -865,9 +881,9 @@ __global__ void __launch_bounds__(THREADS, 1) att_fwd_pipe_kernel(AttArgs a) {
             s[r] = in ? s[r] : -INFINITY;
             top = fmaxf(top, s[r]);
           }
-          top = fmaxf(top, other_half(top)) * sl2;
-          const bool far = follow[cb] && top > m[cb];
-          const float to = far ? top : m[cb], f = far ? __builtin_amdgcn_exp2f(m[cb] - to) : 1.0f;
+          top = fmaxf(top, other_half(top));
+          const bool far = follow[cb] && top > m[cb];         // (m: a score; of the others, the reference in powers of 2)
+          const float to = far ? top : m[cb], f = far ? __builtin_amdgcn_exp2f((m[cb] - to) * sl2) : 1.0f;
           const float down = __uint_as_float(0x7f000000u - __float_as_uint(up[cb]));        // 1 / up
           m[cb] = to;
           l[cb] *= f;
@@ -877,7 +893,7 @@ __global__ void __launch_bounds__(THREADS, 1) att_fwd_pipe_kernel(AttArgs a) {
           u32x4 p[NP];
 #pragma unroll
           for (int r = 0; r < 16; ++r) {
-            s[r] = __builtin_amdgcn_exp2f(fmaf(s[r], sl2, -from)) * down;
+            s[r] = __builtin_amdgcn_exp2f(follow[cb] ? (s[r] - from) * sl2 : fmaf(s[r], sl2, -from)) * down;
             l[cb] += s[r];
           }
 #pragma unroll
@@ -894,7 +910,9 @@ __global__ void __launch_bounds__(THREADS, 1) att_fwd_pipe_kernel(AttArgs a) {
   for (int cb = 0; cb < 2; ++cb) {
     const int n = cb ? nB : nA;
     if (a.lse && n < a.T && lane < 32)
-      a.lse[(int64_t)head * a.T + n] = at[cb].live ? LN2 * (m[cb] + __builtin_amdgcn_logf(l[cb] * up[cb])) : 0.0f;
+      a.lse[(int64_t)head * a.T + n] = !at[cb].live  ? 0.0f
+                                       : follow[cb] ? row_lse(m[cb], a.scale, l[cb])
+                                                    : LN2 * (m[cb] + __builtin_amdgcn_logf(l[cb] * up[cb]));
     put_row<T, DP, FULL>((T*)a.o.p + head * a.o.hs + (int64_t)n * a.o.ld, o[cb], 1.0f / l[cb], !at[cb].live,
                          n < a.T, a.d);
   }
@@ -909,7 +927,9 @@ struct DeltaArgs {
   float *lse2, *delta;
   const int32_t* start;
   int32_t* order;       // [tiles of BM keys], those with the most rows first
+  uint8_t* far;         // [FLAGS] whether a workgroup met a row whose lse is past FAR
 };
+constexpr int FLAGS = 16 * THREADS;
 
 // The key tiles by the rows that count them, in 256 classes (the order within one does not matter: each tile's
 // results are its own).  One workgroup.
@@ -948,8 +968,12 @@ __device__ __forceinline__ void order_tiles(const DeltaArgs& a) {
 
 template <typename T>
 __global__ void __launch_bounds__(256) att_delta_kernel(DeltaArgs a) {
-  if (blockIdx.x == gridDim.x - 1) return order_tiles(a);
+  if (blockIdx.x == gridDim.x - 1) {
+    for (int i = gridDim.x - 1 + threadIdx.x; i < FLAGS; i += 256) a.far[i] = 0;
+    return order_tiles(a);
+  }
   const int l = threadIdx.x & 15, team = threadIdx.x >> 4;
+  bool far = false;
   for (int64_t i = (int64_t)blockIdx.x * 16 + team; i < (int64_t)a.T * a.n_head; i += (int64_t)(gridDim.x - 1) * 16) {
     const int n = (int)(i / a.n_head), h = (int)(i - (int64_t)n * a.n_head);
     const T* o = (const T*)a.o.p + (int64_t)n * a.o.ld + h * a.o.hs;
@@ -973,9 +997,13 @@ __global__ void __launch_bounds__(256) att_delta_kernel(DeltaArgs a) {
     sum = dpp_add<0x140>(sum);
     if (l == 0) {
       a.delta[(int64_t)h * a.T + n] = sum;
-      a.lse2[(int64_t)h * a.T + n] = a.lse[(int64_t)h * a.T + n] * LOG2E;
+      const float z = a.lse[(int64_t)h * a.T + n] * LOG2E;
+      a.lse2[(int64_t)h * a.T + n] = z;
+      far = far || fabsf(z) > FAR;
     }
   }
+  far = __syncthreads_or(far);
+  if (threadIdx.x == 0) a.far[blockIdx.x] = far;
 }
 
 // dq: queries in the columns as in the forward; dS^T is the operand that meets K^T.
@@ -1003,11 +1031,10 @@ __global__ void __launch_bounds__(THREADS, sizeof(T) == 2 ? 2 : 1) att_dq_kernel
   u32x4 q[TL::NS], g[TL::NS];
   hold<T, DP, FULL>(q, (const T*)a.q.p + head * a.q.hs + (int64_t)n * a.q.ld, at.live, a.d);
   hold<T, DP, FULL>(g, (const T*)a.dout.p + head * a.dout.hs + (int64_t)n * a.dout.ld, at.live, a.d);
-  const float lse2 = at.live ? a.lse2[(int64_t)head * a.T + n] : 0.0f;
+  const float lse = at.live ? a.lse_in[(int64_t)head * a.T + n] : 0.0f;
   const float delta = at.live ? a.delta[(int64_t)head * a.T + n] : 0.0f;
   const T* kp = (const T*)a.k.p + kv * a.k.hs;
   const T* vp = (const T*)a.v.p + kv * a.v.hs;
-  const float sl2 = a.scale * LOG2E;
   f32x16 dq[TL::ND] = {};
   Stage<T, DP, R, THREADS, FULL> sk, sv;
   const int kt0 = lo / R * R;
@@ -1034,7 +1061,7 @@ __global__ void __launch_bounds__(THREADS, sizeof(T) == 2 ? 2 : 1) att_dq_kernel
         uint32_t ok = 0;
 #pragma unroll
         for (int r = 0; r < 16; ++r) {
-          s[r] = __builtin_amdgcn_exp2f(fmaf(s[r], sl2, -lse2)) * (dp[r] - delta);
+          s[r] = __builtin_amdgcn_exp2f(weight_log2(s[r], a.scale, lse)) * (dp[r] - delta);
           if constexpr (MASKED) {
             const bool in = (uint32_t)(k0 + 32 * b + acc_row(r) - at.begin) < len;
             ok |= in ? 1u << r : 0u;
@@ -1132,7 +1159,7 @@ __global__ void __launch_bounds__(THREADS, 1) att_dkv_kernel(AttArgs a) {
   __shared__ __align__(16) float lds_s[2][2][R];     // lse and D of the tile's rows
   __shared__ int lds_span[2][WAVES];
   const KeyTile w(a, blockIdx.x);
-  const int tile = a.order[w.rank], kv = w.kv, reps = w.heads;
+  const int tile = a.order[w.rank], kv = w.kv;
   const int wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6), lane = threadIdx.x & 63;
   const int first = tile * BM + wave * 32, n = first + (lane & 31);
   const Place at(a.start, a.n_seq, a.T, offsets_upto(a.start, a.n_seq, first),
@@ -1149,7 +1176,6 @@ __global__ void __launch_bounds__(THREADS, 1) att_dkv_kernel(AttArgs a) {
   u32x4 k[TL::NS], v[TL::NS];
   hold<T, DP, FULL>(k, (const T*)a.k.p + kv * a.k.hs + (int64_t)n * a.k.ld, at.live, a.d);
   hold<T, DP, FULL>(v, (const T*)a.v.p + kv * a.v.hs + (int64_t)n * a.v.ld, at.live, a.d);
-  const float sl2 = a.scale * LOG2E;
   f32x16 dk[TL::ND] = {}, dv[TL::ND] = {};
   Stage<T, DP, R, THREADS, FULL> sq, sg;
   float stat = 0.0f;
@@ -1160,7 +1186,7 @@ __global__ void __launch_bounds__(THREADS, 1) att_dkv_kernel(AttArgs a) {
     sg.load((const T*)a.dout.p + head * a.dout.hs, a.dout.ld, q0, a.T, a.d);
     const int r = q0 + (threadIdx.x & (R - 1));
     if (threadIdx.x < 2 * R && r < a.T)
-      stat = (threadIdx.x < R ? a.lse2 : a.delta)[(int64_t)head * a.T + r];
+      stat = (threadIdx.x < R ? a.lse_in : a.delta)[(int64_t)head * a.T + r];
   };
   auto store = [&](int buf) {
     sq.store(lds_q[buf]);
@@ -1190,7 +1216,7 @@ __global__ void __launch_bounds__(THREADS, 1) att_dkv_kernel(AttArgs a) {
 #pragma unroll
           for (int e = 0; e < 4; ++e) {
             const int r = 4 * g + e;
-            s[r] = __builtin_amdgcn_exp2f(fmaf(s[r], sl2, -z[e]));
+            s[r] = __builtin_amdgcn_exp2f(weight_log2(s[r], a.scale, z[e]));
             ds[r] = s[r] * (ds[r] - del[e]);
             if constexpr (MASKED) {
               const uint32_t after = q0 + 32 * b + acc_row(r) - n;
@@ -1226,13 +1252,20 @@ __global__ void __launch_bounds__(THREADS, 1) att_dkv_kernel(AttArgs a) {
 // ------------------------------------------------------------------ backward, pipelined
 // As in the forward: a slot per MFMA, the vector ALU's share of a half of 32 rows spread over the slots of a phase,
 // fragments read AHEAD of their use, tiles of 64 rows copied into rings.  Weights are at most 1, so nothing needs
-// a reference; a result that is not finite sends the workgroup through its tile again, step by step
-// with masked elements taken out.
+// a reference; a result that is not finite, or a row whose lse is past FAR, sends the workgroup through its tile again, step by
+// step with masked elements taken out.
 
 // lane R of the lane's group of 16, as an operand
 template <int R>
 __device__ __forceinline__ float row_lane(float v) {
   return __int_as_float(__builtin_amdgcn_update_dpp(0, __float_as_int(v), 0x150 + R, 0xf, 0xf, false));
+}
+
+// log2 of a weight as the pipeline of dk and dv forms it, from the forward's lse
+__device__ __forceinline__ float near_log2(float s, float lse, float sl2) {
+#pragma clang fp contract(off)
+  const float lse2 = lse * LOG2E, z = lse2 * (1.0f / sl2);
+  return (s - z) * sl2;
 }
 
 // dk, dv: 32 keys a wave.  A phase forms the next half's S and dP, the previous half's shares of dv and dk, and on the
@@ -1362,7 +1395,7 @@ __global__ void __launch_bounds__(THREADS, 1) att_dkv_pipe_kernel(AttArgs a) {
   // Step u of the walk: all heads of the group at one tile, from the last tile to the first.  Key tiles of one sequence
   // then start on the same rows and stay with each other, sharing them through the XCD's L2.
   float stat = 0.0f;
-  const float to_stat = threadIdx.x < 64 ? 1.0f / sl2 : 1.0f;
+  float to_stat = threadIdx.x < 64 ? 1.0f / sl2 : 1.0f;
   auto load_stat = [&](int u) {
     const int row = (t1 - 1 - u / reps) * 64 + (threadIdx.x & 63);
     if (threadIdx.x < 128 && u < steps && row < a.T) stat = stats[(int64_t)(u % reps) * a.T + row];
@@ -1453,9 +1486,20 @@ __global__ void __launch_bounds__(THREADS, 1) att_dkv_pipe_kernel(AttArgs a) {
   for (int c = 0; c < ND; ++c)
 #pragma unroll
     for (int r = 0; r < 16; ++r) bad = fmaf(dk[c][r], 0.0f, fmaf(dv[c][r], 0.0f, bad));
-  if (__syncthreads_or(at.live && bad != 0.0f)) {
+  // Rows past FAR: looked for where some row of the stream is one.  (A maximum kept where the statistics pass by cost the
+  // pipeline 4%, a look at all of the tile's rows each time 1.5%.)
+  bool far = false;
+  const u32x4 some = ((const u32x4*)a.far)[threadIdx.x];
+  if (__syncthreads_or((some.x | some.y | some.z | some.w) != 0))
+    for (int h = 0; h < reps; ++h) {
+      const float* z = a.lse2 + (int64_t)(w.head + h) * a.T;
+      for (int r = lo + threadIdx.x; r < hi; r += THREADS) far = far || fabsf(z[r]) > FAR;
+    }
+  if (__syncthreads_or((at.live && bad != 0.0f) || far)) {
 #pragma unroll
     for (int c = 0; c < ND; ++c) dk[c] = dv[c] = f32x16{};
+    if (threadIdx.x < 64) stats = a.lse_in + (int64_t)w.head * a.T;
+    to_stat = 1.0f;
     begin();
     for (u = 0; u < steps; ++u) {
         arrive(u, true);
@@ -1472,7 +1516,9 @@ __global__ void __launch_bounds__(THREADS, 1) att_dkv_pipe_kernel(AttArgs a) {
             const uint32_t after = t * 64 + 32 * b + acc_row(r) - n;
             const bool in = after < len;
             ok |= in ? 1u << r : 0u;
-            s[r] = __builtin_amdgcn_exp2f(in ? (s[r] - st[acc_row(r)]) * sl2 : -INFINITY);
+            const float lse = st[acc_row(r)];
+            const float x = fabsf(lse * LOG2E) <= FAR ? near_log2(s[r], lse, sl2) : weight_log2(s[r], a.scale, lse);
+            s[r] = __builtin_amdgcn_exp2f(in ? x : -INFINITY);
             ds[r] = in && !(head_of && after == 0) ? s[r] * (ds[r] - st[64 + acc_row(r)]) : 0.0f;
             s[r] = in ? s[r] : 0.0f;
           }
@@ -1684,7 +1730,7 @@ __global__ void __launch_bounds__(THREADS, 1) att_dq_pipe_kernel(AttArgs a) {
     for (int c = 0; c < ND; ++c)
 #pragma unroll
       for (int r = 0; r < 16; ++r) z = fmaf(dq[cb][c][r], 0.0f, z);
-    lost = lost || (at[cb].live && z != 0.0f);
+    lost = lost || (at[cb].live && (z != 0.0f || !(fabsf(lse2[cb]) <= FAR)));
   }
   if (__syncthreads_or(lost)) {
 #pragma unroll
@@ -1698,6 +1744,7 @@ __global__ void __launch_bounds__(THREADS, 1) att_dq_pipe_kernel(AttArgs a) {
 #pragma unroll
       for (int cb = 0; cb < 2; ++cb) {
         if (t * 64 + 64 <= part[cb].lo || t * 64 >= part[cb].hi) continue;
+        const float lse = at[cb].live ? a.lse_in[(int64_t)head * a.T + (cb ? nB : nA)] : 0.0f;
 #pragma unroll 1
         for (int b = 0; b < 2; ++b) {
           f32x16 s = mul_rows<T, DP>(k + b * 32 * ROW, L, 0, q[cb]);
@@ -1707,7 +1754,9 @@ __global__ void __launch_bounds__(THREADS, 1) att_dq_pipe_kernel(AttArgs a) {
           for (int r = 0; r < 16; ++r) {
             const bool in = (uint32_t)(t * 64 + 32 * b + acc_row(r) - at[cb].begin) < len[cb];
             ok |= in ? 1u << r : 0u;
-            s[r] = __builtin_amdgcn_exp2f(fmaf(in ? s[r] : -INFINITY, sl2, -lse2[cb]));
+            s[r] = in ? s[r] : -INFINITY;
+            s[r] = __builtin_amdgcn_exp2f(fabsf(lse2[cb]) <= FAR ? fmaf(s[r], sl2, -lse2[cb])
+                                                                 : weight_log2(s[r], a.scale, lse));
             s[r] = in && len[cb] > 1 ? s[r] * (d[r] - delta[cb]) : 0.0f;
           }
           u32x4 e[NP];
@@ -1757,7 +1806,7 @@ int att_splits(int64_t T, int32_t n_head, int32_t n_kv) {
 }
 
 struct AttSpace {
-  size_t delta, order, part, total;
+  size_t delta, order, far, part, total;
 };
 AttSpace att_space(int64_t T, int32_t n_head, int32_t n_kv, int32_t d) {
   auto up = [](size_t n) { return (n + 255) & ~(size_t)255; };
@@ -1765,7 +1814,8 @@ AttSpace att_space(int64_t T, int32_t n_head, int32_t n_kv, int32_t d) {
   AttSpace s;
   s.delta = up((size_t)T * n_head * 4);
   s.order = 2 * s.delta;
-  s.part = s.order + up((size_t)cdiv(T, (int64_t)BM) * 4);
+  s.far = s.order + up((size_t)cdiv(T, (int64_t)BM) * 4);
+  s.part = s.far + FLAGS;
   s.total = s.part + (splits > 1 ? (size_t)splits * 2 * T * n_kv * d * 4 : 0);
   return s;
 }
@@ -1879,10 +1929,12 @@ extern "C" int agrl_attention_bwd(int64_t T, int32_t n_seq, int32_t n_head, int3
   float* lse2 = (float*)ws;
   float* delta = (float*)(ws + sp.delta);
   int32_t* order = (int32_t*)(ws + sp.order);
+  uint8_t* far = ws + sp.far;
   const DeltaArgs de = {(int32_t)T, n_head, d, n_seq, {o, ld_o, head_o}, {dout, ld_do, head_do}, lse, lse2, delta,
-                        seq_start, order};
+                        seq_start, order, far};
   const int64_t need = cdiv(T * n_head, (int64_t)16), most = (int64_t)device_cu_count() * 16;
-  const dim3 dgrid((unsigned)(need < most ? need : most) + 1);
+  const int64_t dwork = need < most ? need : most;
+  const dim3 dgrid((unsigned)(dwork < FLAGS ? dwork : FLAGS) + 1);
   if (dtype == AGRL_BF16)
     hipLaunchKernelGGL(att_delta_kernel<uint16_t>, dgrid, dim3(256), 0, s, de);
   else
@@ -1891,7 +1943,7 @@ extern "C" int agrl_attention_bwd(int64_t T, int32_t n_seq, int32_t n_head, int3
   a.T = (int32_t)T, a.n_seq = n_seq, a.n_head = n_head, a.n_kv = n_kv, a.rep = n_head / n_kv, a.d = d;
   a.q = {q, ld_q, head_q}, a.k = {k, ld_k, head_k}, a.v = {v, ld_v, head_v};
   a.start = seq_start, a.scale = scale, a.err = device_error_ptr();
-  a.dout = {dout, ld_do, head_do}, a.lse2 = lse2, a.delta = delta, a.order = order;
+  a.dout = {dout, ld_do, head_do}, a.lse_in = lse, a.lse2 = lse2, a.delta = delta, a.order = order, a.far = far;
   a.splits = att_splits(T, n_head, n_kv), a.part = (float*)(ws + sp.part);
   a.dq = {dq, ld_dq, head_dq}, a.dk = {dk, ld_dk, head_dk}, a.dv = {dv, ld_dv, head_dv};
   const int64_t tiles = cdiv(T, (int64_t)BM);
