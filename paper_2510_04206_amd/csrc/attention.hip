@@ -350,6 +350,22 @@ __device__ __forceinline__ f32x16 mul_rows(const uint8_t* x, const typename Tile
   return acc;
 }
 
+// The same of a padded head of whole chunks, for the second pass of the pipelines.  Past d their tiles repeat the last chunk,
+// and the zeros that it meets there would make a NaN of an infinite element: taken as 0.
+template <typename T, int DP, bool FULL, int NS>
+__device__ __forceinline__ f32x16 mul_rows_upto(const uint8_t* x, const typename Tile<T, DP>::Lane& L, int b,
+                                                const u32x4 (&f)[NS], int d) {
+  if constexpr (FULL) return mul_rows<T, DP>(x, L, b, f);
+  const int h = (threadIdx.x & 63) >> 5;
+  f32x16 acc = {};
+#pragma unroll
+  for (int s = 0; s < NS; ++s) {
+    const u32x4 v = Tile<T, DP>::rows(x, L, b, s);
+    acc = Mma<T>::mma((2 * s + h) * Mma<T>::E < d ? v : u32x4{0, 0, 0, 0}, f[s], acc);
+  }
+  return acc;
+}
+
 // row of accumulator element r within its block
 __device__ __forceinline__ int acc_row(int r) { return 8 * (r >> 2) + (r & 3) + 4 * ((threadIdx.x & 63) >> 5); }
 
@@ -600,7 +616,8 @@ struct Copy {
   uint32_t r, c, off;        // lane's row and byte of the first copy, its offset
   uint32_t lds;
   int T;
-  // (the places past a head of d elements get its last chunk again: they meet zeros, or are not stored)
+  // (the places past a head of d elements get its last chunk again: they meet zeros, or are not stored; where that chunk is not
+  // finite the second pass takes them out)
   __device__ __forceinline__ void init(const void* head, int64_t ld, uint32_t lds_base, int wave, int rows, int d) {
     const int lane = threadIdx.x & 63;
     p = (const uint8_t*)head;
@@ -871,7 +888,7 @@ __global__ void __launch_bounds__(THREADS, 1) att_fwd_pipe_kernel(AttArgs a) {
         if (t * 64 + 64 <= part[cb].lo || t * 64 >= part[cb].hi) continue;
 #pragma unroll
         for (int b = 0; b < 2; ++b) {
-          f32x16 s = mul_rows<T, DP>(lds_k + at_k, L, b, q[cb]);
+          f32x16 s = mul_rows_upto<T, DP, FULL>(lds_k + at_k, L, b, q[cb], a.d);
           uint32_t ok = 0;
           float top = -INFINITY;
 #pragma unroll
@@ -1508,7 +1525,8 @@ __global__ void __launch_bounds__(THREADS, 1) att_dkv_pipe_kernel(AttArgs a) {
         const uint8_t* q = lds + (u & 3) * SLOT;
 #pragma unroll 1
         for (int b = 0; b < 2; ++b) {
-          f32x16 s = mul_rows<T, DP>(q + b * 32 * ROW, L, 0, k), ds = mul_rows<T, DP>(q + b * 32 * ROW + TB, L, 0, v);
+          f32x16 s = mul_rows_upto<T, DP, FULL>(q + b * 32 * ROW, L, 0, k, a.d);
+          f32x16 ds = mul_rows_upto<T, DP, FULL>(q + b * 32 * ROW + TB, L, 0, v, a.d);
           const float* st = (const float*)(lds_s + (u & 3) * STAT) + 32 * b;
           uint32_t ok = 0;
 #pragma unroll
@@ -1747,8 +1765,8 @@ __global__ void __launch_bounds__(THREADS, 1) att_dq_pipe_kernel(AttArgs a) {
         const float lse = at[cb].live ? a.lse_in[(int64_t)head * a.T + (cb ? nB : nA)] : 0.0f;
 #pragma unroll 1
         for (int b = 0; b < 2; ++b) {
-          f32x16 s = mul_rows<T, DP>(k + b * 32 * ROW, L, 0, q[cb]);
-          const f32x16 d = mul_rows<T, DP>(v + b * 32 * ROW, L, 0, g[cb]);
+          f32x16 s = mul_rows_upto<T, DP, FULL>(k + b * 32 * ROW, L, 0, q[cb], a.d);
+          const f32x16 d = mul_rows_upto<T, DP, FULL>(v + b * 32 * ROW, L, 0, g[cb], a.d);
           uint32_t ok = 0;
 #pragma unroll
           for (int r = 0; r < 16; ++r) {
