@@ -464,7 +464,8 @@ size_t agrl_token_embed_bwd_workspace_size(int64_t T, int32_t d, int32_t V);
 /*
  * Gradient of the embedding: dweight[v] = scale * sum of dy[n] over the live tokens n with
  * token_id[n] = v, in the tokens' order, in fp32.
- *   V                 <= 2^31 - 1024
+ *   V                 <= 2^31 - 1024; ceil(T / 32) ceil(d / 1024) (T <= 512: T of them), and ceil(V / 8) with accumulate 0,
+ *                     below 2^24 together
  *   dy[T, d]          in dy_dtype, rows ld_dy >= d elements apart, from any element
  *   accumulate        0: every row of dweight is written (0 where no token has its id); 1: the
  *                     sums are added, rows without a token are not touched.  A tied head's
@@ -505,7 +506,8 @@ int agrl_rotate_heads(int64_t T, int32_t n_head, int32_t d, int32_t rot, int32_t
  * Causal attention within each sequence of a packed stream of T tokens:
  *   S = scale q k^T over the keys of the token's sequence up to the token itself,
  *   o = softmax(S) v,  lse = log sum exp S
- *   n_head, n_kv      query heads; key heads, a divisor: query head h reads key head h / (n_head / n_kv)
+ *   n_head, n_kv      query heads; key heads, a divisor: query head h reads key head h / (n_head / n_kv);
+ *                     ceil(T / 128) n_head < 2^24
  *   d                 head size, <= 128 (AGRL_E_UNSUPPORTED above)
  *   dtype             type of q, k, v and o: AGRL_BF16 or AGRL_F32
  *   q [T, n_head, d]; k, v [T, n_kv, d]

@@ -1795,6 +1795,7 @@ __global__ void __launch_bounds__(THREADS, 1) att_dq_pipe_kernel(AttArgs a) {
 
 constexpr int32_t ATT_MAX_D = 128;
 constexpr int64_t ATT_MAX_T = ((int64_t)1 << 31) - 65536;
+constexpr int64_t ATT_MAX_TILES = ((int64_t)1 << 24) - 1;      // workgroups of 256: less than the 2^32 lanes that HIP takes
 
 int att_check(const char* fn, int64_t T, int32_t n_seq, int32_t n_head, int32_t n_kv, int32_t d, int32_t dtype,
               float scale) {
@@ -1804,7 +1805,7 @@ int att_check(const char* fn, int64_t T, int32_t n_seq, int32_t n_head, int32_t 
     return fail(AGRL_E_SHAPE, fn, "bad T or n_seq");
   if (n_head <= 0 || n_kv <= 0 || n_head % n_kv || d <= 0)
     return fail(AGRL_E_SHAPE, fn, "n_head must be a multiple of n_kv, d positive");
-  if (cdiv(T, (int64_t)BM) * n_head >= 0x7fffffff) return fail(AGRL_E_SHAPE, fn, "T n_head is too large");
+  if (cdiv(T, (int64_t)BM) * n_head > ATT_MAX_TILES) return fail(AGRL_E_SHAPE, fn, "T n_head is too large");
   if (d > ATT_MAX_D) return fail(AGRL_E_UNSUPPORTED, fn, "d is larger than 128");
   // (the backward divides lse by it)
   if (!(scale >= 0x1p-60f && scale <= 0x1p60f))
@@ -1907,7 +1908,7 @@ extern "C" size_t agrl_attention_bwd_workspace_size(int64_t T, int32_t n_head, i
                                                     int32_t dtype) {
   using namespace agrl;
   if ((dtype != AGRL_BF16 && dtype != AGRL_F32) || T <= 0 || T > ATT_MAX_T || n_head <= 0 || n_kv <= 0 ||
-      n_head % n_kv || d <= 0 || d > ATT_MAX_D || cdiv(T, (int64_t)BM) * n_head >= 0x7fffffff)
+      n_head % n_kv || d <= 0 || d > ATT_MAX_D || cdiv(T, (int64_t)BM) * n_head > ATT_MAX_TILES)
     return 0;
   return att_space(T, n_head, n_kv, d).total;
 }

@@ -430,12 +430,14 @@ Space embed_space(int64_t T, int32_t d, int32_t V) {
 bool embed_sizes(int64_t T, int32_t d, int32_t V) {
   return T >= 0 && T <= MAX_TOKENS && d > 0 && d <= (1 << 20) && V > 0 && V < 0x7fffffff;
 }
-// The gradient's: a range of ids or rows past the last one still counts in 32 bits, every launch is within the grid's 2^31
-// workgroups
+// The gradient's: a range of ids or rows past the last one still counts in 32 bits, and every launch has less than the 2^32
+// lanes that HIP takes: workgroups of 256 that add, and with `clear` others that clear (the sort's have 1024 lanes and up to
+// 512 ids)
 constexpr int32_t MAX_IDS = 0x7fffffff - 1023;
-bool embed_bwd_sizes(int64_t T, int32_t d, int32_t V) {
+constexpr int64_t MAX_GROUPS = ((int64_t)1 << 24) - 1;
+bool embed_bwd_sizes(int64_t T, int32_t d, int32_t V, bool clear) {
   return embed_sizes(T, d, V) && V <= MAX_IDS &&
-         cdiv(T, (int64_t)MIN_CHUNK) * cdiv(d, SLAB) + cdiv(V, ZROWS) < 0x7fffffff;
+         (T <= FEW ? T : cdiv(T, (int64_t)chunk_of(T, d))) * cdiv(d, SLAB) + (clear ? cdiv(V, ZROWS) : 0) <= MAX_GROUPS;
 }
 
 }  // namespace
@@ -471,7 +473,7 @@ extern "C" int agrl_token_embed_fwd(int64_t T, int32_t d, int32_t V, int32_t w_d
 }
 
 extern "C" size_t agrl_token_embed_bwd_workspace_size(int64_t T, int32_t d, int32_t V) {
-  return agrl::embed_bwd_sizes(T, d, V) ? agrl::embed_space(T, d, V).total : 0;
+  return agrl::embed_bwd_sizes(T, d, V, false) ? agrl::embed_space(T, d, V).total : 0;
 }
 
 extern "C" int agrl_token_embed_bwd(int64_t T, int32_t d, int32_t V, int32_t dy_dtype,
@@ -482,7 +484,7 @@ extern "C" int agrl_token_embed_bwd(int64_t T, int32_t d, int32_t V, int32_t dy_
   const char* fn = "agrl_token_embed_bwd";
   if (dy_dtype != AGRL_BF16 && dy_dtype != AGRL_F32)
     return fail(AGRL_E_DTYPE, fn, "dy_dtype must be AGRL_BF16 or AGRL_F32");
-  if (!embed_bwd_sizes(T, d, V)) return fail(AGRL_E_SHAPE, fn, "bad T, d or V");
+  if (!embed_bwd_sizes(T, d, V, !accumulate)) return fail(AGRL_E_SHAPE, fn, "bad T, d or V");
   if (ld_dy < d) return fail(AGRL_E_SHAPE, fn, "ld_dy is smaller than d");
   if (!isfinite(scale)) return fail(AGRL_E_FLAGS, fn, "scale must be finite");
   if (accumulate != 0 && accumulate != 1) return fail(AGRL_E_FLAGS, fn, "accumulate must be 0 or 1");
