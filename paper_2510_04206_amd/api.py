@@ -457,10 +457,11 @@ class PackedAttention(_Owned):
     key heads (agrl_attention_*).
 
     ``forward(q, k, v, seq_start)`` returns (o [T, n_head, d], lse [n_head, T] fp32); ``backward(q, k, v,
-    seq_start, do)`` reads the o and lse of the last forward and returns (dq, dk, dv), three views of
+    seq_start, do)`` reads the o and lse of the last forward, or those given (copies that a program keeps of an earlier
+    one, so that layers can share a handle), and returns (dq, dk, dv), three views of
     ``dqkv`` [T, n_head + 2 n_kv, d], the gradient of a fused projection's output.  seq_start
-    [n_seq + 1] int32: sequence i is the tokens seq_start[i] .. seq_start[i + 1] - 1; tokens outside
-    are not read and get +0.  q, k and v may be views with any strides of rows and heads.
+    [n_seq + 1] int32: sequence i is the tokens seq_start[i] .. seq_start[i + 1] - 1; the values of tokens outside
+    do not matter, and they get +0.  q, k and v may be views with any strides of rows and heads.
     scale=None: 1 / sqrt(d).  grads=False leaves the backward out.
     """
 
@@ -499,15 +500,22 @@ class PackedAttention(_Owned):
                              _CODES[self.dtype], q, k, v, seq_start, self.scale, self.o, self.lse, on)
         return self.o, self.lse
 
-    def backward(self, q, k, v, seq_start, do, stream=None):
+    def backward(self, q, k, v, seq_start, do, stream=None, o=None, lse=None):
         if self.dqkv is None:
             raise ValueError("agrl: this PackedAttention was made with grads=False")
+        if (o is None) != (lse is None):
+            raise ValueError("agrl: o and lse of one forward belong together")
         self._check(q, k, v, seq_start)
         self._need(do, "do", (self.T, self.n_head, self.d), (self.dtype,))
+        if o is not None:
+            self._need(o, "o", (self.T, self.n_head, self.d), (self.dtype,))
+            self._need(lse, "lse", (self.n_head, self.T), (torch.float32,))
         on = self._order(stream)
         if on is None:
-            return self._there(self.backward, q, k, v, seq_start, do, stream)
+            return self._there(self.backward, q, k, v, seq_start, do, stream, o, lse)
+        if o is None:
+            o, lse = self.o, self.lse
         B.agrl_attention_bwd(self.T, seq_start.numel() - 1, self.n_head, self.n_kv, self.d,
-                             _CODES[self.dtype], q, k, v, seq_start, self.scale, self.o, self.lse, do,
+                             _CODES[self.dtype], q, k, v, seq_start, self.scale, o, lse, do,
                              self.workspace, self.ws_bytes, self.dq, self.dk, self.dv, on)
         return self.dq, self.dk, self.dv
