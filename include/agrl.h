@@ -464,7 +464,7 @@ size_t agrl_token_embed_bwd_workspace_size(int64_t T, int32_t d, int32_t V);
 /*
  * Gradient of the embedding: dweight[v] = scale * sum of dy[n] over the live tokens n with
  * token_id[n] = v, in the tokens' order, in fp32.
- *   V                 <= 2^31 - 1024; ceil(T / 32) ceil(d / 1024) (T <= 512: T of them), and ceil(V / 8) with accumulate 0,
+ *   V                 <= 2^31 - 1024; ceil(T / 32) ceil(d / 1024) (T <= 256: T of them), and ceil(V / 8) with accumulate 0,
  *                     below 2^24 together
  *   dy[T, d]          in dy_dtype, rows ld_dy >= d elements apart, from any element
  *   accumulate        0: every row of dweight is written (0 where no token has its id); 1: the

@@ -17,7 +17,7 @@
 //         is added by as many workgroups).  The rows of ids that do not occur are cleared by
 //         further workgroups of the same launch.
 //   join  adds the pieces of each crossing run in order.
-// Up to 512 tokens one launch does it all (embed_few_kernel).
+// Up to 256 tokens one launch does it all (embed_few_kernel).
 //
 // Measured (MI355X; a copy of 2 GiB moves 4.9 TB/s, a fill 6.9): forward of 65536 x 5120 bf16 out of [152064, 5120]
 // 213 us (6.2 TB/s of rows, the repeated ones from the caches).  Backward of the same, the whole gradient written,
@@ -350,8 +350,11 @@ int chunk_of(int64_t T, int32_t d) {
 
 // Few tokens: one launch, no sort.  A workgroup per token and slab of columns looks all ids over: the first token of an
 // id adds up those that follow, the others leave.  Workgroups behind them clear the rows of absent ids.
-// [4096, 256], added to: 8 tokens 6.7 us, 256 9.4, 512 15.7; 520 by the sort 18.2.
-constexpr int FEW = 512;
+// Added to [V, d] in bf16, here and by the sort: a text's ids, [4096, 256] 64 tokens 7.3 and 13.6 us, 256 7.7 and 15.4, 512
+// 16.5 and 16.7; [4096, 1001] 256 10.6 and 17.5, 512 26 and 19; [4096, 8192] 256 8.9 and 16, 512 19 and 18.  What it is slow at is
+// one id in every token, whose rows one workgroup a slab adds up: 64 tokens 14 to 20 and 15 us, 256 47 to 76 and 15 to 18
+// (512: 150 and 21).
+constexpr int FEW = 256;
 template <typename Y, bool ADD>
 __global__ void __launch_bounds__(256) embed_few_kernel(SortArgs t, RowsArgs a) {
   const int T = (int)t.T, adding = T * a.slabs, lane = threadIdx.x & 63, wave = threadIdx.x >> 6;

@@ -106,3 +106,11 @@ def test_repeats_and_replays():
         eager.backward(ids, dy)
         torch.cuda.synchronize()
         assert torch.equal(op.dweight, eager.dweight)
+
+
+@pytest.mark.parametrize("T", [255, 256, 257, 511, 512, 513])
+@pytest.mark.parametrize("kind", ["same", "all", "text"])
+def test_around_the_one_launch(T, kind):
+    """Up to 256 tokens go without the sort."""
+    _grad(T, 300, 700, F32, kind=kind, mask="some")
+    _grad(T, 1025, 90, BF, kind=kind, accumulate=True, pitch=5)
