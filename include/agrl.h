@@ -463,7 +463,7 @@ size_t agrl_token_embed_bwd_workspace_size(int64_t T, int32_t d, int32_t V);
 
 /*
  * Gradient of the embedding: dweight[v] = scale * sum of dy[n] over the live tokens n with
- * token_id[n] = v, in the tokens' order, in fp32.
+ * token_id[n] = v, in fp32, in an order that the ids fix.
  *   V                 <= 2^31 - 1024; ceil(T / 32) ceil(d / 1024) (T <= 256: T of them), and ceil(V / 8) with accumulate 0,
  *                     below 2^24 together
  *   dy[T, d]          in dy_dtype, rows ld_dy >= d elements apart, from any element

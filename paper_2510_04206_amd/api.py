@@ -358,7 +358,7 @@ class TokenEmbedding(_Owned):
     """Embedding of T packed token ids, rows of a [V, d] weight (agrl_token_embed_*).
 
     ``forward`` returns y [T, d] = scale weight[token_id], in ``dtype`` whatever the weight's type (w_dtype,
-    by default the same).  ``backward`` adds up dy's rows by id, in the tokens' order, into ``dweight`` [V, d]
+    by default the same).  ``backward`` adds up dy's rows by id, in a fixed order, into ``dweight`` [V, d]
     fp32: its own, or the one given (a tied head's: ``dweight=loss.dW`` and accumulate=True).  Tokens whose
     live_mask is 0 are not read: y is +0 there, dy goes nowhere.  grads=False leaves the backward out.
     """

@@ -22,10 +22,15 @@
 // Kernels: att_fwd, att_dq and att_dkv serve every case with one simple loop; the pipelined ones further down serve bf16
 // with heads of whole 16-byte chunks, wherever those can be copied 16 bytes at a time.
 //
-// Measured (MI355X, bf16; a large library product reaches 1.6 PFLOP/s): forward of 32768 tokens, 40 heads over 8
-// of 128, in sequences of 26524 and 6244, 6.4 to 6.7 ms, 1.14 to 1.19 PFLOP/s, matrix cores busy 0.59 at 1.81 GHz (the power
-// limit); of 28 heads over 4, in ten sequences around 3400, 1.0 ms, 0.9 PFLOP/s.  Backward of 16384 tokens of the
-// latter in five, 2.0 ms: dk and dv 1.24, dq 0.74 (0.58 PFLOP/s counting five products; seven are formed).  The
+// P, and dS in the backward, meet v, dout, k and q in the inputs' type, the matrix core's operand: in bf16 each is off by 2^-8 of
+// itself at most (o by 1.6e-3 to 2.2e-3 of its norm, gradients by up to 2.3e-3, measured; their own rounding alone is 1.6e-3).
+// Keeping 16 bits of them takes two products for one, a third to a half more matrix-core time in kernels that it bounds.
+//
+// Measured (MI355X, bf16; a large library product reaches 1.6 PFLOP/s; the lower times over hundreds of calls in a row, the
+// higher ones in a trace of the first dozen): forward of 32768 tokens, 40 heads over 8
+// of 128, in sequences of 26524 and 6244, 6.4 to 6.8 ms, 1.12 to 1.19 PFLOP/s, matrix cores busy 0.59 at 1.83 GHz (the power
+// limit); of 28 heads over 4, in ten sequences around 3400, 0.99 to 1.18 ms, 0.9 PFLOP/s at best.  Backward of 16384 tokens of the
+// latter in five, 2.0 to 2.1 ms: dk and dv 1.26 to 1.3, dq 0.74 (0.58 PFLOP/s counting five products; seven are formed).  The
 // simple loops took 17.9, 2.15 and 10.4 ms: their registers spill, and every fragment read is waited for.
 #include <math.h>
 
@@ -484,7 +489,8 @@ __global__ void __launch_bounds__(THREADS, sizeof(T) == 2 ? 2 : 1) att_fwd_kerne
   __shared__ __align__(16) uint8_t lds_k[2][R * TL::ROW], lds_v[2][R * TL::ROW];
   __shared__ int lds_span[2][WAVES];
   if (a.err) check_offsets(a.start, a.n_seq, a.T, a.err);
-  // the longest ranges first; a key head's query heads on one XCD (8 in turn) as far as the numbers allow
+  // the stream's last tiles first (of one sequence: the longest ranges); a key head's query heads on one XCD (8 in turn) as far
+  // as the numbers allow
   const int tiles = (a.T + BM - 1) / BM;
   const int tile = tiles - 1 - blockIdx.x / a.n_head, j = blockIdx.x % a.n_head;
   const int kv = j % a.n_kv, head = kv * a.rep + j / a.n_kv;
@@ -1816,9 +1822,16 @@ int att_strides(const char* fn, int64_t ld, int64_t hs) {
   return ld < 0 || hs < 0 ? fail(AGRL_E_SHAPE, fn, "a stride is negative") : AGRL_OK;
 }
 
-// Parts that the heads of a group are dealt to where the key tiles do not fill the chip.  1519 tokens of 4 heads over 2 in
-// fp32, 24 key tiles: dk and dv 73 us in one part, 42 in two and 5 to join them.  Where they do fill it a part costs more
-// than it evens out: 8191 tokens of 16 heads over 4 in short sequences, 256 key tiles, 45 us in one, 91 in four.
+// Parts that the heads of a group are dealt to where the key tiles alone do not fill the chip's 256 units.  How long a tile is
+// the host does not know: long ones gain, tiles of short sequences have little to share out and pay for the join.  Whole
+// backward, by this rule and in one part:
+//                                         one sequence      four             of 33 tokens
+//   1519 tokens, 4/2 heads of 64 fp32     444 and 671 us    259 and 392      75 and 97
+//   2048, 16/2 of 128 bf16 (8 parts)      171 and 518       118 and 283      77 and 104
+//   4096, 28/4 of 128 (2 parts)           636 and 919       348 and 487      136 and 138
+//   7168, 28/4 of 128 (2 parts)           1352 and 1790     659 and 887      241 and 200
+// Where the tiles do fill it a part costs more than it evens out: 8191 tokens of 16 heads over 4 in short sequences, 256 key
+// tiles, dk and dv 45 us in one, 91 in four.
 int att_splits(int64_t T, int32_t n_head, int32_t n_kv) {
   const int64_t items = cdiv(T, (int64_t)BM) * n_kv, want = cdiv((int64_t)256, items), rep = n_head / n_kv;
   return (int)(want < rep ? want : rep);

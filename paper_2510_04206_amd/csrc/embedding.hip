@@ -1,7 +1,7 @@
 // Embedding of a packed stream of token ids, and its gradient by sorted tokens (gfx950).
 //
 //   forward   y[n] = scale W[id[n]]
-//   backward  dW[v] (+)= scale * sum over tokens n with id[n] = v of dy[n], n ascending
+//   backward  dW[v] (+)= scale * sum over tokens n with id[n] = v of dy[n], in an order that depends on the ids alone
 //
 // Forward: a wave copies up to 2048 elements of a row.  Memory bounds it.
 //
@@ -16,7 +16,7 @@
 //         another chunk to a partial sum (a separator's run is thousands of tokens: it
 //         is added by as many workgroups).  The rows of ids that do not occur are cleared by
 //         further workgroups of the same launch.
-//   join  adds the pieces of each crossing run in order.
+//   join  adds the pieces of each crossing run: every fourth one in turn, then the four sums.
 // Up to 256 tokens one launch does it all (embed_few_kernel).
 //
 // Measured (MI355X; a copy of 2 GiB moves 4.9 TB/s, a fill 6.9): forward of 65536 x 5120 bf16 out of [152064, 5120]
@@ -314,7 +314,7 @@ __global__ void __launch_bounds__(256) embed_rows_kernel(RowsArgs a) {
   }
 }
 
-// The runs that cross: their pieces in order, 256 columns a workgroup, its four waves every fourth piece.
+// The runs that cross, 256 columns a workgroup: each of its four waves every fourth piece in order, then the four sums.
 __global__ void __launch_bounds__(256) embed_join_kernel(RowsArgs a) {
   constexpr int COLS = 256;
   __shared__ f32x4 sums[3][64];

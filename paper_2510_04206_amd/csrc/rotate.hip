@@ -6,7 +6,8 @@
 //
 // Memory bounds it: each head is read and written once.  A lane keeps its place in a head (8
 // elements of each half, or of four pairs) over all tokens and heads it meets, so its frequencies are
-// formed once, and a token's angles once for all of its heads.  The angle is counted in turns in 64
+// formed once, and a token's angles once for the heads that it takes of it (a workgroup has 256 lanes, 32 heads of
+// 128, and goes through the rest).  The angle is counted in turns in 64
 // bits (position 2^20: what 32 bits would leave of it is off by 0.06 radians) and its fraction
 // is rounded to 32, where sine and cosine are taken.
 //
