@@ -23,8 +23,9 @@
 // with heads of whole 16-byte chunks, wherever those can be copied 16 bytes at a time.
 //
 // P, and dS in the backward, meet v, dout, k and q in the inputs' type, the matrix core's operand: in bf16 each is off by 2^-8 of
-// itself at most (o by 1.6e-3 to 2.2e-3 of its norm, gradients by up to 2.3e-3, measured; their own rounding alone is 1.6e-3).
-// Keeping 16 bits of them takes two products for one, a third to a half more matrix-core time in kernels that it bounds.
+// itself at most.  Against 64 bits, of a tensor's norm: o 2.2e-3 to 2.3e-3, with 32-bit weights 1.6e-3 (all of it o's own
+// rounding); gradients of packed 16k 2.8e-3 and 2.0e-3, of short sequences 3.2e-3 and 2.6e-3.  Keeping 16 bits of them would
+// take two products for one, a third to a half more matrix-core time in kernels that it bounds.
 //
 // Measured (MI355X, bf16; a large library product reaches 1.6 PFLOP/s; the lower times over hundreds of calls in a row, the
 // higher ones in a trace of the first dozen): forward of 32768 tokens, 40 heads over 8
@@ -51,8 +52,9 @@ constexpr float LOG2E = 1.44269504088896341f, LN2 = 0.693147180559945309f;
 // Scores past some 2^24 are many units apart in fp32, and an exponent formed from two roundings of one score is off by as
 // much.  Such rows therefore subtract before they scale in the forward (the largest weight is exactly 1), their lse is scale m
 // + ln l, rounded once, and the backward takes S with the same rounding: where one key is all of a row,
-// S is the lse and the weight 1.  (No weight is above 1: both roundings are of growing functions.)  Up to FAR powers of 2
-// one fused operation does: it is off by 3 FAR 2^-24 = 2^-10.4 of a weight at most, less than a bf16 weight's rounding.
+// S is the lse and the weight 1.  (And a row's largest S is not above its lse: both roundings are of growing functions.)  Up
+// to FAR powers of 2 one fused operation does: it is off by 3 FAR 2^-24 = 2^-10.4 of a weight at most, less than a bf16
+// weight's rounding.
 constexpr float FAR = 4096.0f;
 __device__ __forceinline__ float row_lse(float m, float scale, float l) {
   return fmaf(m, scale, LN2 * __builtin_amdgcn_logf(l));
@@ -603,8 +605,9 @@ __global__ void __launch_bounds__(THREADS, sizeof(T) == 2 ? 2 : 1) att_fwd_kerne
 // there is no running maximum to follow.  Weights may grow to 2^96 before that fails (scores 66 above the row's own);
 // then, or where a result is not finite (a NaN or infinite element of V met a weight of 0, or a weight times a large one
 // left the range), the workgroup goes through its tile again step by step, masked elements taken out.  There a row whose
-// sum had left its range, or whose own score is past FAR, follows its maximum.  Any other keeps its reference: its results have the bits of the first pass, and
-// where they were not finite its weights are taken down by the power of 2 of its sum, which changes no mantissa.
+// sum had left its range, or whose own score is past FAR, follows its maximum.  Any other keeps its reference: its results have
+// the bits of the first pass, and where they were not finite its weights are taken down by the power of 2 of its sum, which
+// changes no mantissa.
 constexpr int PIPE_ROWS = 64 * WAVES;
 
 template <int N, class F>
