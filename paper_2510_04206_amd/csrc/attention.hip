@@ -28,11 +28,11 @@
 // take two products for one, a third to a half more matrix-core time in kernels that it bounds.
 //
 // Measured (MI355X, bf16; a large library product reaches 1.6 PFLOP/s; the lower times over hundreds of calls in a row, the
-// higher ones in a trace of the first dozen): forward of 32768 tokens, 40 heads over 8
-// of 128, in sequences of 26524 and 6244, 6.4 to 6.8 ms, 1.12 to 1.19 PFLOP/s, matrix cores busy 0.59 at 1.83 GHz (the power
-// limit); of 28 heads over 4, in ten sequences around 3400, 0.99 to 1.18 ms, 0.9 PFLOP/s at best.  Backward of 16384 tokens of the
-// latter in five, 2.0 to 2.1 ms: dk and dv 1.26 to 1.3, dq 0.74 (0.58 PFLOP/s counting five products; seven are formed).  The
-// simple loops took 17.9, 2.15 and 10.4 ms: their registers spill, and every fragment read is waited for.
+// higher ones in traces of a first dozen, while the clock settles): forward of 32768 tokens, 40 heads over 8 of 128, in
+// sequences of 26524 and 6244, 6.4 to 6.9 ms, 1.10 to 1.19 PFLOP/s, matrix cores busy 0.59 at 1.8 GHz (the power limit); of 28
+// heads over 4, in ten sequences around 3400, 0.99 to 1.19 ms, 0.9 PFLOP/s at best.  Backward of 16384 tokens of the latter
+// in five, 2.0 to 2.1 ms: dk and dv 1.26 to 1.30, dq 0.74 to 0.76 (0.58 PFLOP/s counting five products; seven are formed).
+// The simple loops took 17.9, 2.15 and 10.4 ms: their registers spill, and every fragment read is waited for.
 #include <math.h>
 
 #include <type_traits>

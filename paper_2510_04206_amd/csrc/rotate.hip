@@ -11,7 +11,7 @@
 // bits (position 2^20: what 32 bits would leave of it is off by 0.06 radians) and its fraction
 // is rounded to 32, where sine and cosine are taken.
 //
-// Measured (MI355X; a copy of 2 GiB moves 4.9 TB/s): 65536 tokens, 48 of 56 heads of 128 bf16, 352 us, 4.6 TB/s; 150
+// Measured (MI355X; a copy of 2 GiB moves 4.9 TB/s): 65536 tokens, 48 of 56 heads of 128 bf16, 351 us, 4.6 TB/s (a first dozen 371); 150
 // tokens, 12 heads of 64 fp32, 3.5 us on the GPU, 7.7 from Python.
 #include <math.h>
 
